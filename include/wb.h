@@ -60,7 +60,11 @@ typedef enum {
   WB_ERR_REPLICA_MISMATCH = 13 /* two trainer replicas of a checkpoint region differ          */
 } wb_status;
 
-typedef enum { WB_F32 = 0, WB_BF16 = 1 } wb_dtype;
+typedef enum {
+  WB_F32 = 0,
+  WB_BF16 = 1,
+  WB_E4M3 = 2 /* key/value caches only (wb_kv_open); layouts, rows and outputs refuse it */
+} wb_dtype;
 
 /* One local tensor of a virtual rank (a flat array of `numel` elements). */
 typedef struct {
@@ -576,6 +580,130 @@ wb_status wb_scan_slices(const wb_diff2_entry* nz, size_t n, uint64_t rows, uint
                          const uint64_t* ckpt_base, const uint64_t* ckpt_rows, const uint64_t* ckpt_cols,
                          size_t n_ckpt, uint32_t tensor, uint64_t elem_off, wb_slice* out, size_t cap,
                          size_t* n_out);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rollout step: paged key/value cache, attention over it, verification of drafted tokens.
+ *
+ * What a rollout engine runs on the remapped weights between two updates: the fused qkv_proj
+ * yields the new tokens' queries, keys and values; wb_kv_write appends the keys and values to a
+ * paged cache, wb_kv_attend lets the new tokens attend over everything the cache holds of their
+ * sequence, wb_kv_read copies rows back out, and wb_verify_drafts accepts or rejects the tokens a
+ * drafter proposed.  All calls are asynchronous on the given stream, allocate nothing, copy
+ * nothing between host and device, and can be captured in a CUDA graph.
+ *
+ * The cache.  Keys and values each live in n_pages pages of page_size slots; the rows (head_dim
+ * elements) of one (page, head) are contiguous: slot s of head h in page p starts at element
+ * p * page_stride + h * head_stride + s * head_dim.  A cache is bf16, or E4M3 codes with one fp32
+ * scale per row, scales contiguous as [n_pages][n_kv_heads][page_size]; the quantisation rule is
+ * that of wb_bucket_quantize with the row in the place of the checkpoint tensor: s = amax / 448
+ * (1 for a row of zeros, never zero otherwise), code = e4m3(x * (448 / amax)), saturating, or
+ * e4m3(x / s) where 448 / amax is not finite; the value of a code is code * s in fp32.
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+  uint32_t dtype;       /* WB_BF16 or WB_E4M3                                                    */
+  uint32_t n_kv_heads;
+  uint32_t head_dim;    /* 64 or 128                                                             */
+  uint32_t page_size;   /* slots per page: a multiple of 16, at most 65536                       */
+  uint64_t n_pages;     /* n_pages * n_kv_heads * page_size < 2^31 rows                          */
+  uint64_t page_stride; /* elements; multiples of 16, and of 16 bytes; < 2^39 bytes              */
+  uint64_t head_stride;
+  void* k;              /* device, 16-byte aligned                                               */
+  void* v;              /* device, 16-byte aligned; same strides as k                            */
+  float* k_scale;       /* device; E4M3 caches only, NULL for bf16                               */
+  float* v_scale;
+} wb_kv_desc;
+
+typedef struct wb_kv wb_kv;
+
+/* Validates a cache's description and encodes its tensor maps (host memory only; nothing of the
+ * cache is read or written).  The handle stays valid while the cache's memory does. */
+wb_status wb_kv_open(const wb_kv_desc* desc, wb_kv** out);
+void wb_kv_free(wb_kv* kv);
+
+/* A step's batch.  Sequence b's cache rows are found through row b of page_table: position t is in
+ * slot t % page_size of page page_table[b][t / page_size].  After the step the cache holds kv_len[b]
+ * tokens of it; the last new_start[b+1] - new_start[b] of them are the new ones, which are rows
+ * [new_start[b], new_start[b+1]) of the step's tensors.  max_new and max_len are the host's upper
+ * bounds on a sequence's new tokens and on kv_len (they size the launch; a loose max_len only costs
+ * blocks that end at once, results beyond a max_new that is too small are not computed).  A position
+ * that the table does not cover, or whose page is not in [0, n_pages), is not written, reads as zeros
+ * and is attended over as zeros: table entries past a sequence's last page may hold anything. */
+typedef struct {
+  uint32_t n_seqs;            /* at most WB_KV_MAX_SEQS                                            */
+  uint32_t n_tokens;          /* rows of the step's tensors                                        */
+  uint32_t max_new, max_len;
+  uint32_t table_stride;      /* entries per row of page_table                                     */
+  uint32_t reserved;          /* must be 0                                                         */
+  const int32_t* page_table;  /* device, n_seqs x table_stride                                     */
+  const int32_t* new_start;   /* device, n_seqs + 1, non-decreasing, new_start[0] = 0              */
+  const int32_t* kv_len;      /* device, n_seqs                                                    */
+} wb_kv_batch;
+#define WB_KV_MAX_SEQS 4096u
+
+/* A step's tensor [n_tokens][heads][head_dim]; row t of head h starts at element
+ * t * token_stride + h * head_stride.  data and both strides are multiples of 16 bytes, so slices of a
+ * fused projection's output can be passed as they are. */
+typedef struct {
+  void* data;            /* device */
+  uint32_t dtype;        /* WB_F32 or WB_BF16 */
+  uint32_t reserved;     /* must be 0 */
+  uint64_t token_stride;
+  uint64_t head_stride;
+} wb_heads;
+
+/* Append the batch's new keys and values to the cache (rounded to bf16, or quantised).  Two tokens
+ * must not share a slot. */
+wb_status wb_kv_write(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* k, const wb_heads* v,
+                      void* cuda_stream);
+/* The inverse: the cache's rows of the batch's "new" positions -> k, v.  With new_start the running
+ * sum of kv_len the whole of every sequence is read. */
+wb_status wb_kv_read(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* k, const wb_heads* v,
+                     void* cuda_stream);
+
+/* Attention of the new tokens over the cache (their own keys and values already written):
+ *   out[t, h] = sum_j softmax_j(scale * q[t, h] . K[j, g]) V[j, g],   g = h / (n_heads / n_kv_heads),
+ * over the positions j <= pos(t) of t's sequence, with window > 0 only those with j > pos(t) - window.
+ * lse[t, h] (fp32, contiguous [n_tokens][n_heads], may be NULL) is the natural logarithm of the
+ * softmax's denominator.  A row with nothing to attend over gives zeros and lse = -inf; what masked
+ * slots and unused parts of pages hold does not matter (NaN included).  q and out are bf16;
+ * n_heads is a multiple of n_kv_heads, n_heads / n_kv_heads at most 64, and scale is positive and finite.
+ * workspace: wb_kv_attend_workspace_bytes device bytes, 256-byte aligned, zeroed once by the caller
+ * before its first use; it carries nothing from call to call, and calls that may overlap need one each. */
+wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* q, uint32_t n_heads,
+                       const wb_heads* out, float* lse, float scale, uint32_t window, void* workspace,
+                       size_t workspace_bytes, void* cuda_stream);
+size_t wb_kv_attend_workspace_bytes(const wb_kv* kv, uint32_t n_heads, uint32_t n_seqs);
+
+/* Verification of drafted tokens.  Sequence b drafted K = draft_start[b+1] - draft_start[b] tokens
+ * x_0 .. x_{K-1} (K may be 0; at most max_drafts count), which are entries draft_start[b] + i of draft_tokens.
+ * Row draft_start[b] + b + i of target holds the target's probabilities p_i for i = 0 .. K; row
+ * draft_start[b] + i of draft the drafter's q_i.  Token x_i is accepted if all before it are and
+ *   uniform[i] * q_i(x_i) < p_i(x_i)      (fp32 product; false for NaN and for x_i outside the vocabulary).
+ * With a the number accepted, one more token is drawn: by the exponential race
+ *   argmax_v w(v) / race[b][v]   (fp32 division; the lowest index of equal ones)
+ * from w = max(p_a - q_a, 0) if x_a was rejected, and from w = p_K if all were accepted.  If no w(v) is
+ * positive, w = p_a is used.  With race[b][v] independent Exp(1) variates and uniform in [0, 1) the
+ * emitted tokens are distributed as the target's own.  draft = NULL means a drafter that proposes one
+ * token with certainty (q one-hot at x_i).  accepted[b] = a; tokens[b][0 .. a] are the accepted tokens
+ * and the drawn one, tokens[b][a + 1 ..] = -1.  Probabilities are fp32 or bf16, rows `*_stride` elements
+ * apart; no alignment beyond the element's is needed. */
+typedef struct {
+  uint32_t n_seqs, vocab, max_drafts;
+  uint32_t dtype;               /* of target and draft: WB_F32 or WB_BF16                        */
+  uint32_t n_drafts;            /* drafted tokens of all sequences: entries of draft_tokens and uniform, rows of
+                                   draft; target has n_drafts + n_seqs rows                       */
+  uint32_t reserved;            /* must be 0 */
+  const void* target;           /* device */
+  const void* draft;            /* device or NULL */
+  uint64_t target_stride, draft_stride, race_stride;
+  const int32_t* draft_tokens;  /* device; may be NULL if n_drafts is 0  */
+  const int32_t* draft_start;   /* device, n_seqs + 1 */
+  const float* uniform;         /* device; may be NULL if n_drafts is 0  */
+  const float* race;            /* device, n_seqs rows */
+  int32_t* accepted;            /* device, n_seqs */
+  int32_t* tokens;              /* device, n_seqs x (max_drafts + 1) */
+} wb_verify_args;
+wb_status wb_verify_drafts(const wb_verify_args* args, void* cuda_stream);
 
 /* Number of kernels wb_remap / wb_pack / wb_unpack launch per call (always 1). */
 int wb_launches_per_call(void);

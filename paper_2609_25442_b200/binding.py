@@ -15,7 +15,7 @@ import numpy as np
 from . import build as _build
 
 WB_OK = 0
-WB_F32, WB_BF16 = 0, 1
+WB_F32, WB_BF16, WB_E4M3 = 0, 1, 2
 WB_TABLE_REMAP, WB_TABLE_PACK, WB_TABLE_UNPACK = 0, 1, 2
 WB_TILE_FANOUT_CONT = 1
 WB_PLAN_NO_REPLICA_SPLIT = 1
@@ -48,6 +48,32 @@ class wb_slice(C.Structure):
                 ("stride_r", C.c_int64), ("stride_c", C.c_int64),
                 ("ckpt_tensor", C.c_uint64), ("ckpt_rows", C.c_uint64), ("ckpt_cols", C.c_uint64),
                 ("r0", C.c_uint64), ("c0", C.c_uint64), ("nr", C.c_uint64), ("nc", C.c_uint64)]
+
+
+class wb_kv_desc(C.Structure):
+    _fields_ = [("dtype", C.c_uint32), ("n_kv_heads", C.c_uint32), ("head_dim", C.c_uint32), ("page_size", C.c_uint32),
+                ("n_pages", C.c_uint64), ("page_stride", C.c_uint64), ("head_stride", C.c_uint64),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class wb_kv_batch(C.Structure):
+    _fields_ = [("n_seqs", C.c_uint32), ("n_tokens", C.c_uint32), ("max_new", C.c_uint32), ("max_len", C.c_uint32),
+                ("table_stride", C.c_uint32), ("reserved", C.c_uint32),
+                ("page_table", C.c_void_p), ("new_start", C.c_void_p), ("kv_len", C.c_void_p)]
+
+
+class wb_heads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_uint32), ("reserved", C.c_uint32),
+                ("token_stride", C.c_uint64), ("head_stride", C.c_uint64)]
+
+
+class wb_verify_args(C.Structure):
+    _fields_ = [("n_seqs", C.c_uint32), ("vocab", C.c_uint32), ("max_drafts", C.c_uint32), ("dtype", C.c_uint32),
+                ("n_drafts", C.c_uint32), ("reserved", C.c_uint32),
+                ("target", C.c_void_p), ("draft", C.c_void_p),
+                ("target_stride", C.c_uint64), ("draft_stride", C.c_uint64), ("race_stride", C.c_uint64),
+                ("draft_tokens", C.c_void_p), ("draft_start", C.c_void_p), ("uniform", C.c_void_p), ("race", C.c_void_p),
+                ("accepted", C.c_void_p), ("tokens", C.c_void_p)]
 
 
 class wb_plan_opts(C.Structure):
@@ -86,6 +112,7 @@ EXPORTS = [
     "wb_plan_num_ckpts", "wb_plan_ckpt_ids", "wb_plan_qbucket_bytes", "wb_absmax", "wb_bucket_quantize",
     "wb_bucket_dequantize", "wb_transfer_rounds_fp8", "wb_pack_fp8", "wb_unpack_fp8", "wb_transfer_rounds_fp8_fused",
     "wb_diff2_nonzeros", "wb_diff2_nonzeros_batch", "wb_diff2_batch_scratch_bytes", "wb_diff2_recombine", "wb_diff2_chunk_pass", "wb_diff2_chunk_scratch_bytes", "wb_scan_slices", "wb_route_account", "wb_wait_probe", "wb_plan_check_replicas", "wb_launches_per_call", "wb_status_str", "wb_version",
+    "wb_kv_open", "wb_kv_free", "wb_kv_write", "wb_kv_read", "wb_kv_attend", "wb_kv_attend_workspace_bytes", "wb_verify_drafts",
 ]
 
 _lib: Optional[C.CDLL] = None
@@ -152,6 +179,15 @@ def load() -> C.CDLL:
     lib.wb_diff2_recombine.argtypes = [vp, vp, sz, C.c_uint32, vp, sz, C.POINTER(sz)]
     lib.wb_scan_slices.argtypes = [vp, sz, C.c_uint64, C.c_uint64, vp, vp, vp, sz, C.c_uint32, C.c_uint64,
                                    vp, sz, C.POINTER(sz)]
+    lib.wb_kv_open.argtypes = [C.POINTER(wb_kv_desc), C.POINTER(vp)]
+    lib.wb_kv_free.argtypes = [vp]
+    lib.wb_kv_free.restype = None
+    lib.wb_kv_write.argtypes = [vp, vp, vp, vp, vp]
+    lib.wb_kv_read.argtypes = [vp, vp, vp, vp, vp]
+    lib.wb_kv_attend.argtypes = [vp, vp, vp, C.c_uint32, vp, vp, C.c_float, C.c_uint32, vp, sz, vp]
+    lib.wb_kv_attend_workspace_bytes.argtypes = [vp, C.c_uint32, C.c_uint32]
+    lib.wb_kv_attend_workspace_bytes.restype = sz
+    lib.wb_verify_drafts.argtypes = [vp, vp]
     lib.wb_launches_per_call.restype = C.c_int
     lib.wb_status_str.argtypes = [C.c_int]
     lib.wb_status_str.restype = C.c_char_p
@@ -506,3 +542,37 @@ def wb_route_account(plan: Plan, trainer_node: Sequence[int], rollout_node: Sequ
 def wb_wait_probe(limit_ms: int, stream: int = 0) -> int:
     """Returns the raw status: WB_ERR_INTERNAL (11) means the bounded wait gave up as designed."""
     return load().wb_wait_probe(limit_ms, stream)
+
+
+# ---- rollout step ---------------------------------------------------------------------------------
+class Kv:
+    """Owns a wb_kv* (a validated paged cache); all pointers are device."""
+
+    def __init__(self, desc: wb_kv_desc):
+        lib = load()
+        self.handle = C.c_void_p()
+        _check(lib.wb_kv_open(C.byref(desc), C.byref(self.handle)), "wb_kv_open")
+
+    def __del__(self):
+        if _lib is not None and getattr(self, "handle", None):
+            _lib.wb_kv_free(self.handle)
+            self.handle = None
+
+    def write(self, batch: wb_kv_batch, k: wb_heads, v: wb_heads, stream: int = 0) -> None:
+        _check(_lib.wb_kv_write(self.handle, C.byref(batch), C.byref(k), C.byref(v), stream), "wb_kv_write")
+
+    def read(self, batch: wb_kv_batch, k: wb_heads, v: wb_heads, stream: int = 0) -> None:
+        _check(_lib.wb_kv_read(self.handle, C.byref(batch), C.byref(k), C.byref(v), stream), "wb_kv_read")
+
+    def attend_workspace_bytes(self, n_heads: int, n_seqs: int) -> int:
+        return int(_lib.wb_kv_attend_workspace_bytes(self.handle, n_heads, n_seqs))
+
+    def attend(self, batch: wb_kv_batch, q: wb_heads, n_heads: int, out: wb_heads, lse_ptr: int, scale: float, window: int,
+               workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
+        _check(_lib.wb_kv_attend(self.handle, C.byref(batch), C.byref(q), n_heads, C.byref(out), lse_ptr, scale, window,
+                                 workspace_ptr, workspace_bytes, stream), "wb_kv_attend")
+
+
+def wb_verify_drafts(args: wb_verify_args, stream: int = 0) -> None:
+    load()
+    _check(_lib.wb_verify_drafts(C.byref(args), stream), "wb_verify_drafts")

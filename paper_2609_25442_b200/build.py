@@ -8,7 +8,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwb.so")
-SOURCES = ["wb_layout.cpp", "wb_plan.cpp", "wb_exec.cu", "wb_extract.cu", "wb_scan.cpp", "wb_quant.cu"]
+SOURCES = ["wb_layout.cpp", "wb_plan.cpp", "wb_exec.cu", "wb_extract.cu", "wb_scan.cpp", "wb_quant.cu",
+           "wb_kv.cu", "wb_attend.cu", "wb_verify.cu"]
 
 
 def _nvcc() -> str:
@@ -31,7 +32,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     cmd = [_nvcc(), "-std=c++17", "-O3", "-lineinfo",
            "-gencode", "arch=compute_100a,code=sm_100a",
-           "-Xcompiler", "-fPIC,-Wall,-Wno-unused-function", "-shared",
+           "--threads", "0", "-Xcompiler", "-fPIC,-Wall,-Wno-unused-function", "-shared",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC]
     if verbose:
         cmd += ["-Xptxas", "-v"]

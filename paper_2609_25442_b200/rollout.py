@@ -1,0 +1,182 @@
+"""A rollout engine's step on torch tensors: the paged key/value cache (written, read back, attended over)
+and the verification of drafted tokens.  The work is done by libwb.so; this module checks tensors,
+allocates results and passes torch's current stream.
+
+    cache = KvCache.empty(n_pages, n_kv_heads, page_size, head_dim, dtype=torch.float8_e4m3fn)
+    batch = KvBatch(page_table, new_start, kv_len, n_tokens=T, max_new=..., max_len=...)
+    cache.write(batch, k, v)                      # k, v: [T, n_kv_heads, head_dim], e.g. slices of qkv
+    out, lse = cache.attend(batch, q, workspace=AttendWorkspace(cache, n_heads, n_seqs))
+    accepted, tokens = verify_drafts(target, draft, draft_tokens, draft_start, uniform, race, max_drafts=K)
+"""
+from __future__ import annotations
+
+from typing import Optional, Tuple
+
+import torch
+
+from . import binding as wb
+
+_DTYPE = {torch.float32: wb.WB_F32, torch.bfloat16: wb.WB_BF16, torch.float8_e4m3fn: wb.WB_E4M3}
+_E4M3 = torch.float8_e4m3fn
+
+
+def _stream(device: torch.device) -> int:
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _require(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _ints(t: torch.Tensor, name: str, device: torch.device) -> torch.Tensor:
+    _require(t.dtype == torch.int32 and t.device == device, f"{name}: an int32 tensor on {device} is needed")
+    return t
+
+
+def _heads(t: torch.Tensor, name: str, n_tokens: int, heads: int, dim: int, device: torch.device) -> wb.wb_heads:
+    """A step's tensor [tokens, heads, dim] with contiguous rows, as the C ABI takes it."""
+    _require(t.dim() == 3 and t.shape[0] == n_tokens and t.shape[1] == heads and t.shape[2] == dim,
+             f"{name}: shape {tuple(t.shape)}, expected {(n_tokens, heads, dim)}")
+    _require(t.device == device and t.dtype in _DTYPE, f"{name}: {t.dtype} on {t.device}")
+    st, sh, se = t.stride()
+    _require(se == 1 and (st >= 0 and sh >= 0), f"{name}: rows must be contiguous")
+    return wb.wb_heads(t.data_ptr(), _DTYPE[t.dtype], 0, st, sh)
+
+
+class KvBatch:
+    """One step's sequences: `page_table` [n_seqs, pages] (a position's page), `new_start` [n_seqs + 1] (the rows of a
+    sequence's new tokens), `kv_len` [n_seqs] (tokens in the cache after the step), all int32 on the device.
+    `max_new` and `max_len` bound a sequence's new tokens and its length; they size the launches."""
+
+    def __init__(self, page_table: torch.Tensor, new_start: torch.Tensor, kv_len: torch.Tensor, *, n_tokens: int,
+                 max_new: Optional[int] = None, max_len: Optional[int] = None):
+        dev = kv_len.device
+        self.n_seqs = int(kv_len.shape[0])
+        self.n_tokens = int(n_tokens)
+        _require(page_table.dim() == 2 and page_table.shape[0] == self.n_seqs and (page_table.stride(1) == 1 or page_table.shape[1] <= 1),
+                 "page_table: [n_seqs, pages] with contiguous rows")
+        _require(new_start.shape == (self.n_seqs + 1,) and kv_len.dim() == 1 and new_start.is_contiguous() and kv_len.is_contiguous(),
+                 "new_start: [n_seqs + 1], kv_len: [n_seqs], contiguous")
+        _require(self.n_seqs <= 1 or page_table.shape[1] == 0 or page_table.stride(0) >= page_table.shape[1], "page_table: rows overlap")
+        # the C ABI knows one number for the pages of a row and the pitch of the table
+        if self.n_seqs > 1 and page_table.stride(0) != page_table.shape[1]:
+            page_table = page_table.contiguous()
+        self.page_table = _ints(page_table, "page_table", dev)
+        self.new_start, self.kv_len = _ints(new_start, "new_start", dev), _ints(kv_len, "kv_len", dev)
+        self.device = dev
+        most = int(page_table.shape[1]) if max_len is None else None
+        self._max_len, self._table_pages = max_len, most
+        self.args = wb.wb_kv_batch(self.n_seqs, self.n_tokens, min(self.n_tokens if max_new is None else int(max_new), self.n_tokens),
+                                   0 if max_len is None else int(max_len), int(page_table.shape[1]), 0,
+                                   self.page_table.data_ptr(), self.new_start.data_ptr(), self.kv_len.data_ptr())
+
+    def _for(self, cache: "KvCache") -> wb.wb_kv_batch:
+        if self._max_len is None:                       # the table's capacity bounds every length
+            self.args.max_len = self._table_pages * cache.page_size
+        return self.args
+
+
+class KvCache:
+    """Paged keys and values: `k`, `v` [n_pages, n_kv_heads, page_size, head_dim], bf16, or float8_e4m3fn with fp32
+    scales [n_pages, n_kv_heads, page_size].  The tensors stay the caller's; the cache keeps references to them."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        _require(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device,
+                 "k and v: the same shape [n_pages, n_kv_heads, page_size, head_dim], strides, type and device")
+        _require(k.is_cuda, "the cache needs a CUDA device (sm_100a)")
+        _require(k.dtype in (torch.bfloat16, _E4M3), f"cache of {k.dtype}: bfloat16 or float8_e4m3fn")
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = (int(x) for x in k.shape)
+        _require(k.stride(3) == 1 and k.stride(2) == self.head_dim, "a page's slots must be contiguous rows")
+        _require((k_scale is not None) == (v_scale is not None) == (k.dtype == _E4M3), "E4M3 caches, and no others, have scales")
+        for s in (k_scale, v_scale):
+            _require(s is None or (s.dtype == torch.float32 and s.is_contiguous() and s.shape == k.shape[:3] and s.device == k.device),
+                     "scales: contiguous fp32 [n_pages, n_kv_heads, page_size]")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device = k.device
+        self._kv = wb.Kv(wb.wb_kv_desc(_DTYPE[k.dtype], self.n_kv_heads, self.head_dim, self.page_size, self.n_pages,
+                                       k.stride(0), k.stride(1), k.data_ptr(), v.data_ptr(),
+                                       k_scale.data_ptr() if k_scale is not None else None,
+                                       v_scale.data_ptr() if v_scale is not None else None))
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, dtype: torch.dtype = torch.bfloat16,
+              device="cuda") -> "KvCache":
+        shape = (n_pages, n_kv_heads, page_size, head_dim)
+        k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+        if dtype != _E4M3:
+            return cls(k, v)
+        return cls(k, v, *(torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in range(2)))
+
+    def write(self, batch: KvBatch, k: torch.Tensor, v: torch.Tensor) -> None:
+        """Append the new tokens' keys and values (bf16 or fp32, [n_tokens, n_kv_heads, head_dim])."""
+        a = _heads(k, "k", batch.n_tokens, self.n_kv_heads, self.head_dim, self.device)
+        b = _heads(v, "v", batch.n_tokens, self.n_kv_heads, self.head_dim, self.device)
+        self._kv.write(batch._for(self), a, b, _stream(self.device))
+
+    def read(self, batch: KvBatch, dtype: torch.dtype = torch.bfloat16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
+        """Keys and values of the batch's positions, [n_tokens, n_kv_heads, head_dim] each."""
+        shape = (batch.n_tokens, self.n_kv_heads, self.head_dim)
+        k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device))
+        a = _heads(k, "out[0]", *shape, self.device)
+        b = _heads(v, "out[1]", *shape, self.device)
+        self._kv.read(batch._for(self), a, b, _stream(self.device))
+        return k, v
+
+    def attend(self, batch: KvBatch, q: torch.Tensor, *, workspace: "AttendWorkspace", scale: Optional[float] = None,
+               window: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+        """Attention of the new tokens' queries (bf16, [n_tokens, n_heads, head_dim]) over the cache, causal at the
+        sequences' ends; window > 0 limits a query to that many latest positions.  Returns (out, lse)."""
+        _require(q.dim() == 3, "q: [n_tokens, n_heads, head_dim]")
+        n, h = batch.n_tokens, int(q.shape[1])
+        a = _heads(q, "q", n, h, self.head_dim, self.device)
+        if out is None:
+            out = torch.empty((n, h, self.head_dim), dtype=torch.bfloat16, device=self.device)
+        if lse is None:
+            lse = torch.empty((n, h), dtype=torch.float32, device=self.device)
+        _require(lse.shape == (n, h) and lse.dtype == torch.float32 and lse.is_contiguous() and lse.device == self.device,
+                 "lse: contiguous fp32 [n_tokens, n_heads]")
+        b = _heads(out, "out", n, h, self.head_dim, self.device)
+        self._kv.attend(batch._for(self), a, h, b, lse.data_ptr(), self.head_dim ** -0.5 if scale is None else scale, window,
+                        workspace.buffer.data_ptr(), workspace.bytes, _stream(self.device))
+        return out, lse
+
+
+class AttendWorkspace:
+    """Scratch memory of KvCache.attend for up to `n_seqs` sequences; calls that may overlap need one each."""
+
+    def __init__(self, cache: KvCache, n_heads: int, n_seqs: int):
+        self.bytes = cache._kv.attend_workspace_bytes(n_heads, n_seqs)
+        _require(self.bytes > 0, f"no workspace for {n_heads} heads and {n_seqs} sequences over this cache")
+        self.buffer = torch.zeros(self.bytes, dtype=torch.uint8, device=cache.device)
+
+
+def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tokens: torch.Tensor, draft_start: torch.Tensor,
+                  uniform: torch.Tensor, race: torch.Tensor, *, max_drafts: int):
+    """Accept or reject drafted tokens against the target's probabilities and draw the token after them.
+
+    target [n_drafts + n_seqs, vocab], draft [n_drafts, vocab] or None (a drafter that is certain), draft_tokens and
+    uniform [n_drafts], draft_start [n_seqs + 1], race [n_seqs, vocab] (Exp(1) variates).  Returns (accepted [n_seqs],
+    tokens [n_seqs, max_drafts + 1], -1 beyond the drawn token), int32."""
+    dev = target.device
+    n, vocab, total = int(draft_start.shape[0]) - 1, int(target.shape[1]), int(draft_tokens.shape[0])
+    _require(target.is_cuda and target.dim() == 2 and n >= 0 and target.shape[0] == total + n and target.stride(1) == 1,
+             "target: [n_drafts + n_seqs, vocab] with contiguous rows on a CUDA device")
+    _require(target.dtype in (torch.float32, torch.bfloat16), f"probabilities of {target.dtype}: float32 or bfloat16")
+    _require(draft is None or (draft.shape == (total, vocab) and draft.dtype == target.dtype and draft.device == dev and draft.stride(1) == 1),
+             "draft: [n_drafts, vocab] of the target's type")
+    _require(uniform.shape == (total,) and uniform.dtype == torch.float32 and uniform.device == dev and uniform.is_contiguous(),
+             "uniform: fp32 [n_drafts]")
+    _require(race.shape == (n, vocab) and race.dtype == torch.float32 and race.device == dev and race.stride(1) == 1, "race: fp32 [n_seqs, vocab]")
+    _require(draft_tokens.is_contiguous() and draft_start.is_contiguous(), "draft_tokens, draft_start: contiguous")
+    _ints(draft_tokens, "draft_tokens", dev)
+    _ints(draft_start, "draft_start", dev)
+    accepted = torch.empty(n, dtype=torch.int32, device=dev)
+    tokens = torch.empty((n, max_drafts + 1), dtype=torch.int32, device=dev)
+    none = draft is None or total == 0
+    wb.wb_verify_drafts(wb.wb_verify_args(n, vocab, max_drafts, _DTYPE[target.dtype], total, 0, target.data_ptr(),
+                                          None if none else draft.data_ptr(), max(target.stride(0), vocab),
+                                          0 if none else max(draft.stride(0), vocab), max(race.stride(0), vocab),
+                                          draft_tokens.data_ptr(), draft_start.data_ptr(), uniform.data_ptr(), race.data_ptr(),
+                                          accepted.data_ptr(), tokens.data_ptr()), _stream(dev))
+    return accepted, tokens
