@@ -196,6 +196,33 @@ wb_status move_rows(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* k
   return cudaPeekAtLastError() == cudaSuccess ? WB_OK : (cudaGetLastError(), WB_ERR_CUDA);
 }
 
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+bool encode_map(const wb_kv_desc& d, void* base, uint32_t box_rows, CUtensorMap* out) {
+  void* fn = nullptr;
+  cudaDriverEntryPointQueryResult res = cudaDriverEntryPointSymbolNotFound;
+  if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &res) != cudaSuccess ||
+      res != cudaDriverEntryPointSuccess || !fn) {
+    (void)cudaGetLastError();
+    return false;
+  }
+  const bool q = d.dtype == WB_E4M3;
+  const uint64_t e = q ? 1 : 2;
+  const uint32_t width = std::min<uint32_t>(d.head_dim, 128 / (uint32_t)e);
+  const cuuint64_t dims[4] = {d.head_dim, d.page_size, d.n_kv_heads, d.n_pages};
+  // a stride of an extent of one is never used, but has to be a legal one
+  const uint64_t row = d.head_dim * e, head = d.n_kv_heads > 1 ? d.head_stride * e : row * d.page_size;
+  const uint64_t page = d.n_pages > 1 ? d.page_stride * e : head * d.n_kv_heads;
+  const cuuint64_t strides[3] = {row, head, page};
+  const cuuint32_t box[4] = {width, box_rows, 1, 1}, unit[4] = {1, 1, 1, 1};
+  return reinterpret_cast<EncodeTiledFn>(fn)(
+             out, q ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, unit,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, width * e == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace
 
 extern "C" wb_status wb_kv_open(const wb_kv_desc* d, wb_kv** out) {
@@ -215,10 +242,15 @@ extern "C" wb_status wb_kv_open(const wb_kv_desc* d, wb_kv** out) {
       (d->n_pages > 1 && d->page_stride < (uint64_t)(d->n_kv_heads - 1) * d->head_stride + (uint64_t)d->page_size * d->head_dim))
     return WB_ERR_INVALID_ARG;
   if ((d->dtype == WB_E4M3) != (d->k_scale != nullptr) || (d->dtype == WB_E4M3) != (d->v_scale != nullptr)) return WB_ERR_INVALID_ARG;
-  if (((uintptr_t)d->k_scale & 3u) || ((uintptr_t)d->v_scale & 3u)) return WB_ERR_INVALID_ARG;
+  if (((uintptr_t)d->k_scale & 15u) || ((uintptr_t)d->v_scale & 15u)) return WB_ERR_INVALID_ARG;
   wb_kv* kv = new (std::nothrow) wb_kv();
   if (!kv) return WB_ERR_OOM;
   kv->d = *d;
+  kv->box_rows = std::gcd(d->page_size, kKvTile);
+  if (!encode_map(kv->d, d->k, kv->box_rows, &kv->map_k) || !encode_map(kv->d, d->v, kv->box_rows, &kv->map_v)) {
+    delete kv;
+    return WB_ERR_CUDA;
+  }
   *out = kv;
   return WB_OK;
 }

@@ -11,8 +11,11 @@
 // The opaque handle: a validated description and the tensor maps of keys and values.
 struct wb_kv {
   wb_kv_desc d;
-  CUtensorMap map_k, map_v;   // 4-D (element, slot, head, page); box: 128 bytes (or a row, if shorter) x box_rows slots
-  uint32_t box_rows;          // rows of a tile that one page holds at least: gcd(page_size, kKvTile)
+  // 4-D maps (element, slot, head, page) with a box of 128 bytes (or a row, if shorter) x box_rows slots,
+  // swizzled for conflict-free matrix loads; box_rows = gcd(page_size, kKvTile), so a box never crosses
+  // a page, and coordinates outside the cache read as zeros
+  CUtensorMap map_k, map_v;
+  uint32_t box_rows;
 };
 
 namespace wbi {
@@ -39,10 +42,11 @@ struct KvBatch {
   const int32_t* new_start;
   const int32_t* kv_len;
   uint32_t n_seqs, n_tokens, table_stride;
+  int32_t max_len;
 };
 
 inline KvBatch kv_batch(const wb_kv_batch* b) {
-  return KvBatch{b->page_table, b->new_start, b->kv_len, b->n_seqs, b->n_tokens, b->table_stride};
+  return KvBatch{b->page_table, b->new_start, b->kv_len, b->n_seqs, b->n_tokens, b->table_stride, (int32_t)b->max_len};
 }
 
 inline wb_status check_batch(const wb_kv* kv, const wb_kv_batch* b) {

@@ -14,6 +14,12 @@ DEV = torch.device("cuda:0")
 E4M3 = torch.float8_e4m3fn
 
 
+def out_bound(want, mag):
+    """bf16 has eight significant bits: a rounding is off by at most 2^-8 of its value.  One of the result, one of every
+    softmax weight (it enters the second product as bf16; mag = sum_j w_j |v_j|), and fp32 sums."""
+    return 2.0 ** -8 * (1 + 2.0 ** -6) * (np.abs(want) + mag) + 1e-6
+
+
 class Case:
     """Sequences of the given lengths in a paged cache whose every unused byte is NaN, pages in random order, table
     entries past a sequence's end pointing at a page of NaN or nowhere."""
@@ -80,9 +86,8 @@ class Case:
         return out
 
     def check_attend(self, q, out, lse, window=0, scale=None, only=None):
-        """|out - exact| <= 2^-8 (1 + 2^-6) sum_j w_j |v_j| + 1e-6: half an ulp (2^-9) of bf16 for the result, as much for
-        every softmax weight, which enters the second product as bf16, and fp32 sums; lse within the fp32 error of a
-        dot product of D terms (D * 2^-24 of sum |q||k|, about 1e-5 of the largest score) and of exp2 / log."""
+        """|out - exact| <= out_bound, and lse within the fp32 error of a dot product of D terms (D * 2^-24 of
+        sum |q||k|, about 1e-5 of the largest score) and of exp2 / log."""
         scale = self.dim ** -0.5 if scale is None else scale
         o, l, qq = out.float().cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64), q.float().cpu().numpy()
         t = 0
@@ -91,7 +96,7 @@ class Case:
             want, wl, mag = orc.attend(qq[t:t + n], k, v, n, scale, window)
             if only is None or s in only:
                 err = np.abs(o[t:t + n] - want)
-                assert (err <= 2.0 ** -8 * (1 + 2.0 ** -6) * mag + 1e-6).all(), (s, float((err - 2.0 ** -8 * mag).max()))
+                assert (err <= out_bound(want, mag)).all(), (s, float((err - out_bound(want, mag)).max()))
                 empty = np.isneginf(wl)
                 assert np.array_equal(np.isneginf(l[t:t + n]), empty)
                 top = np.abs(qq[t:t + n]).max(initial=0) * np.abs(k).max(initial=0) * self.dim * scale
@@ -270,7 +275,7 @@ def test_attend_on_pages_that_do_not_exist():
         vv = v[40 * s:40 * s + 40].float().cpu().numpy().transpose(1, 0, 2).copy()
         kk[:, 16:32] = vv[:, 16:32] = 0
         want, wl, mag = orc.attend(q[t:t + n].float().cpu().numpy(), kk, vv, n, 64 ** -0.5)
-        assert (np.abs(out[t:t + n].float().cpu().numpy() - want) <= 2.0 ** -8 * (1 + 2.0 ** -6) * mag + 1e-6).all()
+        assert (np.abs(out[t:t + n].float().cpu().numpy() - want) <= out_bound(want, mag)).all()
         assert np.allclose(lse[t:t + n].cpu().numpy(), wl, rtol=0, atol=1e-5)
         t += n
 
@@ -354,7 +359,7 @@ def test_offsets_beyond_32_bits(dtype):
     rk, rv = rk.cpu().numpy(), rv.cpu().numpy()
     for s, (a, b, t) in enumerate(((0, 300, 0), (300, 1000, 1))):
         want, _, mag = orc.attend(q[t:t + new[s]].float().cpu().numpy(), rk[a:b].transpose(1, 0, 2), rv[a:b].transpose(1, 0, 2), new[s], dim ** -0.5)
-        assert (np.abs(out[t:t + new[s]].float().cpu().numpy() - want) <= 2.0 ** -8 * (1 + 2.0 ** -6) * mag + 1e-6).all()
+        assert (np.abs(out[t:t + new[s]].float().cpu().numpy() - want) <= out_bound(want, mag)).all()
 
 
 def test_nothing_to_do():
