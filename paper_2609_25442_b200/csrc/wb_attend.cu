@@ -5,6 +5,7 @@
 
 #include "wb_attend.cuh"
 #include "wb_attend_rows.cuh"
+#include "wb_attend_tiles.cuh"
 
 using namespace wbi;
 
@@ -13,60 +14,6 @@ namespace {
 constexpr uint32_t kHeaderBytes = 256;
 constexpr uint32_t kMaxRowTiles = 3;                    // wb_attend_rows_kernel: up to 16 * 3 rows
 constexpr uint32_t kMaxRowBlocks = 2 * kNumSMs;
-
-// One warp per (token, head): lanes own D / 32 elements, keys one after the other, the softmax's maximum
-// and sum carried along.
-template <int D, bool Q>
-__global__ void __launch_bounds__(128) wb_attend_plain_kernel(AttendArgs a, uint32_t skip_rows) {
-  constexpr int N = D / 32;
-  const uint32_t lane = threadIdx.x & 31;
-  const uint64_t id = (uint64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (id >= (uint64_t)a.b.n_tokens * a.n_heads) return;
-  const int32_t row = (int32_t)(id / a.n_heads);
-  const uint32_t h = (uint32_t)(id - (uint64_t)row * a.n_heads), g = h / a.group;
-  const uint32_t s = kv_seq_of_row(a.b, row);
-  const KvSeq q = attend_seq(a.b, s);
-  if (row - q.row0 >= q.n_new || (uint32_t)q.n_new * a.group <= skip_rows) return;
-  const int32_t pos = q.len - q.n_new + row - q.row0;
-  const int32_t first = a.window && pos >= (int32_t)a.window ? pos - (int32_t)a.window + 1 : 0;
-  float x[N], acc[N], top = -INFINITY, sum = 0.f;
-  for (int e = 0; e < N; ++e) {
-    x[e] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(a.q + row * a.q_token + h * a.q_head)[lane * N + e] << 16) * a.scale_log2 * kLn2;
-    acc[e] = 0.f;
-  }
-  for (int32_t j = first; j <= pos; ++j) {
-    const int32_t page = kv_page(a.b, a.c.n_pages, a.c.page_size, s, j);
-    float kk[N], vv[N];
-    for (int e = 0; e < N; ++e) kk[e] = vv[e] = 0.f;
-    if (page >= 0) {
-      const uint32_t slot = (uint32_t)j % a.c.page_size;
-      const uint64_t off = (uint64_t)page * a.c.page_stride + g * a.c.head_stride + slot * D + lane * N;
-      const uint64_t sc = ((uint64_t)page * a.c.n_kv_heads + g) * a.c.page_size + slot;
-      for (int e = 0; e < N; ++e) {
-        if (Q) {
-          kk[e] = unpack_e4m3x2((uint8_t)a.c.k[off + e]).x * a.c.k_scale[sc];
-          vv[e] = unpack_e4m3x2((uint8_t)a.c.v[off + e]).x * a.c.v_scale[sc];
-        } else {
-          kk[e] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(a.c.k)[off + e] << 16);
-          vv[e] = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(a.c.v)[off + e] << 16);
-        }
-      }
-    }
-    float d = 0.f;
-    for (int e = 0; e < N; ++e) d += x[e] * kk[e];
-    for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xFFFFFFFFu, d, o);
-    const float m = fmaxf(top, d);
-    if (m == -INFINITY) continue;
-    const float old = __expf(top - m), w = __expf(d - m);
-    sum = sum * old + w;
-    for (int e = 0; e < N; ++e) acc[e] = acc[e] * old + w * vv[e];
-    top = m;
-  }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-  for (int e = 0; e < N; ++e)
-    reinterpret_cast<uint16_t*>(a.out + row * a.o_token + h * a.o_head)[lane * N + e] = (uint16_t)pack_bf16x2(acc[e] * inv, 0.f);
-  if (a.lse && lane == 0) a.lse[(uint64_t)row * a.n_heads + h] = sum > 0.f ? top + logf(sum) : -INFINITY;
-}
 
 template <int D, bool Q, int MT>
 cudaError_t launch_rows(const AttendArgs& a, const wb_kv* kv, cudaStream_t stream) {
@@ -89,16 +36,39 @@ cudaError_t launch_rows_of(uint32_t rows, const AttendArgs& a, const wb_kv* kv, 
   return launch_rows<D, Q, 3>(a, kv, stream);
 }
 
-size_t counter_bytes(const wb_kv* kv, uint32_t n_seqs) { return ((size_t)n_seqs * kv->d.n_kv_heads * 4 + 255) / 256 * 256; }
+template <int D, bool Q>
+cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_rows, cudaStream_t stream) {
+  using C = TilesCfg<D, Q>;
+  auto kernel = wb_attend_tiles_kernel<D, Q>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemBytes);
+  if (e != cudaSuccess) return e;
+  // the softmax warps wait for registers that the others give back: the launch has to have them
+  cudaFuncAttributes f;
+  if ((e = cudaFuncGetAttributes(&f, kernel)) != cudaSuccess) return e;
+  if (f.numRegs != C::kLaunchRegs || f.sharedSizeBytes != 0) return cudaErrorInvalidConfiguration;
+  for (uint32_t s0 = 0; s0 < all.b.n_seqs; s0 += C::kMaxSeqs) {
+    AttendArgs a = all;
+    a.b.n_seqs = std::min(C::kMaxSeqs, all.b.n_seqs - s0);
+    a.b.table += (uint64_t)s0 * a.b.table_stride;
+    a.b.new_start += s0;
+    a.b.kv_len += s0;
+    kernel<<<kNumSMs, C::kThreads, C::kSmemBytes, stream>>>(a, kv->map_k, kv->map_v, skip_rows);
+    if ((e = cudaPeekAtLastError()) != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+constexpr uint32_t kCounterBytes = (kMaxRowBlocks * 4 + 255) / 256 * 256;
 template <int D> constexpr size_t partial_bytes() {
-  return (size_t)2 * 4 * std::max(kMaxRowBlocks * RowsCfg<D, false, 1>::kPartFloats, kNumSMs * RowsCfg<D, false, 3>::kPartFloats);
+  return (size_t)2 * 4 * std::max({kMaxRowBlocks * RowsCfg<D, false, 1>::kPartFloats, kNumSMs * RowsCfg<D, false, kMaxRowTiles>::kPartFloats,
+                                   kNumSMs * TilesCfg<D, false>::kPartFloats});
 }
 
 }  // namespace
 
 extern "C" size_t wb_kv_attend_workspace_bytes(const wb_kv* kv, uint32_t n_heads, uint32_t n_seqs) {
   if (!kv || !n_heads || n_seqs > WB_KV_MAX_SEQS) return 0;
-  return kHeaderBytes + counter_bytes(kv, n_seqs) + (kv->d.head_dim == 128 ? partial_bytes<128>() : partial_bytes<64>());
+  return kHeaderBytes + kCounterBytes + (kv->d.head_dim == 128 ? partial_bytes<128>() : partial_bytes<64>());
 }
 
 extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* q, uint32_t n_heads,
@@ -127,7 +97,7 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   a.box_rows = kv->box_rows;
   a.error = (uint32_t*)workspace;
   a.counters = (uint32_t*)((char*)workspace + kHeaderBytes);
-  a.partials = (float*)((char*)workspace + kHeaderBytes + counter_bytes(kv, batch->n_seqs));
+  a.partials = (float*)((char*)workspace + kHeaderBytes + kCounterBytes);
   const bool e = kv->d.dtype == WB_E4M3;
   const cudaStream_t st = (cudaStream_t)stream;
   const uint64_t rows = (uint64_t)batch->max_new * a.group;
@@ -139,10 +109,8 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   }
   if (err == cudaSuccess && rows > 16 * kMaxRowTiles) {
     const uint32_t skip = batch->n_seqs > 1 ? 16 * kMaxRowTiles : 0;
-    const uint32_t grid = (uint32_t)(((uint64_t)batch->n_tokens * n_heads + 3) / 4);
-    if (kv->d.head_dim == 128) e ? wb_attend_plain_kernel<128, true><<<grid, 128, 0, st>>>(a, skip) : wb_attend_plain_kernel<128, false><<<grid, 128, 0, st>>>(a, skip);
-    else e ? wb_attend_plain_kernel<64, true><<<grid, 128, 0, st>>>(a, skip) : wb_attend_plain_kernel<64, false><<<grid, 128, 0, st>>>(a, skip);
-    err = cudaPeekAtLastError();
+    if (kv->d.head_dim == 128) err = e ? launch_tiles<128, true>(a, kv, skip, st) : launch_tiles<128, false>(a, kv, skip, st);
+    else err = e ? launch_tiles<64, true>(a, kv, skip, st) : launch_tiles<64, false>(a, kv, skip, st);
   }
   if (err != cudaSuccess) (void)cudaGetLastError();
   return err == cudaSuccess ? WB_OK : WB_ERR_CUDA;

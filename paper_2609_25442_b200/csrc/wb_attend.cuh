@@ -16,7 +16,7 @@ struct AttendArgs {
   uint32_t n_heads, group, window;
   uint32_t box_rows;
   uint32_t* error;                              // workspace: first word
-  uint32_t* counters;                           // one per (sequence, kv head[, row block]); zero between calls
+  uint32_t* counters;                           // one per block, for the cut item that begins in it; zero between calls
   float* partials;
 };
 

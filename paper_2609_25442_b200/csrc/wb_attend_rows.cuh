@@ -452,7 +452,6 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
 
     // ---- result: whole items directly, cut ones through the workspace ------------------------------
     const bool whole = item0 >= begin && item1 <= end;
-    const uint32_t item = s * hk + (uint32_t)h;
     if (!whole && kw == 3) {
       float* part = a.partials + (size_t)(2 * blockIdx.x + (item0 >= begin ? 1 : 0)) * C::kPartFloats + mt * (C::kRegs * 32 + 32);
 #pragma unroll
@@ -475,8 +474,8 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
       const uint32_t first = (uint32_t)(item0 / per), count = (uint32_t)((item1 - 1) / per) - first + 1;
       if (tid == 0) {
         __threadfence();
-        s_last = atomicAdd(a.counters + item, 1u) == count - 1;
-        if (s_last) a.counters[item] = 0;
+        s_last = atomicAdd(a.counters + first, 1u) == count - 1;
+        if (s_last) a.counters[first] = 0;
       }
       asm volatile("bar.sync 1, %0;" ::"n"(32 * C::kWarps) : "memory");
       if (s_last) {
