@@ -54,11 +54,22 @@ cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_r
     a.b.kv_len += s0;
     kernel<<<kNumSMs, C::kThreads, C::kSmemBytes, stream>>>(a, kv->map_k, kv->map_v, skip_rows);
     if ((e = cudaPeekAtLastError()) != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kNumSMs, kQRows / 32);
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // set up while the kernel before still runs
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if ((e = cudaLaunchKernelEx(&cfg, wb_attend_join_kernel<D>, a)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
 
-constexpr uint32_t kCounterBytes = (kMaxRowBlocks * 4 + 255) / 256 * 256;
+
+constexpr uint32_t kCounterBytes = (kMaxRowBlocks * 4 + 255) / 256 * 256, kCutBytes = (kNumSMs * sizeof(CutItem) + 255) / 256 * 256;
 template <int D> constexpr size_t partial_bytes() {
   return (size_t)2 * 4 * std::max({kMaxRowBlocks * RowsCfg<D, false, 1>::kPartFloats, kNumSMs * RowsCfg<D, false, kMaxRowTiles>::kPartFloats,
                                    kNumSMs * TilesCfg<D, false>::kPartFloats});
@@ -68,7 +79,7 @@ template <int D> constexpr size_t partial_bytes() {
 
 extern "C" size_t wb_kv_attend_workspace_bytes(const wb_kv* kv, uint32_t n_heads, uint32_t n_seqs) {
   if (!kv || !n_heads || n_seqs > WB_KV_MAX_SEQS) return 0;
-  return kHeaderBytes + kCounterBytes + (kv->d.head_dim == 128 ? partial_bytes<128>() : partial_bytes<64>());
+  return kHeaderBytes + kCounterBytes + kCutBytes + (kv->d.head_dim == 128 ? partial_bytes<128>() : partial_bytes<64>());
 }
 
 extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* q, uint32_t n_heads,
@@ -97,7 +108,8 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   a.box_rows = kv->box_rows;
   a.error = (uint32_t*)workspace;
   a.counters = (uint32_t*)((char*)workspace + kHeaderBytes);
-  a.partials = (float*)((char*)workspace + kHeaderBytes + kCounterBytes);
+  a.cuts = (char*)workspace + kHeaderBytes + kCounterBytes;
+  a.partials = (float*)((char*)workspace + kHeaderBytes + kCounterBytes + kCutBytes);
   const bool e = kv->d.dtype == WB_E4M3;
   const cudaStream_t st = (cudaStream_t)stream;
   const uint64_t rows = (uint64_t)batch->max_new * a.group;

@@ -16,7 +16,8 @@ struct AttendArgs {
   uint32_t n_heads, group, window;
   uint32_t box_rows;
   uint32_t* error;                              // workspace: first word
-  uint32_t* counters;                           // one per block, for the cut item that begins in it; zero between calls
+  uint32_t* counters;                           // row kernel: one per block, for the cut item that begins in it; zero between calls
+  char* cuts;                                   // CutItem of every block of the tile kernel
   float* partials;
 };
 

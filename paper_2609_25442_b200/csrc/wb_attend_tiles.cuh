@@ -34,6 +34,8 @@ struct TilesCfg {
   static constexpr uint32_t kScaleSlots = 4;                       // 128 scales each; keys and values in turn
   static constexpr uint32_t kRowSpan = D * (Q ? 1 : 2) < 128 ? D * (Q ? 1 : 2) : 128;   // bytes of a row in a box
   static constexpr uint32_t kRowSpans = D * (Q ? 1 : 2) / kRowSpan;
+  // the quarter of a row's weights after which their product may start (3: all; measured best of 0, 1, 3)
+  static constexpr int kHalfAt = Q ? 3 : 1;
   static constexpr uint32_t kThreads = Q ? 512 : 384;
   // registers: the compiler gives every thread kLaunchRegs; the softmax warps take over what the others leave
   // (256 * kSoftmaxRegs + (kThreads - 256) * kOtherRegs = kThreads * kLaunchRegs)
@@ -45,26 +47,32 @@ struct TilesCfg {
   static constexpr uint32_t kOffRaw = kOffSlots + kSlots * kSlotBytes;
   static constexpr uint32_t kOffScale = kOffRaw + kRaws * kRawBytes;
   static constexpr uint32_t kOffBars = kOffScale + (Q ? kScaleSlots * kKeys * 4 : 0);
-  static constexpr uint32_t kBars = 1 + 6 + 2 * kSlots + (Q ? 2 * kRaws + 2 * kScaleSlots : 0);
-  static constexpr uint32_t kOffMisc = kOffBars + kBars * 8;       // tensor memory address, last flag, odd flags
-  static constexpr uint32_t kOffCum = kOffMisc + 32;
+  static constexpr uint32_t kBars = 1 + 8 + 2 * kSlots + (Q ? 2 * kRaws + 3 * kScaleSlots : 0);
+  static constexpr uint32_t kOffMisc = kOffBars + kBars * 8;  // tensor memory address, flags, share
+  static constexpr uint32_t kOffCum = kOffMisc + 64;
   static constexpr uint32_t kSmemBytes = kOffCum + (kMaxSeqs + 1) * 4;
   static_assert(kSmemBytes <= 232448, "");
 };
 
 // ---- tcgen05 ------------------------------------------------------------------------------------
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// The warp that issues products stays converged: every lane computes the same descriptors (so that they live in uniform
+// registers) and only the leader's instruction is let through.  Issued from a branch that one lane takes, each product costs
+// about 80 clocks of moves into uniform registers, more than the product itself.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
+__device__ __forceinline__ void tc_commit(uint32_t bar, uint32_t leader) {
+  asm volatile("{ .reg .pred e; setp.ne.u32 e, %1, 0; @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }"
+               ::"r"(bar), "r"(leader) : "memory");
 }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add, uint32_t leader) {
+  asm volatile("{ .reg .pred p, e; setp.ne.u32 p, %4, 0; setp.ne.u32 e, %5, 0; @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p; }"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add), "r"(leader) : "memory");
 }
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile("{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
-               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t add, uint32_t leader) {
+  asm volatile("{ .reg .pred p, e; setp.ne.u32 p, %4, 0; setp.ne.u32 e, %5, 0; @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p; }"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(add), "r"(leader) : "memory");
 }
 #define WB_R32(r) "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), \
     "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), \
@@ -80,6 +88,11 @@ __device__ __forceinline__ void tm_load32(uint32_t addr, uint32_t* r) {
 __device__ __forceinline__ void tm_store32(uint32_t addr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
                "%24,%25,%26,%27,%28,%29,%30,%31};" ::WB_R32(r), "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
+               "r"(r[14]), "r"(r[15]), "r"(addr) : "memory");
 }
 __device__ __forceinline__ void tm_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -113,6 +126,19 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
   return r;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// Four scales; volatile, so that they are not all fetched ahead (128 registers hold the scores already).
+__device__ __forceinline__ ulonglong2 load_scales(uint32_t addr) {
+  ulonglong2 f;
+  asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f.x), "=l"(f.y) : "r"(addr));
+  return f;
+}
+
 // ---- geometry -----------------------------------------------------------------------------------
 struct RowBlock {
   int32_t kt0, n;          // first tile of 128 cache rows, number of tiles (at least one)
@@ -131,6 +157,24 @@ __device__ __forceinline__ uint32_t row_blocks(const KvSeq& q, uint32_t group, u
   const uint64_t rows = (uint64_t)q.n_new * group;
   return rows > skip_rows ? (uint32_t)((rows + kQRows - 1) / kQRows) : 0;
 }
+
+// A block's share of the line begins at the multiple of `per` that is its number, moved to the next end of an item where that is
+// not more than kSnap tiles away: joining a cut item costs more than so many tiles.  So an item [i0, i1) is cut at the multiples
+// of `per` that lie more than kSnap tiles inside.
+constexpr int32_t kSnap = 2;
+struct Cuts {
+  int32_t first, n;        // the block that holds the item's first tile, number of cuts
+};
+__device__ __forceinline__ Cuts cuts_of(int32_t i0, int32_t i1, int32_t per) {
+  const int32_t lo = (i0 + kSnap + per) / per, hi = (i1 - kSnap - 1) / per;    // multiples in (i0 + kSnap, i1 - kSnap)
+  return Cuts{lo - 1, max(0, hi - lo + 1)};
+}
+
+// What the joining kernel reads of the item that is cut first in a block.
+struct CutItem {
+  uint32_t parts;          // 0: none
+  uint32_t s, h, rb;
+};
 
 // Where a block is in the line of tiles; every warp walks it alike.
 struct Walk {
@@ -197,22 +241,98 @@ __device__ __forceinline__ void walk_on(Walk& w, const AttendArgs& a, const int3
   w.blk = row_block(w.seq, a.group, a.window, w.rb);
 }
 
-// Values that are not finite were taken out of a tile some rows of which do not see them: a row that does see one has it
-// added here (its weight is positive, whatever it is).  Rare, so straight from the cache.
-__device__ __noinline__ void add_odd_values(const AttendArgs& a, const Walk& w, int32_t kt_begin, int32_t kt_end, int32_t lo, int32_t hi,
-                                            int32_t cut_hi, int32_t cut_lo, uint32_t d0, float* o) {
-  for (int32_t kt = kt_begin; kt < kt_end; ++kt) {
-    if (!(kt * (int32_t)kKeys + (int32_t)kKeys - 1 > cut_hi || kt * (int32_t)kKeys < cut_lo)) continue;
-    for (int32_t pos = max(lo, kt * (int32_t)kKeys); pos <= min(hi, kt * (int32_t)kKeys + (int32_t)kKeys - 1); ++pos) {
-      const int32_t page = kv_page(a.b, a.c.n_pages, a.c.page_size, w.s, pos);
-      if (page < 0) continue;
-      const uint16_t* v = reinterpret_cast<const uint16_t*>(a.c.v) + (uint64_t)page * a.c.page_stride + w.h * a.c.head_stride +
-                          ((uint32_t)pos % a.c.page_size) * a.c.head_dim + d0;
+// The beginning of block x's share.
+__device__ __forceinline__ int32_t share_begin(const AttendArgs& a, const int32_t* cum, uint32_t skip_rows, int32_t x, int32_t per, int32_t total) {
+  const int32_t t = x * per;
+  if (t <= 0 || t >= total) return t <= 0 ? 0 : total;
+  const Walk w = walk_to(a, cum, skip_rows, t);
+  if (t - w.item0 <= kSnap) return w.item0;
+  if (w.item0 + w.blk.n - t <= kSnap) return w.item0 + w.blk.n;
+  return t;
+}
+
+// Values that are not finite were taken out of a tile that not every row sees (of any tile, where a scale was not finite): a row that
+// does see one has it added here (its weight is positive, whatever it is).  Rare, so straight from the cache.
+template <bool Q>
+__device__ __noinline__ void add_odd_values(const AttendArgs& a, const Walk& w, int32_t kt_begin, int32_t kt_end, int32_t lo, int32_t hi, uint32_t d0,
+                                            float* o) {
+  for (int32_t pos = max(lo, kt_begin * (int32_t)kKeys); pos <= min(hi, kt_end * (int32_t)kKeys - 1); ++pos) {
+    const int32_t page = kv_page(a.b, a.c.n_pages, a.c.page_size, w.s, pos);
+    if (page < 0) continue;
+    const uint32_t slot = (uint32_t)pos % a.c.page_size;
+    const uint64_t at = (uint64_t)page * a.c.page_stride + w.h * a.c.head_stride + slot * a.c.head_dim + d0;
+    if (Q) {
+      const float s = a.c.v_scale[((uint64_t)page * a.c.n_kv_heads + w.h) * a.c.page_size + slot];
+      if (isfinite(s)) continue;
+      for (int d = 0; d < 32; ++d) o[d] += unpack_e4m3x2((uint8_t)a.c.v[at + d]).x * s;
+    } else {
+      const uint16_t* v = reinterpret_cast<const uint16_t*>(a.c.v) + at;
       for (int d = 0; d < 32; ++d)
         if ((v[d] & 0x7F80u) == 0x7F80u) o[d] += __uint_as_float((uint32_t)v[d] << 16);
     }
   }
 }
+
+// A thread's row of the block.
+struct RowOf {
+  bool in;
+  uint32_t tok, head;      // row and head of the step's tensors
+  int32_t hi, lo;          // positions that it sees
+};
+__device__ __forceinline__ RowOf row_of(const AttendArgs& a, const Walk& w, uint32_t r0) {
+  RowOf x;
+  const uint32_t n_rows = (uint32_t)w.seq.n_new * a.group, r = w.rb * kQRows + r0;
+  x.in = r < n_rows;
+  x.tok = (x.in ? r : n_rows - 1) / a.group;
+  x.head = w.h * a.group + (x.in ? r - x.tok * a.group : 0);
+  x.hi = w.seq.len - w.seq.n_new + (int32_t)x.tok;
+  x.lo = a.window ? x.hi - (int32_t)a.window + 1 : 0;
+  x.tok += (uint32_t)w.seq.row0;
+  return x;
+}
+
+// The row's query into shared memory, swizzled as the products read it.
+template <int D>
+__device__ __forceinline__ void load_query(const AttendArgs& a, char* tile, uint32_t row, const RowOf& x) {
+  const uint4* src = reinterpret_cast<const uint4*>(a.q + (uint64_t)x.tok * a.q_token + x.head * a.q_head);
+#pragma unroll
+  for (uint32_t c = 0; c < D / 8; ++c) {
+    const uint4 y = x.in ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
+    *reinterpret_cast<uint4*>(tile + (c >> 3) * (kKeys * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = y;
+  }
+}
+
+// One cache row of a value tile: cleared if it lies past the end; else its values that are not finite are taken out, and the
+// flag is raised first, so that whoever finds them gone finds the flag.
+template <int D>
+__device__ __forceinline__ void clear_values(char* tile, uint32_t row, bool past, volatile uint32_t* flag) {
+  char* v = tile + row * 128;
+  if (past) {
+#pragma unroll
+    for (uint32_t c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(v + (c >> 3) * (kKeys * 128) + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  bool odd = false;
+#pragma unroll
+  for (uint32_t c = 0; c < D / 8; ++c) {
+    const uint4 y = *reinterpret_cast<const uint4*>(v + (c >> 3) * (kKeys * 128) + ((c & 7) << 4));
+    // an exponent of all ones, in either half: adding the lowest bit of the exponent carries into the sign's place
+    const uint32_t any = (((y.x & 0x7FFF7FFFu) + 0x00800080u) | ((y.y & 0x7FFF7FFFu) + 0x00800080u) | ((y.z & 0x7FFF7FFFu) + 0x00800080u) |
+                          ((y.w & 0x7FFF7FFFu) + 0x00800080u)) & 0x80008000u;
+    odd |= any != 0;
+  }
+  if (!odd) return;
+  *flag = 1;
+  __threadfence_block();
+  for (uint32_t c = 0; c < D / 2; ++c) {
+    uint32_t* at = reinterpret_cast<uint32_t*>(v + (c >> 5) * (kKeys * 128)) + (c & 31);
+    uint32_t y = *at;
+    if ((y & 0x7F80u) == 0x7F80u) y &= 0xFFFF0000u;
+    if ((y & 0x7F800000u) == 0x7F800000u) y &= 0xFFFFu;
+    *at = y;
+  }
+}
+
 
 template <int D, bool Q>
 __global__ void __launch_bounds__(TilesCfg<D, Q>::kThreads, 1)
@@ -221,12 +341,12 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
   using C = TilesCfg<D, Q>;
   extern __shared__ __align__(1024) char smem[];
   const uint32_t base = smem_addr(smem);
-  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
   const uint32_t bars = base + C::kOffBars;
-  const uint32_t q_full = bars, s_full = bars + 8, p_full = bars + 24, o_full = bars + 40, full = bars + 56, empty = full + 8 * C::kSlots,
+  const uint32_t q_full = bars, s_full = bars + 8, p_half = bars + 24, p_full = bars + 40, o_full = bars + 56, full = bars + 72, empty = full + 8 * C::kSlots,
                  raw_full = empty + 8 * C::kSlots, raw_empty = raw_full + 8 * C::kRaws, scale_full = raw_empty + 8 * C::kRaws,
-                 scale_empty = scale_full + 8 * C::kScaleSlots;
-  volatile uint32_t* const misc = reinterpret_cast<volatile uint32_t*>(smem + C::kOffMisc);   // [0] tensor memory, [1] last, [2..4] odd
+                 scale_ready = scale_full + 8 * C::kScaleSlots, scale_empty = scale_ready + 8 * C::kScaleSlots;
+  volatile uint32_t* const misc = reinterpret_cast<volatile uint32_t*>(smem + C::kOffMisc);   // [0] tensor memory, [5, 6] share, [8..15] items' flags
   int32_t* const cum = reinterpret_cast<int32_t*>(smem + C::kOffCum);
   if (base & 1023u) {      // swizzled tiles need it; never the case without static shared memory
     if (tid == 0) atomicMax(a.error, 2u);
@@ -240,6 +360,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
     bar_init(q_full, 256);
     for (uint32_t i = 0; i < 2; ++i) {
       bar_init(s_full + 8 * i, 1);
+      bar_init(p_half + 8 * i, 128);
       bar_init(p_full + 8 * i, 128);
       bar_init(o_full + 8 * i, 1);
     }
@@ -254,11 +375,12 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       }
       for (uint32_t i = 0; i < C::kScaleSlots; ++i) {
         bar_init(scale_full + 8 * i, 32);
+        bar_init(scale_ready + 8 * i, 128);
         bar_init(scale_empty + 8 * i, 256);
       }
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    misc[2] = misc[3] = misc[4] = 0;
+    for (int i = 8; i < 16; ++i) misc[i] = 0;
   }
   for (uint32_t s = warp; s < n_seqs; s += C::kThreads / 32) {
     const KvSeq q = attend_seq(a.b, s);
@@ -288,7 +410,14 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
   const uint32_t tmem = misc[0];
   const int32_t total = cum[n_seqs];
   const int32_t per = (total + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
-  const int32_t begin = min((int32_t)blockIdx.x * per, total), end = min(begin + per, total);
+  if (warp < 2) {
+    const int32_t t = share_begin(a, cum, skip_rows, (int32_t)(blockIdx.x + warp), per, total);
+    if (lane == 0) misc[5 + warp] = (uint32_t)t;
+  }
+  __syncthreads();
+  const int32_t begin = (int32_t)misc[5], end = (int32_t)misc[6];
+  CutItem* const cut_item = reinterpret_cast<CutItem*>(a.cuts) + blockIdx.x;
+  if (tid == 0) cut_item->parts = 0;
 
   if (begin < end) {
     if (warp < 8) {
@@ -298,311 +427,281 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       const uint32_t tm_lane = tmem + ((warp & 3) << 21);
       const uint32_t tm_s = tm_lane + i * 128, tm_o = tm_lane + 256 + i * 128;
       const float c2 = a.scale_log2;
-      uint32_t jg = 0, item = 0;                    // steps and items so far
+      uint32_t jg = 0, item = 0;                    // steps and items of the block so far
+      uint32_t js = 0, is = 0;                      // those that this tile took part in
       bool ok = true;
       Walk w = walk_to(a, cum, skip_rows, begin);
+      RowOf x0 = row_of(a, w, i * 128 + row);
+      load_query<D>(a, smem + i * C::kSlotBytes, row, x0);
+      fence_async();
+      bar_arrive(q_full);
       for (int32_t t = begin; t < end; ++item) {
-        const int32_t item1 = w.item0 + w.blk.n, stop = min(end, item1);
-        const uint32_t n_rows = (uint32_t)w.seq.n_new * a.group, r = w.rb * kQRows + i * 128 + row;
-        const bool in = r < n_rows;
-        const uint32_t tok = (in ? r : n_rows - 1) / a.group;
-        const uint32_t head = w.h * a.group + (in ? r - tok * a.group : 0);
+        const int32_t item1 = w.item0 + w.blk.n, stop = min(end, item1), from = t;
+        const uint32_t n_rows = (uint32_t)w.seq.n_new * a.group;
         const int32_t base_pos = w.seq.len - w.seq.n_new;
-        const int32_t hi = base_pos + (int32_t)tok, lo = a.window ? hi - (int32_t)a.window + 1 : 0;
+        // tiles that not every row of the block sees whole
         const int32_t cut_hi = base_pos + (int32_t)(w.rb * kQRows / a.group);
         const int32_t cut_lo = a.window ? base_pos + (int32_t)((min(n_rows, (w.rb + 1) * kQRows) - 1) / a.group) - (int32_t)a.window + 1 : 0;
-        if (tid == 0) misc[2 + (item + 1) % 3] = 0;
-        // the row's query, swizzled as the products read it
-        {
-          const uint4* src = reinterpret_cast<const uint4*>(a.q + (uint64_t)(w.seq.row0 + (int32_t)tok) * a.q_token + head * a.q_head);
-          char* dst = smem + i * C::kSlotBytes;
-#pragma unroll
-          for (uint32_t c = 0; c < D / 8; ++c) {
-            const uint4 x = in ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4*>(dst + (c >> 3) * C::kSpanBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = x;
-          }
-          fence_async();
-          tc_before();
-          bar_arrive(q_full);
-        }
+        // rows of a warp are in the order of their tokens: its first row sees the least far, its last row's window begins last
+        const int32_t warp_hi = __shfl_sync(0xFFFFFFFFu, x0.hi, 0), warp_lo = a.window ? __shfl_sync(0xFFFFFFFFu, x0.lo, 31) : 0;
+        const bool takes_part = i == 0 || n_rows > w.rb * kQRows + 128;
+        if (tid == 0) misc[8 + (item + 5) % 8] = 0;     // that of three items ago; nobody is five items ahead
         float mref = -INFINITY;                     // the maximum that the weights are relative to, times c2
-        uint64_t sum2 = 0;
+        uint64_t sum2[2] = {0, 0};
         for (bool first = true; t < stop; ++t, ++jg, first = false) {
-          const int32_t kt = w.blk.kt0 + t - w.item0;
-          const int32_t pos0 = kt * (int32_t)kKeys;
+          const uint32_t sk = (2 * jg) % C::kScaleSlots, sv = sk + 1;
+          if (!takes_part) {                        // keeps the pace of the scales' ring
+            if (Q) {
+              ok = wait_or_give_up(scale_ready + 8 * sk, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
+              ok = wait_or_give_up(scale_ready + 8 * sv, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
+              bar_arrive(scale_empty + 8 * sk);
+              bar_arrive(scale_empty + 8 * sv);
+            }
+            continue;
+          }
+          const int32_t pos0 = (w.blk.kt0 + t - w.item0) * (int32_t)kKeys;
           const bool cut = pos0 + (int32_t)kKeys - 1 > cut_hi || pos0 < cut_lo;
-          uint32_t x[128];
-          ok = wait_or_give_up(s_full + 8 * i, jg & 1, ok, a.error);
-          tc_after();
-          tm_load32(tm_s, x);
-          tm_load32(tm_s + 32, x + 32);
-          tm_load32(tm_s + 64, x + 64);
-          tm_load32(tm_s + 96, x + 96);
-          tm_wait_load();
-          const float4* kscale = nullptr;
-          const float4* vscale = nullptr;
-          if (Q) {
-            const uint32_t sk = (2 * jg) % C::kScaleSlots;
-            ok = wait_or_give_up(scale_full + 8 * sk, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
-            kscale = reinterpret_cast<const float4*>(smem + C::kOffScale + sk * (kKeys * 4));
-            vscale = reinterpret_cast<const float4*>(smem + C::kOffScale + (sk + 1) * (kKeys * 4));
-#pragma unroll
-            for (int c = 0; c < 32; ++c) {
-              const float4 f = kscale[c];
-              x[4 * c] = __float_as_uint(__uint_as_float(x[4 * c]) * f.x);
-              x[4 * c + 1] = __float_as_uint(__uint_as_float(x[4 * c + 1]) * f.y);
-              x[4 * c + 2] = __float_as_uint(__uint_as_float(x[4 * c + 2]) * f.z);
-              x[4 * c + 3] = __float_as_uint(__uint_as_float(x[4 * c + 3]) * f.w);
-            }
-          }
-          if (cut) {
-            const int32_t h1 = hi - pos0, l1 = lo - pos0;
-#pragma unroll
-            for (int c = 0; c < 128; ++c)
-              if (c > h1 || c < l1) x[c] = 0xFF800000u;
-          }
-          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int c = 0; c < 128; c += 4)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) m4[e] = fmaxf(m4[e], __uint_as_float(x[c + e]));
-          const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c2;
-          const bool grow = m > mref + 8.f;
-          float corr = 1.f;
-          if (grow) {
-            corr = mref == -INFINITY ? 0.f : fast_exp2(mref - m);
-            mref = m;
-          }
-          // the step's commit covered the previous product, so nothing writes the outputs now
-          if (!first && __any_sync(0xFFFFFFFFu, grow)) {
-#pragma unroll
-            for (int c = 0; c < D; c += 32) {
-              uint32_t o[32];
-              tm_load32(tm_o + c, o);
-              tm_wait_load();
-#pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * corr);
-              tm_store32(tm_o + c, o);
-            }
-          }
-          if (Q) ok = wait_or_give_up(scale_full + 8 * ((2 * jg + 1) % C::kScaleSlots), ((2 * jg + 1) / C::kScaleSlots) & 1, ok, a.error);
-          sum2 = mul2(sum2, pack2(corr, corr));
-          const float ref = mref == -INFINITY ? 0.f : mref;
-          const uint64_t c22 = pack2(c2, c2), ref2 = pack2(-ref, -ref);
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t p[32];
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const int c = half * 64 + 2 * e;
-              float u, v;
-              unpack2(fma2(pack2(__uint_as_float(x[c]), __uint_as_float(x[c + 1])), c22, ref2), u, v);
-              u = fast_exp2(u);
-              v = fast_exp2(v);
-              sum2 = add2(sum2, pack2(u, v));
-              if (Q) {
-                const float2 f = reinterpret_cast<const float2*>(vscale)[half * 32 + e];
-                // a scale of a position that is not seen may be anything
-                u = cut && u == 0.f ? 0.f : u * f.x;
-                v = cut && v == 0.f ? 0.f : v * f.y;
-              }
-              p[e] = pack_bf16x2(u, v);
-            }
-            tm_store32(tm_s + half * 32, p);
-          }
           if (!Q && cut) {
             // values past the end, and values that are not finite, must not meet weights of zero
             const uint32_t vq = 2 * jg + 1, slot = vq % C::kSlots;
             ok = wait_or_give_up(full + 8 * slot, (vq / C::kSlots) & 1, ok, a.error);
-            char* v = smem + C::kOffSlots + slot * C::kSlotBytes + row * 128;
-            const bool past = pos0 + (int32_t)row >= w.seq.len;
-#pragma unroll 1
-            for (uint32_t c = 0; c < D / 8; ++c) {
-              uint4* at = reinterpret_cast<uint4*>(v + (c >> 3) * C::kSpanBytes + (((c & 7) ^ (row & 7)) << 4));
-              uint4 y = *at;
-              uint32_t* yw = reinterpret_cast<uint32_t*>(&y);
-              bool odd = false;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if ((yw[e] & 0x7F80u) == 0x7F80u) { odd = true; yw[e] &= 0xFFFF0000u; }
-                if ((yw[e] & 0x7F800000u) == 0x7F800000u) { odd = true; yw[e] &= 0xFFFFu; }
-              }
-              if (past) {
-                *at = make_uint4(0, 0, 0, 0);
-              } else if (odd) {
-                misc[2 + item % 3] = 1;      // before the value goes: whoever finds it gone finds the flag
-                __threadfence_block();
-                *at = y;
-              }
-            }
+            clear_values<D>(smem + C::kOffSlots + slot * C::kSlotBytes, row, pos0 + (int32_t)row >= w.seq.len, misc + 8 + item % 8);
             fence_async();
           }
-          tm_wait_store();
-          tc_before();
-          bar_arrive(p_full + 8 * i);
+          float x[128];
+          ok = wait_or_give_up(s_full + 8 * i, js & 1, ok, a.error);
+          ++js;
+          tc_after();
+#pragma unroll
+          for (int c = 0; c < 128; c += 32) tm_load32(tm_s + c, reinterpret_cast<uint32_t*>(x) + c);
+          tm_wait_load();
           if (Q) {
-            bar_arrive(scale_empty + 8 * ((2 * jg) % C::kScaleSlots));
-            bar_arrive(scale_empty + 8 * ((2 * jg + 1) % C::kScaleSlots));
+            ok = wait_or_give_up(scale_ready + 8 * sk, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
+            const uint32_t scales = base + C::kOffScale + sk * (kKeys * 4);
+#pragma unroll
+            for (int c = 0; c < 128; c += 4) {
+              const ulonglong2 f = load_scales(scales + 4 * c);
+              unpack2(mul2(pack2(x[c], x[c + 1]), f.x), x[c], x[c + 1]);
+              unpack2(mul2(pack2(x[c + 2], x[c + 3]), f.y), x[c + 2], x[c + 3]);
+            }
           }
+          // masks, in groups of columns that some row of the warp does not see
+          if (pos0 + (int32_t)kKeys - 1 > warp_hi) {
+            const int32_t h1 = x0.hi - pos0, w1 = warp_hi - pos0;
+#pragma unroll
+            for (int c = 0; c < 128; c += 16)
+              if (c + 15 > w1) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[c + e] = c + e > h1 ? -INFINITY : x[c + e];
+              }
+          }
+          if (pos0 < warp_lo) {
+            const int32_t l1 = x0.lo - pos0, w1 = warp_lo - pos0;
+#pragma unroll
+            for (int c = 0; c < 128; c += 16)
+              if (c < w1) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[c + e] = c + e < l1 ? -INFINITY : x[c + e];
+              }
+          }
+          float m4[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+          for (int c = 4; c < 124; c += 8)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m4[e] = max3(m4[e], x[c + 2 * e], x[c + 2 * e + 1]);
+          m4[0] = max3(m4[0], x[124], x[125]);
+          m4[1] = max3(m4[1], x[126], x[127]);
+          const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c2;
+          const bool grow = m > mref + 8.f;
+          // the step's commit covered the previous product, so nothing writes the outputs now
+          if (__any_sync(0xFFFFFFFFu, grow)) {
+            float corr = 1.f;
+            if (grow) {
+              corr = mref == -INFINITY ? 0.f : fast_exp2(mref - m);
+              mref = m;
+            }
+            const uint64_t corr2 = pack2(corr, corr);
+            sum2[0] = mul2(sum2[0], corr2);
+            sum2[1] = mul2(sum2[1], corr2);
+            if (!first) {
+#pragma unroll 1
+              for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tm_load32(tm_o + c, o);
+                tm_wait_load();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * corr);
+                tm_store32(tm_o + c, o);
+              }
+            }
+          }
+          if (Q) ok = wait_or_give_up(scale_ready + 8 * sv, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
+          const float ref = mref == -INFINITY ? 0.f : mref;
+          const uint64_t c22 = pack2(c2, c2), ref2 = pack2(-ref, -ref);
+          const uint32_t vscales = base + C::kOffScale + sv * (kKeys * 4);
+#pragma unroll
+          for (int quarter = 0; quarter < 4; ++quarter) {
+            uint32_t p[16];
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+              const int c = quarter * 32 + 2 * e;
+              ulonglong2 f;
+              if (Q) f = load_scales(vscales + 4 * c);
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                float u, v;
+                unpack2(fma2(pack2(x[c + 2 * k], x[c + 2 * k + 1]), c22, ref2), u, v);
+                const uint64_t y = pack2(fast_exp2(u), fast_exp2(v));
+                sum2[k] = add2(sum2[k], y);
+                unpack2(Q ? mul2(y, k ? f.y : f.x) : y, u, v);
+                p[e + k] = pack_bf16x2(u, v);
+              }
+            }
+            tm_store16(tm_s + quarter * 16, p);
+            if (quarter == C::kHalfAt) {      // the product of these weights starts while the rest is computed
+              tm_wait_store();
+              tc_before();
+              bar_arrive(p_half + 8 * i);
+            }
+          }
+          if (C::kHalfAt < 3) {
+            tm_wait_store();
+            tc_before();
+            bar_arrive(p_full + 8 * i);
+          }
+          if (Q) {
+            bar_arrive(scale_empty + 8 * sk);
+            bar_arrive(scale_empty + 8 * sv);
+          }
+        }
+        // the scores of this item are done with: the next one's queries take their place while its last product runs
+        Walk w2 = w;
+        RowOf x2 = x0;
+        if (t < end) {
+          walk_on(w2, a, cum, skip_rows);
+          x2 = row_of(a, w2, i * 128 + row);
+          load_query<D>(a, smem + i * C::kSlotBytes, row, x2);
+          fence_async();
+          bar_arrive(q_full);
         }
         // ---- outputs ---------------------------------------------------------------------------------
-        float l, l1;
-        unpack2(sum2, l, l1);
-        l += l1;
-        ok = wait_or_give_up(o_full + 8 * i, item & 1, ok, a.error);
-        tc_after();
-        const int32_t from = max(w.item0, begin);
-        const bool odd = !Q && misc[2 + item % 3] != 0;
-        const bool whole = w.item0 >= begin && item1 <= end;
-        char* dst = a.out + (uint64_t)(w.seq.row0 + (int32_t)tok) * a.o_token + head * a.o_head;
-        float* lse = a.lse ? a.lse + (uint64_t)(w.seq.row0 + (int32_t)tok) * a.n_heads + head : nullptr;
-        float* part = a.partials + (size_t)(2 * blockIdx.x + (w.item0 >= begin ? 1 : 0)) * C::kPartFloats + i * (D * 128 + 256) + row;
-        const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+        if (takes_part) {
+          float l, l1;
+          unpack2(add2(sum2[0], sum2[1]), l, l1);
+          l += l1;
+          ok = wait_or_give_up(o_full + 8 * i, is & 1, ok, a.error);
+          ++is;
+          tc_after();
+          const bool odd = misc[8 + item % 8] != 0;
+          const Cuts cuts = cuts_of(w.item0, item1, per);
+          char* dst = a.out + (uint64_t)x0.tok * a.o_token + x0.head * a.o_head;
+          float* part = a.partials + (size_t)(2 * blockIdx.x + (w.item0 >= begin ? 1 : 0)) * C::kPartFloats + i * (D * 128 + 256) + row;
+          const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
 #pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t o[32];
-          tm_load32(tm_o + c, o);
-          tm_wait_load();
-          if (odd && in) {
-            float y[32];
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tm_load32(tm_o + c, o);
+            tm_wait_load();
+            if (odd && x0.in) {
+              float y[32];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(o[e]);
-            add_odd_values(a, w, w.blk.kt0 + from - w.item0, w.blk.kt0 + stop - w.item0, lo, hi, cut_hi, cut_lo, c, y);
+              for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(o[e]);
+              add_odd_values<Q>(a, w, w.blk.kt0 + from - w.item0, w.blk.kt0 + stop - w.item0, x0.lo, x0.hi, c, y);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(y[e]);
-          }
-          if (whole) {
-            if (in)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                uint32_t y[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  y[k] = pack_bf16x2(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv);
-                *reinterpret_cast<uint4*>(dst + (c + 8 * e) * 2) = make_uint4(y[0], y[1], y[2], y[3]);
-              }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) __stcg(part + (c + e) * 128, __uint_as_float(o[e]));
-          }
-        }
-        tc_before();       // the outputs' columns may be written again once every thread has arrived for the next item
-        if (whole) {
-          if (in && lse) *lse = l == 0.f ? -INFINITY : (mref + log2f(l)) * kLn2;
-        } else {
-          __stcg(part + D * 128, l == 0.f ? -INFINITY : mref);
-          __stcg(part + D * 128 + 128, l);
-          __threadfence();
-          asm volatile("bar.sync 1, 256;" ::: "memory");
-          const uint32_t first = (uint32_t)(w.item0 / per), count = (uint32_t)((item1 - 1) / per) - first + 1;
-          if (tid == 0) {
-            __threadfence();
-            const bool last = atomicAdd(a.counters + first, 1u) == count - 1;
-            if (last) a.counters[first] = 0;
-            misc[1] = last;
-          }
-          asm volatile("bar.sync 1, 256;" ::: "memory");
-          if (misc[1]) {
-            __threadfence();
-            const float* parts = a.partials + i * (D * 128 + 256) + row;
-            auto part_of = [&](uint32_t p) { return parts + (size_t)(2 * (first + p) + (p == 0 ? 1 : 0)) * C::kPartFloats; };
-            float top = -INFINITY, all = 0.f;
-            for (uint32_t p = 0; p < count; ++p) top = fmaxf(top, __ldcg(part_of(p) + D * 128));
-            for (uint32_t p = 0; p < count; ++p) {
-              const float mp = __ldcg(part_of(p) + D * 128);
-              all += __ldcg(part_of(p) + D * 128 + 128) * (mp == -INFINITY ? 0.f : fast_exp2(mp - top));
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(y[e]);
             }
-            const float scale = all > 0.f ? 1.f / all : all == 0.f ? 0.f : NAN;
-#pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-              float o[32] = {};
-#pragma unroll 1
-              for (uint32_t p = 0; p < count; ++p) {
-                const float* src = part_of(p);
-                const float mp = __ldcg(src + D * 128), f = mp == -INFINITY ? 0.f : fast_exp2(mp - top);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) o[e] += f * __ldcg(src + (c + e) * 128);
-              }
-              if (in)
+            if (cuts.n == 0) {
+              if (x0.in)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                   uint32_t y[4];
 #pragma unroll
-                  for (int k = 0; k < 4; ++k) y[k] = pack_bf16x2(o[8 * e + 2 * k] * scale, o[8 * e + 2 * k + 1] * scale);
+                  for (int k = 0; k < 4; ++k)
+                    y[k] = pack_bf16x2(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv);
                   *reinterpret_cast<uint4*>(dst + (c + 8 * e) * 2) = make_uint4(y[0], y[1], y[2], y[3]);
                 }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) part[(c + e) * 128] = __uint_as_float(o[e]);
             }
-            if (in && lse) *lse = all == 0.f ? -INFINITY : (top + log2f(all)) * kLn2;
+          }
+          if (cuts.n == 0) {
+            if (x0.in && a.lse)
+              a.lse[(uint64_t)x0.tok * a.n_heads + x0.head] = l == 0.f ? -INFINITY : (mref + log2f(l)) * kLn2;
+          } else {
+            part[D * 128] = l == 0.f ? -INFINITY : mref;
+            part[D * 128 + 128] = l;
+            if (tid == 0 && w.item0 >= begin) *cut_item = CutItem{(uint32_t)cuts.n + 1, w.s, w.h, w.rb};
           }
         }
-        if (t < end) walk_on(w, a, cum, skip_rows);
+        w = w2;
+        x0 = x2;
       }
     } else if (warp < 12) {
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kOtherRegs));
       if (warp == 8) {
-        // ---- products: one lane issues them all --------------------------------------------------------
-        Walk w = walk_to(a, cum, skip_rows, begin);
-        if (lane == 0) {
-          constexpr uint32_t kF32Bf16 = 1u << 4 | 1u << 7 | 1u << 10 | 8u << 24;
-          constexpr uint32_t kQk = kF32Bf16 | (kKeys / 8) << 17, kPv = kF32Bf16 | 1u << 16 | (uint32_t)(D / 8) << 17;
-          uint32_t jg = 0, item = 0;
-          bool ok = true;
-          auto slot_wait = [&](uint32_t q) {
-            const uint32_t slot = q % C::kSlots;
-            ok = wait_or_give_up(full + 8 * slot, (q / C::kSlots) & 1, ok, a.error);
-            return base + C::kOffSlots + slot * C::kSlotBytes;
-          };
-          auto scores = [&](uint32_t i, uint32_t k_addr) {
+        // ---- products ------------------------------------------------------------------------------------
+        constexpr uint32_t kF32Bf16 = 1u << 4 | 1u << 7 | 1u << 10 | 8u << 24;
+        constexpr uint32_t kQk = kF32Bf16 | (kKeys / 8) << 17, kPv = kF32Bf16 | 1u << 16 | (uint32_t)(D / 8) << 17;
+        const uint32_t leader = lane == 0, tm = uniform(tmem);
+        const int32_t t_end = uniform(end);
+        uint32_t jg = 0, item = 0, js = 0;          // steps, items, steps of the second tile
+        bool ok = true;
+        auto wait_all = [&](uint32_t bar, uint32_t parity) {
+          ok = wait_or_give_up(bar, parity, ok, a.error);
+          __syncwarp();
+          tc_after();
+        };
+        auto slot_wait = [&](uint32_t q) {
+          const uint32_t slot = q % C::kSlots;
+          wait_all(full + 8 * slot, (q / C::kSlots) & 1);
+          return base + C::kOffSlots + slot * C::kSlotBytes;
+        };
+        auto scores = [&](uint32_t i, uint32_t k_addr) {
+          const uint64_t qd = smem_desc(base + i * C::kSlotBytes, 16), kd = smem_desc(k_addr, 16);
 #pragma unroll
-            for (uint32_t ks = 0; ks < D / 16; ++ks) {
-              const uint32_t off = (ks >> 2) * C::kSpanBytes + (ks & 3) * 32;
-              tc_mma_ss(tmem + i * 128, smem_desc(base + i * C::kSlotBytes + off, 16), smem_desc(k_addr + off, 16), kQk, ks > 0);
-            }
-          };
-          auto values = [&](uint32_t i, uint32_t v_addr, bool add) {
-#pragma unroll
-            for (uint32_t ks = 0; ks < kKeys / 16; ++ks)
-              tc_mma_ts(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, smem_desc(v_addr + ks * 2048, C::kSpanBytes), kPv, add || ks > 0);
-          };
-          for (int32_t t = begin; t < end; ++item) {
-            const int32_t stop = min(end, w.item0 + w.blk.n);
-            ok = wait_or_give_up(q_full, item & 1, ok, a.error);
-            tc_after();
-            uint32_t k_addr = slot_wait(2 * jg);
-            tc_after();
-            scores(0, k_addr);
-            tc_commit(s_full);
-            scores(1, k_addr);
-            tc_commit(s_full + 8);
-            tc_commit(empty + 8 * ((2 * jg) % C::kSlots));
-            for (bool first = true; t < stop; ++t, ++jg, first = false) {
-              const uint32_t v_addr = slot_wait(2 * jg + 1);
-              const bool more = t + 1 < stop;
-              ok = wait_or_give_up(p_full, jg & 1, ok, a.error);
-              tc_after();
-              values(0, v_addr, !first);
-              if (more) {
-                k_addr = slot_wait(2 * jg + 2);
-                scores(0, k_addr);
-                tc_commit(s_full);
-              } else {
-                tc_commit(o_full);
-              }
-              ok = wait_or_give_up(p_full + 8, jg & 1, ok, a.error);
-              tc_after();
-              values(1, v_addr, !first);
-              tc_commit(empty + 8 * ((2 * jg + 1) % C::kSlots));
-              if (more) {
-                scores(1, k_addr);
-                tc_commit(s_full + 8);
-                tc_commit(empty + 8 * ((2 * jg + 2) % C::kSlots));
-              } else {
-                tc_commit(o_full + 8);
-              }
-            }
-            if (t < end) walk_on(w, a, cum, skip_rows);
+          for (uint32_t ks = 0; ks < D / 16; ++ks) {
+            const uint32_t off = ((ks >> 2) * C::kSpanBytes + (ks & 3) * 32) >> 4;
+            tc_mma_ss(tm + i * 128, qd + off, kd + off, kQk, ks > 0, leader);
           }
+          tc_commit(s_full + 8 * i, leader);
+        };
+        auto values = [&](uint32_t i, uint32_t v_addr, uint32_t add, uint32_t step) {
+          const uint64_t vd = smem_desc(v_addr, C::kSpanBytes);
+          wait_all(p_half + 8 * i, step & 1);
+#pragma unroll
+          for (uint32_t ks = 0; ks < kKeys / 16; ++ks) {
+            if (ks == 2 * (C::kHalfAt + 1)) wait_all(p_full + 8 * i, step & 1);
+            tc_mma_ts(tm + 256 + i * 128, tm + i * 128 + ks * 8, vd + (ks * 2048 >> 4), kPv, ks > 0 ? 1u : add, leader);
+          }
+        };
+        Walk w = walk_to(a, cum, skip_rows, begin);
+        for (int32_t t = uniform(begin); t < t_end; ++item) {
+          const int32_t stop = uniform(min(end, w.item0 + w.blk.n));
+          const uint32_t two = uniform((uint32_t)((uint32_t)w.seq.n_new * a.group > w.rb * kQRows + 128));
+          wait_all(q_full, item & 1);
+          uint32_t k_addr = slot_wait(2 * jg);
+          scores(0, k_addr);
+          if (two) scores(1, k_addr);
+          tc_commit(empty + 8 * ((2 * jg) % C::kSlots), leader);
+          for (uint32_t add = 0; t < stop; ++t, ++jg, add = 1) {
+            const uint32_t v_addr = slot_wait(2 * jg + 1);
+            const bool more = t + 1 < stop;
+            if (more) k_addr = slot_wait(2 * jg + 2);
+            values(0, v_addr, add, jg);
+            if (more) scores(0, k_addr); else tc_commit(o_full, leader);
+            if (two) {
+              values(1, v_addr, add, js);
+              ++js;
+              if (more) scores(1, k_addr); else tc_commit(o_full + 8, leader);
+            }
+            tc_commit(empty + 8 * ((2 * jg + 1) % C::kSlots), leader);
+            if (more) tc_commit(empty + 8 * ((2 * jg + 2) % C::kSlots), leader);
+          }
+          if (t < t_end) walk_on(w, a, cum, skip_rows);
         }
+        // the last commit arrives before the block ends
+        (void)wait_or_give_up(empty + 8 * ((2 * jg - 1) % C::kSlots), ((2 * jg - 1) / C::kSlots) & 1, ok, a.error);
         __syncwarp();
       } else if (warp == 9) {
         // ---- cache tiles: one lane per page piece ------------------------------------------------------
@@ -652,10 +751,29 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       // ---- codes -> bf16: one thread per cache row -------------------------------------------------------
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kOtherRegs));
       const uint32_t row = tid & 127;
-      const uint32_t n = 2 * (uint32_t)(end - begin);
       bool ok = true;
-      for (uint32_t q = 0; q < n; ++q) {
-        const uint32_t raw = q % C::kRaws, slot = q % C::kSlots;
+      Walk w = walk_to(a, cum, skip_rows, begin);
+      int32_t t = begin;
+      uint32_t item = 0;
+      for (uint32_t q = 0; t < end; ++q) {
+        const uint32_t raw = q % C::kRaws, slot = q % C::kSlots, sc = q % C::kScaleSlots;
+        ok = wait_or_give_up(scale_full + 8 * sc, (q / C::kScaleSlots) & 1, ok, a.error);
+        if (q & 1) {
+          // a weight of zero must not meet a scale that is none: one past the end may be anything, and one that is not
+          // finite is taken out here and added to the rows that see it at the end
+          float* at = reinterpret_cast<float*>(smem + C::kOffScale) + sc * kKeys + row;
+          if ((w.blk.kt0 + t - w.item0) * (int32_t)kKeys + (int32_t)row >= w.seq.len) {
+            *at = 0.f;
+          } else if (!isfinite(*at)) {
+            misc[8 + item % 8] = 1;
+            *at = 0.f;
+          }
+          if (++t == min(end, w.item0 + w.blk.n) && t < end) {
+            walk_on(w, a, cum, skip_rows);
+            ++item;
+          }
+        }
+        bar_arrive(scale_ready + 8 * sc);
         ok = wait_or_give_up(raw_full + 8 * raw, (q / C::kRaws) & 1, ok, a.error);
         if (q >= C::kSlots) ok = wait_or_give_up(empty + 8 * slot, (q / C::kSlots + 1) & 1, ok, a.error);
         const char* src = smem + C::kOffRaw + raw * C::kRawBytes + row * D;
@@ -683,6 +801,46 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
   tc_before();
   __syncthreads();
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// Joins the items that blocks' shares cut: block (x, y) takes 32 rows of the item that is cut first in block x, its parts in order;
+// a lane owns a row, a warp an eighth of the columns.  A kernel of its own, because the last of many blocks to finish an
+// item would read all of its parts alone (256 rows x D fp32 each: 18 parts took it 20 us, this takes 3).
+template <int D>
+__global__ void __launch_bounds__(256) wb_attend_join_kernel(const __grid_constant__ AttendArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  constexpr uint32_t kPart = 2 * (D * 128 + 256), N = D / 8;
+  const uint32_t x = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const CutItem it = reinterpret_cast<const CutItem*>(a.cuts)[x];
+  if (!it.parts) return;
+  Walk w;
+  w.seq = attend_seq(a.b, it.s);
+  w.h = it.h;
+  w.rb = it.rb;
+  const uint32_t r = blockIdx.y * 32 + lane;
+  const RowOf row = row_of(a, w, r);
+  if (!__any_sync(0xFFFFFFFFu, row.in)) return;
+  const float* parts = a.partials + (r >> 7) * (D * 128 + 256) + (r & 127);
+  auto part_of = [&](uint32_t p) { return parts + (size_t)(2 * (x + p) + (p == 0 ? 1 : 0)) * kPart; };
+  float top = -INFINITY, sum = 0.f, o[N] = {};
+#pragma unroll 4
+  for (uint32_t p = 0; p < it.parts; ++p) top = fmaxf(top, part_of(p)[D * 128]);
+#pragma unroll 2
+  for (uint32_t p = 0; p < it.parts; ++p) {
+    const float* src = part_of(p);
+    const float m = src[D * 128], f = m == -INFINITY ? 0.f : fast_exp2(m - top);
+    sum += f * src[D * 128 + 128];
+#pragma unroll
+    for (uint32_t e = 0; e < N; ++e) o[e] += f * src[(warp * N + e) * 128];
+  }
+  if (!row.in) return;
+  const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : NAN;
+  uint4* dst = reinterpret_cast<uint4*>(a.out + (uint64_t)row.tok * a.o_token + row.head * a.o_head + warp * N * 2);
+#pragma unroll
+  for (uint32_t e = 0; e < N; e += 8)
+    dst[e / 8] = make_uint4(pack_bf16x2(o[e] * inv, o[e + 1] * inv), pack_bf16x2(o[e + 2] * inv, o[e + 3] * inv),
+                            pack_bf16x2(o[e + 4] * inv, o[e + 5] * inv), pack_bf16x2(o[e + 6] * inv, o[e + 7] * inv));
+  if (warp == 0 && a.lse) a.lse[(uint64_t)row.tok * a.n_heads + row.head] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 }  // namespace wbi
