@@ -597,7 +597,8 @@ wb_status wb_scan_slices(const wb_diff2_entry* nz, size_t n, uint64_t rows, uint
  * scale per row, scales contiguous as [n_pages][n_kv_heads][page_size]; the quantisation rule is
  * that of wb_bucket_quantize with the row in the place of the checkpoint tensor: s = amax / 448
  * (1 for a row of zeros, never zero otherwise), code = e4m3(x * (448 / amax)), saturating, or
- * e4m3(x / s) where 448 / amax is not finite; the value of a code is code * s in fp32.
+ * e4m3(x / s) where 448 / amax is not finite; the value of a code is code * s in fp32.  (A NaN code
+ * stands only in rows whose scale is not finite; wb_kv_attend relies on that.)
  * ------------------------------------------------------------------------------------------- */
 typedef struct {
   uint32_t dtype;       /* WB_BF16 or WB_E4M3                                                    */

@@ -12,28 +12,28 @@ using namespace wbi;
 namespace {
 
 constexpr uint32_t kHeaderBytes = 256;
-constexpr uint32_t kMaxRowTiles = 3;                    // wb_attend_rows_kernel: up to 16 * 3 rows
-constexpr uint32_t kMaxRowBlocks = 2 * kNumSMs;
+constexpr uint32_t kMaxRows = 32;                       // of wb_attend_rows_kernel
+constexpr uint32_t kMaxRowBlocks = 3 * kNumSMs;
 
-template <int D, bool Q, int MT>
-cudaError_t launch_rows(const AttendArgs& a, const wb_kv* kv, cudaStream_t stream) {
-  using C = RowsCfg<D, Q, MT>;
+template <int D, bool Q, int NT>
+cudaError_t launch_rows(const AttendArgs& a, cudaStream_t stream) {
+  using C = RowsCfg<D, Q, NT>;
   const size_t smem = C::smem_bytes(a.b.n_seqs);
-  auto kernel = wb_attend_rows_kernel<D, Q, MT>;
-  // every block gets the same share of the tiles, so the grid is exactly what fits at once: two blocks per SM for
-  // up to 16 rows (unless thousands of sequences make the table of prefix sums too large), else one
-  const uint32_t per_sm = MT == 1 && smem <= 113 * 1024 ? 2 : 1;
+  auto kernel = wb_attend_rows_kernel<D, Q, NT>;
+  // every block gets the same share of the tiles, so the grid is what fits at once (with thousands of sequences the table of
+  // prefix sums takes the place of a block)
+  const uint32_t per_sm = std::min<uint32_t>(C::kBlocksPerSm, (uint32_t)(kSmemPerSm / (smem + 2048)));
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  kernel<<<kNumSMs * per_sm, C::kThreads, smem, stream>>>(a, kv->map_k, kv->map_v);
+  kernel<<<kNumSMs * std::max(1u, per_sm), C::kThreads, smem, stream>>>(a);
   return cudaPeekAtLastError();
 }
 
 template <int D, bool Q>
-cudaError_t launch_rows_of(uint32_t rows, const AttendArgs& a, const wb_kv* kv, cudaStream_t stream) {
-  if (rows <= 16) return launch_rows<D, Q, 1>(a, kv, stream);
-  if (rows <= 32) return launch_rows<D, Q, 2>(a, kv, stream);
-  return launch_rows<D, Q, 3>(a, kv, stream);
+cudaError_t launch_rows_of(uint32_t rows, const AttendArgs& a, cudaStream_t stream) {
+  if (rows <= 8) return launch_rows<D, Q, 1>(a, stream);
+  if (rows <= 16) return launch_rows<D, Q, 2>(a, stream);
+  return launch_rows<D, Q, 4>(a, stream);
 }
 
 template <int D, bool Q>
@@ -71,7 +71,7 @@ cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_r
 
 constexpr uint32_t kCounterBytes = (kMaxRowBlocks * 4 + 255) / 256 * 256, kCutBytes = (kNumSMs * sizeof(CutItem) + 255) / 256 * 256;
 template <int D> constexpr size_t partial_bytes() {
-  return (size_t)2 * 4 * std::max({kMaxRowBlocks * RowsCfg<D, false, 1>::kPartFloats, kNumSMs * RowsCfg<D, false, kMaxRowTiles>::kPartFloats,
+  return (size_t)2 * 4 * std::max({kMaxRowBlocks * RowsCfg<D, true, 2>::kPartFloats, 2 * kNumSMs * RowsCfg<D, true, 4>::kPartFloats,
                                    kNumSMs * TilesCfg<D, false>::kPartFloats});
 }
 
@@ -114,13 +114,13 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   const cudaStream_t st = (cudaStream_t)stream;
   const uint64_t rows = (uint64_t)batch->max_new * a.group;
   cudaError_t err = cudaSuccess;
-  if (rows <= 16 * kMaxRowTiles || batch->n_seqs > 1) {
-    const uint32_t r = (uint32_t)std::min<uint64_t>(rows, 16 * kMaxRowTiles);
-    if (kv->d.head_dim == 128) err = e ? launch_rows_of<128, true>(r, a, kv, st) : launch_rows_of<128, false>(r, a, kv, st);
-    else err = e ? launch_rows_of<64, true>(r, a, kv, st) : launch_rows_of<64, false>(r, a, kv, st);
+  if (rows <= kMaxRows || batch->n_seqs > 1) {
+    const uint32_t r = (uint32_t)std::min<uint64_t>(rows, kMaxRows);
+    if (kv->d.head_dim == 128) err = e ? launch_rows_of<128, true>(r, a, st) : launch_rows_of<128, false>(r, a, st);
+    else err = e ? launch_rows_of<64, true>(r, a, st) : launch_rows_of<64, false>(r, a, st);
   }
-  if (err == cudaSuccess && rows > 16 * kMaxRowTiles) {
-    const uint32_t skip = batch->n_seqs > 1 ? 16 * kMaxRowTiles : 0;
+  if (err == cudaSuccess && rows > kMaxRows) {
+    const uint32_t skip = batch->n_seqs > 1 ? kMaxRows : 0;
     if (kv->d.head_dim == 128) err = e ? launch_tiles<128, true>(a, kv, skip, st) : launch_tiles<128, false>(a, kv, skip, st);
     else err = e ? launch_tiles<64, true>(a, kv, skip, st) : launch_tiles<64, false>(a, kv, skip, st);
   }

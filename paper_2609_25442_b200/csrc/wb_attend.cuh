@@ -64,7 +64,11 @@ __device__ __forceinline__ bool wait_or_give_up(uint32_t bar, uint32_t parity, b
   return ok;
 }
 
-// One box of a cache map: elements [x, ..) of slots [slot, slot + box_rows) of (head, page).
+// A value that all lanes of a converged warp share, such that the compiler knows it.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
+__device__ __forceinline__ int32_t uniform(int32_t x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
+
+// One box of a cache map: elements [x, ..) of the box's slots from `slot` on of (head, page).
 __device__ __forceinline__ void load_box(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t slot, int32_t head, int32_t page, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                ::"r"(dst), "l"(map), "r"(x), "r"(slot), "r"(head), "r"(page), "r"(bar) : "memory");

@@ -1,41 +1,51 @@
-// Attention for few rows: sequences whose new tokens times query heads per kv head are at most 64 rows
-// (single tokens, drafted chunks).  Every byte of the cache is used for a handful of products, so the bound
-// is memory bandwidth, and the kernel is a stream of cache tiles through shared memory:
+// Attention for few rows: sequences whose new tokens times query heads per kv head are at most 32 rows (single tokens, drafted
+// chunks).  Every byte of the cache is used for a handful of products, so the bound is memory bandwidth, and the kernel is a
+// stream of cache rows through shared memory:
 //
-//   - A tile is 64 cache rows of one kv head, keys and values.  One warp requests it by tensor-map loads (a box
-//     per page piece; pages that do not exist read as zeros), several tiles ahead.
-//   - A compute warp owns 16 of a tile's rows and 16 query rows, with its own running maximum and sum: scores
-//     and products on m16n8k16 matrix instructions, P straight from the score registers.  No two warps talk
-//     until an item ends.  The legacy matrix path is enough here: a tile takes 32 instructions per warp,
-//     far less time than its 16-32 KB take to arrive.
-//   - E4M3 tiles are widened to bf16 in registers between the shared load and the matrix instruction; the row
-//     scales multiply scores and weights.
-//   - Work is cut evenly over the SMs whatever the lengths: all (sequence, kv head) items form one line of
-//     tiles, every block takes the same number of consecutive tiles, and an item that crosses blocks is joined by
-//     the block that finishes it last, in the order of the tiles (so results do not depend on timing).
+//   - A warp owns 16 cache rows of every 64-row tile: it requests them itself, a few tiles ahead, into slots of its own, and it
+//     alone reads them.  16 divides the page size, so they are one contiguous piece of keys and one of values.  No warp waits
+//     for another until an item ends.  (Tensor-map loads of such small pieces cost the issuing warp 90 ns each, more
+//     than the arithmetic on them; a lane's 16-byte copies cost an instruction.)
+//   - Scores are computed as K Q^T and outputs as V^T P^T, so that the cache's 16 rows fill the instruction's 16 and the query
+//     rows, few as they are, only its 8 columns: for up to 8 query rows half the work of the usual orientation, and each
+//     code of an E4M3 cache is widened once for all rows.
+//   - E4M3 codes become f16 (exact, one instruction for two), queries f16 after a power of two that brings the row's largest
+//     value near 2^8 (what falls below f16's range is under 2^-32 of that value), and weights times row scales f16
+//     relative to a power of two that follows their maximum like the softmax's own: each keeps 11 bits down to 2^-14 of the
+//     largest so far, and is off by at most 2^-25 of it below.  (Widening to bf16 took 10 instructions for
+//     four codes, and the kernel was bound by them: 115 us where this takes WB_T_DEC8.)
+//   - The running maximum and the f16 exponent move only when a weight would pass 2^8, checked without any exchange: one vote.
+//   - Work is cut evenly over the SMs whatever the lengths: all (sequence, kv head) items form one line of tiles, every block
+//     takes the same number of consecutive tiles, and an item that crosses blocks is joined by the block that finishes it
+//     last, in the order of the tiles (so results do not depend on timing).
 #pragma once
 #include "wb_attend.cuh"
 
 namespace wbi {
 
-template <int D, bool Q, int MT>
+constexpr uint32_t kSmemPerSm = 233472, kSmemPerBlock = 232448;
+
+template <int D, bool Q, int NT>
 struct RowsCfg {
   static constexpr uint32_t kElem = Q ? 1 : 2;
   static constexpr uint32_t kRowBytes = D * kElem;
   static constexpr uint32_t kSpan = kRowBytes < 128 ? kRowBytes : 128;       // bytes of a row in one box
   static constexpr uint32_t kSpans = kRowBytes / kSpan;
-  static constexpr uint32_t kTileBytes = kKvTile * kRowBytes;                // keys, and as much of values
-  static constexpr uint32_t kScaleBytes = Q ? kKvTile * 4 : 0;
-  static constexpr uint32_t kStageBytes = 2 * kTileBytes;                    // the scales lie behind all stages
-  static constexpr uint32_t kStages = (MT == 1 ? 98304u : 163840u) / (2 * kTileBytes) > 8 ? 8 : (MT == 1 ? 98304u : 163840u) / (2 * kTileBytes);
-  static constexpr uint32_t kWarps = 4 * MT;                                 // compute warps
-  static constexpr uint32_t kThreads = 32 * (kWarps + 1);
-  static constexpr uint32_t kRegs = D / 2;                                   // accumulator registers of a lane: 16 x D
-  static constexpr uint32_t kJoinBytes = MT * kRegs * 32 * 4;
-  static constexpr uint32_t kPartFloats = MT * (kRegs * 32 + 32);            // one partial: accumulators, maxima, sums
-  static size_t smem_bytes(uint32_t n_seqs) {
-    return 1024 + kStages * (kStageBytes + 2 * kScaleBytes) + kJoinBytes + (n_seqs + 1) * 4 + MT * 4 * 16 * 8;
-  }
+  static constexpr uint32_t kPartBytes = 16 * kRowBytes;                     // a warp's keys of a tile, and as much of values
+  static constexpr uint32_t kSlotBytes = 2 * kPartBytes;
+  static constexpr uint32_t kScaleBytes = Q ? 128 : 0;                       // 16 scales of keys and of values
+  static constexpr uint32_t kRows = 8 * NT;                                  // query rows
+  static constexpr uint32_t kPitch = D + 4;                                  // floats; keeps the join free of bank conflicts
+  static constexpr uint32_t kJoinBytes = kRows * kPitch * 4;
+  static constexpr uint32_t kBlocksPerSm = NT == 4 || !Q ? 2 : 3;
+  static constexpr uint32_t kThreads = 128;
+  static constexpr uint32_t kPartFloats = kRows * D + 2 * kRows;             // one partial: outputs, maxima, sums
+  static constexpr uint32_t kFixedBytes = kJoinBytes + 4 * kRows * 8 + 1024; // with warps' maxima and sums, and alignment
+  // as many slots as leave room for the prefix sums of about 250 sequences
+  static constexpr uint32_t kSlots = (kSmemPerSm / kBlocksPerSm - 1024 - kFixedBytes - 1536) / (4 * (kSlotBytes + kScaleBytes)) > 8
+                                         ? 8 : (kSmemPerSm / kBlocksPerSm - 1024 - kFixedBytes - 1536) / (4 * (kSlotBytes + kScaleBytes));
+  static_assert(kSlots >= 2, "");
+  static size_t smem_bytes(uint32_t n_seqs) { return kFixedBytes + 4 * kSlots * (kSlotBytes + kScaleBytes) + (n_seqs + 1) * 4; }
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t a, uint32_t* r) {
@@ -44,10 +54,46 @@ __device__ __forceinline__ void ldsm4(uint32_t a, uint32_t* r) {
 __device__ __forceinline__ void ldsm4t(uint32_t a, uint32_t* r) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a));
 }
-__device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+template <bool F16> __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  if (F16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// 8 x 8 transposition: a lane's pair (row lane / 4, columns 2t, 2t + 1) -> (row 2t, 2t + 1 of column lane / 4)
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// the two codes of a half word as f16
+__device__ __forceinline__ uint32_t codes_to_f16x2(uint32_t codes) {
+  uint32_t r;
+  asm("{ .reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, l; }" : "=r"(r) : "r"(codes));
+  return r;
+}
+__device__ __forceinline__ uint32_t codes_hi_to_f16x2(uint32_t codes) {
+  uint32_t r;
+  asm("{ .reg .b16 l, h; mov.b32 {l, h}, %1; cvt.rn.f16x2.e4m3x2 %0, h; }" : "=r"(r) : "r"(codes));
+  return r;
+}
+
+// Asynchronous copies of a lane; with fewer source bytes the rest is zeros.
+__device__ __forceinline__ void copy16(uint32_t to, const void* from, uint32_t bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void* from, uint32_t bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Byte offset of 16-byte chunk `c` of row `row` in a swizzled block of rows of `SPAN` bytes.
 template <uint32_t SPAN> __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t c) {
@@ -58,41 +104,42 @@ __device__ __forceinline__ bool not_finite_bf16x2(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u) | ((w & 0x7F800000u) == 0x7F800000u);
 }
 
-template <int D, bool Q, int MT>
-__global__ void __launch_bounds__(RowsCfg<D, Q, MT>::kThreads, MT == 1 ? 2 : 1)
-wb_attend_rows_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
-  using C = RowsCfg<D, Q, MT>;
+// A warp's place in the line of tiles for its loads: sequence s, kv head h, tile j of the item's nt; its 16 rows of that
+// tile are slots [slot, slot + 16) of the table's entry `entry`.
+struct LoadWalk {
+  uint32_t s, entry, slot, entry0, slot0;
+  int32_t h, j, nt, left;  // left: positions from here to the end of the sequence
+  int32_t left0;
+  const int32_t* row;      // of the page table
+  int32_t page;            // -1: none
+};
+
+template <int D, bool Q, int NT>
+__global__ void __launch_bounds__(128, RowsCfg<D, Q, NT>::kBlocksPerSm)
+wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
+  using C = RowsCfg<D, Q, NT>;
   extern __shared__ char smem_raw[];
-  // stages (1024-byte aligned), their scales, join buffer, warps' maxima and sums, prefix sums
+  // slots (1024-byte aligned), their scales, join buffer, warps' maxima and sums, prefix sums
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
   char* const gen = smem_raw + (base - smem_addr(smem_raw));
-  const uint32_t scale_base = C::kStages * C::kStageBytes;
-  float* const join = reinterpret_cast<float*>(gen + scale_base + C::kStages * 2 * C::kScaleBytes);
-  float2* const warp_ml = reinterpret_cast<float2*>(join + C::kJoinBytes / 4);        // [mt][kw][16]
-  int32_t* const cum = reinterpret_cast<int32_t*>(warp_ml + MT * 4 * 16);
-  __shared__ __align__(8) uint64_t bars[2 * C::kStages];
-  __shared__ int32_t scan_tmp[32];
+  constexpr uint32_t kScaleBase = 4 * C::kSlots * C::kSlotBytes;
+  float* const join = reinterpret_cast<float*>(gen + kScaleBase + 4 * C::kSlots * C::kScaleBytes);
+  float2* const warp_ml = reinterpret_cast<float2*>(join + C::kJoinBytes / 4);        // [warp][row]
+  int32_t* const cum = reinterpret_cast<int32_t*>(warp_ml + 4 * C::kRows);
+  __shared__ int32_t scan_tmp[4];
   __shared__ uint32_t s_last;
-  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t full = smem_addr(bars), empty = full + 8 * C::kStages;
-
-  if (tid == 0) {
-    for (uint32_t i = 0; i < C::kStages; ++i) {
-      bar_init(full + 8 * i, 32);
-      bar_init(empty + 8 * i, C::kWarps);
-    }
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
+  __shared__ float down_of[C::kRows];      // what undoes the scaling of a row's query
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t4 = lane & 3, r8 = lane >> 2;
 
   // ---- the line of tiles: cum[s] = tiles of the sequences before s ---------------------------------
-  const uint32_t n_seqs = a.b.n_seqs, hk = a.c.n_kv_heads, rows_max = 16 * MT;
+  const uint32_t n_seqs = a.b.n_seqs, hk = a.c.n_kv_heads;
   {
-    const uint32_t per = (n_seqs + C::kThreads - 1) / C::kThreads, s0 = min(tid * per, n_seqs), s1 = min(s0 + per, n_seqs);
+    const uint32_t per = (n_seqs + 127) / 128, s0 = min(tid * per, n_seqs), s1 = min(s0 + per, n_seqs);
     int32_t sum = 0;
     for (uint32_t s = s0; s < s1; ++s) {
       const KvSeq q = attend_seq(a.b, s);
       int32_t nt = 0;
-      if (q.n_new > 0 && (uint32_t)q.n_new * a.group <= rows_max) {
+      if (q.n_new > 0 && (uint32_t)q.n_new * a.group <= C::kRows) {
         const int32_t lo = first_position(q, a.window) / (int32_t)kKvTile;
         nt = max(1, (q.len + (int32_t)kKvTile - 1) / (int32_t)kKvTile - lo);
       }
@@ -121,75 +168,106 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
   const int32_t begin = min((int32_t)blockIdx.x * per, total), end = min(begin + per, total);
   if (begin >= end) return;
 
-  // the sequence that tile `t` of the line belongs to
-  auto find = [&](int32_t t) {
-    uint32_t lo = 0, hi = n_seqs;        // cum[lo] <= t < cum[hi]
-    while (hi - lo > 1) {
-      const uint32_t mid = (lo + hi) >> 1;
-      if (cum[mid] <= t) lo = mid; else hi = mid;
+  uint32_t s = 0;
+  {
+    uint32_t hi = n_seqs;                // cum[s] <= begin < cum[hi]
+    while (hi - s > 1) {
+      const uint32_t mid = (s + hi) >> 1;
+      if (cum[mid] <= begin) s = mid; else hi = mid;
     }
-    return lo;
-  };
-
-  if (warp == C::kWarps) {
-    // ---- producer: one lane per page piece of a tile ---------------------------------------------
-    const uint32_t pieces = kKvTile / a.box_rows;
-    uint32_t s = find(begin);
-    int32_t t = begin;
-    uint32_t k = 0;
-    bool ok = true;
-    while (t < end) {
-      while (cum[s + 1] <= t) ++s;
-      const KvSeq q = attend_seq(a.b, s);
-      const int32_t tile0 = first_position(q, a.window) / (int32_t)kKvTile;
-      const int32_t nt = (cum[s + 1] - cum[s]) / (int32_t)hk;
-      const int32_t stop = min(end, cum[s + 1]);
-      for (; t < stop; ++t, ++k) {
-        const int32_t local = t - cum[s], h = local / nt, tile = tile0 + local - h * nt;
-        const uint32_t stage = k % C::kStages;
-        int32_t page = -1;
-        const int32_t pos = tile * (int32_t)kKvTile + (int32_t)(lane * a.box_rows);
-        if (lane < pieces && pos < q.len) page = kv_page(a.b, a.c.n_pages, a.c.page_size, s, pos);
-        if (k >= C::kStages) ok = wait_or_give_up(empty + 8 * stage, (k / C::kStages + 1) & 1, ok, a.error);
-        const uint32_t st = base + stage * C::kStageBytes, bar = full + 8 * stage;
-        if (lane < pieces) {
-          const uint32_t slot = (uint32_t)pos % a.c.page_size, row = lane * a.box_rows;
-          const int32_t where = page < 0 ? (int32_t)a.c.n_pages : page;      // outside: zeros
-          uint32_t bytes = 2 * a.box_rows * C::kRowBytes;
-          if (Q && page >= 0) bytes += 2 * a.box_rows * 4;
-          if (Q && page < 0)
-            for (uint32_t i = 0; i < a.box_rows; ++i) {
-              float* sc = reinterpret_cast<float*>(gen + scale_base + stage * (2 * C::kScaleBytes)) + row + i;
-              sc[0] = 0.f;
-              sc[kKvTile] = 0.f;
-            }
-          bar_arrive_tx(bar, bytes);
-#pragma unroll
-          for (uint32_t i = 0; i < C::kSpans; ++i) {
-            const uint32_t off = i * (kKvTile * C::kSpan) + row * C::kSpan;
-            load_box(st + off, &map_k, (int32_t)(i * C::kSpan / C::kElem), (int32_t)slot, h, where, bar);
-            load_box(st + C::kTileBytes + off, &map_v, (int32_t)(i * C::kSpan / C::kElem), (int32_t)slot, h, where, bar);
-          }
-          if (Q && page >= 0) {
-            const uint64_t at = ((uint64_t)page * hk + h) * a.c.page_size + slot;
-            const uint32_t to = base + scale_base + stage * (2 * C::kScaleBytes) + row * 4;
-            load_bulk(to, a.c.k_scale + at, a.box_rows * 4, bar);
-            load_bulk(to + C::kScaleBytes, a.c.v_scale + at, a.box_rows * 4, bar);
-          }
-        } else {
-          bar_arrive(bar);
-        }
-      }
-    }
-    return;      // the compute warps wait for every load
+    while (cum[s + 1] <= begin) ++s;
   }
 
-  // ---- compute warps ---------------------------------------------------------------------------------
-  const uint32_t mt = warp >> 2, kw = warp & 3, t4 = lane & 3, r8 = lane >> 2;
+  // ---- loads: the warp's 16 rows of a tile ------------------------------------------------------------
+  LoadWalk lw = {};
+  const uint32_t step_entry = kKvTile / a.c.page_size, step_slot = kKvTile % a.c.page_size;
+  auto enter_seq = [&]() {
+    const KvSeq q = attend_seq(a.b, lw.s);
+    const int32_t pos = first_position(q, a.window) / (int32_t)kKvTile * (int32_t)kKvTile + (int32_t)(warp * 16);
+    lw.nt = (cum[lw.s + 1] - cum[lw.s]) / (int32_t)hk;
+    lw.entry0 = (uint32_t)pos / a.c.page_size;
+    lw.slot0 = (uint32_t)pos % a.c.page_size;
+    lw.left0 = q.len - pos;
+    lw.row = a.b.table + (uint64_t)lw.s * a.b.table_stride;
+  };
+  auto enter_item = [&]() {
+    lw.j = 0;
+    lw.entry = lw.entry0;
+    lw.slot = lw.slot0;
+    lw.left = lw.left0;
+  };
+  auto fetch_page = [&]() {
+    lw.page = -1;
+    if (lw.left > 0 && lw.entry < a.b.table_stride) {
+      const int32_t x = __ldg(lw.row + lw.entry);
+      lw.page = (uint32_t)x < a.c.n_pages ? x : -1;
+    }
+  };
+  lw.s = s;
+  enter_seq();
+  enter_item();
+  lw.h = (begin - cum[s]) / lw.nt;
+  lw.j = begin - cum[s] - lw.h * lw.nt;
+  {
+    const uint32_t pos = lw.entry0 * a.c.page_size + lw.slot0 + (uint32_t)lw.j * kKvTile;
+    lw.entry = pos / a.c.page_size;
+    lw.slot = pos % a.c.page_size;
+    lw.left -= lw.j * (int32_t)kKvTile;
+  }
+  fetch_page();
+  // Requests tile number k of the block and steps on; the next tile's page is looked up now, for the next call.  The 16 rows are
+  // one contiguous piece of keys and one of values, so a lane's copies are at fixed distances from two addresses.
+  const uint32_t warp_slots = base + warp * C::kSlots * C::kSlotBytes;
+  auto request = [&](uint32_t k) {
+    const uint32_t slot = k % C::kSlots, at = warp_slots + slot * C::kSlotBytes;
+    const bool live = lw.page >= 0;
+    const uint64_t row = live ? (uint64_t)(uint32_t)lw.page * a.c.page_stride + (uint32_t)lw.h * a.c.head_stride + lw.slot * D : 0;
+    const char* src_k = a.c.k + row * C::kElem + lane * 16;
+    const char* src_v = a.c.v + row * C::kElem + lane * 16;
+    const uint32_t bytes = live ? 16 : 0;                                   // a page that does not exist reads as zeros
+#pragma unroll
+    for (uint32_t i = 0; i < C::kPartBytes / 512; ++i) {
+      const uint32_t off = i * 512 + lane * 16, r = off / C::kRowBytes, c = off % C::kRowBytes / 16;
+      const uint32_t to = at + c / 8 * (16 * C::kSpan) + swizzled<C::kSpan>(r, c % 8);
+      copy16(to, src_k + i * 512, bytes);
+      copy16(to + C::kPartBytes, src_v + i * 512, bytes);
+    }
+    if (Q) {
+      const float* scales = lane < 16 ? a.c.k_scale : a.c.v_scale;
+      const uint64_t sr = live ? ((uint64_t)(uint32_t)lw.page * hk + (uint32_t)lw.h) * a.c.page_size + lw.slot + (lane & 15) : 0;
+      copy4(base + kScaleBase + (warp * C::kSlots + slot) * C::kScaleBytes + lane * 4, scales + sr, live ? 4 : 0);
+    }
+    if (begin + (int32_t)k + 1 < end) {
+      if (++lw.j == lw.nt) {
+        if (++lw.h == (int32_t)hk) {
+          lw.h = 0;
+          do ++lw.s; while (cum[lw.s + 1] == cum[lw.s]);
+          enter_seq();
+        }
+        enter_item();
+      } else {
+        lw.entry += step_entry;
+        lw.slot += step_slot;
+        if (lw.slot >= a.c.page_size) {
+          lw.slot -= a.c.page_size;
+          ++lw.entry;
+        }
+        lw.left -= (int32_t)kKvTile;
+      }
+      fetch_page();
+    }
+  };
+  const uint32_t n_tiles = (uint32_t)(end - begin);
+  uint32_t requested = 0;
+  for (; requested < C::kSlots; ++requested) {
+    if (requested < n_tiles) request(requested);
+    copies_commit();
+  }
+
+  // ---- compute ---------------------------------------------------------------------------------------
   const float c2 = a.scale_log2;
-  uint32_t s = find(begin), k = 0;
+  uint32_t k = 0;
   int32_t t = begin;
-  bool ok = true;
   while (t < end) {
     while (cum[s + 1] <= t) ++s;
     const KvSeq seq = attend_seq(a.b, s);
@@ -197,22 +275,19 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
     const int32_t nt = (cum[s + 1] - cum[s]) / (int32_t)hk;
     const int32_t h = (t - cum[s]) / nt, item0 = cum[s] + h * nt, item1 = item0 + nt, stop = min(end, item1);
     const uint32_t n_rows = (uint32_t)seq.n_new * a.group;
+    const int32_t first_hi = seq.len - seq.n_new, last_lo = a.window ? seq.len - (int32_t)a.window : 0;
 
-    // this lane's two query rows: their range of positions and their fragments
-    int32_t hi[2], lo[2];
-    uint32_t qf[D / 16][4];
-    int32_t token[2];
-    uint32_t head[2];
+    // query fragments: rows lane / 4 of every group of 8 (32 rows: one group per warp, shared through the join buffer)
+    constexpr bool kShared = NT == 4;
+    uint32_t qf[kShared ? 1 : NT][D / 16][2];
+    float c2q[NT][2];                     // the softmax scale (of the scaled queries) of rows 2t, 2t + 1
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t r = mt * 16 + r8 + 8 * j;
+    for (int n = 0; n < (kShared ? 1 : NT); ++n) {
+      const uint32_t r = (kShared ? warp : n) * 8 + r8;
       const bool in = r < n_rows;
       const uint32_t i = in ? r / a.group : 0;
-      token[j] = in ? seq.row0 + (int32_t)i : -1;
-      head[j] = (uint32_t)h * a.group + (in ? r - i * a.group : 0);
-      hi[j] = in ? seq.len - seq.n_new + (int32_t)i : 0x7FFFFFFF;      // a row that is none sees everything
-      lo[j] = in && a.window ? hi[j] - (int32_t)a.window + 1 : 0;
-      const char* src = a.q + (uint64_t)max(token[j], 0) * a.q_token + head[j] * a.q_head;
+      const char* src = a.q + (uint64_t)(seq.row0 + (int32_t)i) * a.q_token + ((uint32_t)h * a.group + (in ? r - i * a.group : 0)) * a.q_head;
+      uint32_t big = 0;
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         uint32_t x = 0, y = 0;
@@ -225,317 +300,398 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a, const __grid_constan
             y = __ldg(reinterpret_cast<const uint32_t*>(src + ks * 32 + 16 + t4 * 4));
           }
         }
-        qf[ks][j] = x;
-        qf[ks][2 + j] = y;
+        if (Q) big = max(max(max(x & 0x7FFFu, (x >> 16) & 0x7FFFu), max(y & 0x7FFFu, (y >> 16) & 0x7FFFu)), big);
+        qf[n][ks][0] = x;
+        qf[n][ks][1] = y;
+      }
+      if (Q) {
+        big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
+        big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
+        // 2^(7 - exponent): an exponent field of e becomes 134; what is not finite stays so
+        const int32_t e = min(max((int32_t)(big >> 7), 8), 253);
+        const float up = __uint_as_float((uint32_t)(134 - e + 127) << 23), down = __uint_as_float((uint32_t)(e - 134 + 127) << 23);
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) qf[n][ks][b] = pack_f16x2(bf16_lo(qf[n][ks][b]) * up, bf16_hi(qf[n][ks][b]) * up);
+        if (kShared) {
+          if (t4 == 0) down_of[r] = down;
+        } else {
+          c2q[n][0] = c2 * __shfl_sync(0xFFFFFFFFu, down, t4 * 8);
+          c2q[n][1] = c2 * __shfl_sync(0xFFFFFFFFu, down, t4 * 8 + 4);
+        }
       }
     }
-    const int32_t first_hi = seq.len - seq.n_new, last_lo = a.window ? seq.len - (int32_t)a.window : 0;
-
-    float acc[D / 8][4];
+    const uint2* const shared_q = reinterpret_cast<const uint2*>(join) + lane;      // [group][k step][lane]
+    if (kShared) {
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
-    float top[2] = {-INFINITY, -INFINITY}, mc[2] = {0.f, 0.f}, sum[2] = {0.f, 0.f};   // raw maximum; maximum * c2, rounded once
+      for (int ks = 0; ks < D / 16; ++ks) reinterpret_cast<uint2*>(join)[(warp * (D / 16) + ks) * 32 + lane] = make_uint2(qf[0][ks][0], qf[0][ks][1]);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if (!Q) c2q[n][0] = c2q[n][1] = c2;
+      if (Q && kShared) {
+        c2q[n][0] = c2 * down_of[n * 8 + 2 * t4];
+        c2q[n][1] = c2 * down_of[n * 8 + 2 * t4 + 1];
+      }
+    }
+    auto query = [&](int n, int ks, uint32_t& b0, uint32_t& b1) {
+      if (kShared) {
+        const uint2 x = shared_q[(n * (D / 16) + ks) * 32];
+        b0 = x.x;
+        b1 = x.y;
+      } else {
+        b0 = qf[kShared ? 0 : n][ks][0];
+        b1 = qf[kShared ? 0 : n][ks][1];
+      }
+    };
+    // how far row r sees; a row that is none sees everything
+    const uint32_t group_inv = (65536 + a.group - 1) / a.group;      // r / group = r * group_inv >> 16 for r < 64
+    auto sees_to = [&](uint32_t r) { return r < n_rows ? first_hi + (int32_t)(r * group_inv >> 16) : 0x7FFFFFFF; };
+
+    float acc[NT][D / 16][4];
+    // what the weights are relative to (log2, negated), the score above which it moves, sums; 2^-(f16 exponent), the weight
+    // above which it moves
+    float refn[NT][2], thr[NT][2], sum[NT][2], ei[NT][2], lim[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) acc[n][i][0] = acc[n][i][1] = acc[n][i][2] = acc[n][i][3] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        refn[n][e] = 0.f;
+        thr[n][e] = -INFINITY;
+        sum[n][e] = ei[n][e] = lim[n][e] = 0.f;
+      }
+    }
 
     for (; t < stop; ++t, ++k) {
-      const uint32_t stage = k % C::kStages;
-      ok = wait_or_give_up(full + 8 * stage, (k / C::kStages) & 1, ok, a.error);
-      const uint32_t st = base + stage * C::kStageBytes;
-      const int32_t pos0 = (tile0 + t - item0) * (int32_t)kKvTile + (int32_t)(kw * 16);
-      float sc[2][4] = {};
-      // scores of 16 rows x 16 keys
+      const uint32_t slot = k % C::kSlots;
+      copies_wait<C::kSlots - 1>();
+      __syncwarp();
+      const uint32_t sk = base + (warp * C::kSlots + slot) * C::kSlotBytes, sv = sk + C::kPartBytes;
+      const int32_t pos0 = (tile0 + t - item0) * (int32_t)kKvTile + (int32_t)(warp * 16);
+      // scores: keys lane / 4, + 8 (registers 0 1, 2 3) x rows 2t, 2t + 1
+      float sc[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.f;
       if (Q) {
-        const uint32_t row = kw * 16 + (lane & 15);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ks += 2) {
           uint32_t w[4];
-          ldsm4(st + swizzled<C::kSpan>(row, ks + (lane >> 4)), w);
+          ldsm4(sk + swizzled<C::kSpan>(lane & 15, ks + (lane >> 4)), w);
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t f[4] = {codes_to_f16x2(w[2 * u]), codes_to_f16x2(w[2 * u + 1]), codes_hi_to_f16x2(w[2 * u]), codes_hi_to_f16x2(w[2 * u + 1])};
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-              const uint32_t x = w[2 * u + n];
-              mma16816(sc[n], qf[ks + u], e4m3_to_bf16x2(__byte_perm(x, 0, 0x1404)), e4m3_to_bf16x2(__byte_perm(x, 0, 0x3424)));
+            for (int n = 0; n < NT; ++n) {
+              uint32_t b0, b1;
+              query(n, ks + u, b0, b1);
+              mma16816<true>(sc[n], f, b0, b1);
             }
+          }
         }
       } else {
-        const uint32_t row = kw * 16 + (lane & 7) + ((lane >> 4) << 3);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
           uint32_t w[4];
-          ldsm4(st + (ks >> 2) * (kKvTile * 128) + swizzled<128>(row, (ks & 3) * 2 + ((lane >> 3) & 1)), w);
-          mma16816(sc[0], qf[ks], w[0], w[1]);
-          mma16816(sc[1], qf[ks], w[2], w[3]);
-        }
-      }
-      float vs[2][2] = {{1.f, 1.f}, {1.f, 1.f}};
-      if (Q) {
-        const float2* scales = reinterpret_cast<const float2*>(gen + scale_base + stage * (2 * C::kScaleBytes)) + kw * 8;
+          ldsm4(sk + (ks >> 2) * 2048 + swizzled<128>(lane & 15, (ks & 3) * 2 + (lane >> 4)), w);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          const float2 ksc = scales[n * 4 + t4], vsc = scales[kKvTile / 2 + n * 4 + t4];
-          sc[n][0] *= ksc.x; sc[n][1] *= ksc.y; sc[n][2] *= ksc.x; sc[n][3] *= ksc.y;
-          vs[n][0] = vsc.x; vs[n][1] = vsc.y;
+          for (int n = 0; n < NT; ++n) {
+            uint32_t b0, b1;
+            query(n, ks, b0, b1);
+            mma16816<false>(sc[n], w, b0, b1);
+          }
         }
       }
-      // a tile that some row sees only in part, or that passes the end of the cache
+      float vs[2] = {1.f, 1.f};
+      if (Q) {
+        const float* scales = reinterpret_cast<const float*>(gen + kScaleBase + (warp * C::kSlots + slot) * C::kScaleBytes) + r8;
+        const float k0 = scales[0], k1 = scales[8];
+        vs[0] = scales[16];
+        vs[1] = scales[24];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) { sc[n][0] *= k0; sc[n][1] *= k0; sc[n][2] *= k1; sc[n][3] *= k1; }
+      }
+      // rows that some query row does not see, or that lie past the end of the cache
       const bool partial = pos0 + 15 > first_hi || pos0 < last_lo;
       if (partial) {
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int32_t pos = pos0 + n * 8 + (int32_t)t4 * 2 + (e & 1);
-            if (pos > hi[e >> 1] || pos < lo[e >> 1]) sc[n][e] = -INFINITY;
+          for (int e = 0; e < 2; ++e) {
+            const int32_t up = sees_to(n * 8 + 2 * t4 + e), low = a.window && up != 0x7FFFFFFF ? up - (int32_t)a.window + 1 : 0;
+            const int32_t pos = pos0 + (int32_t)r8;
+            if (pos > up || pos < low) sc[n][e] = -INFINITY;
+            if (pos + 8 > up || pos + 8 < low) sc[n][2 + e] = -INFINITY;
           }
       }
-      // running maximum; the accumulators are rescaled only when some row's maximum moved
-      float corr[2];
-      bool moved = false;
+      // a new reference where a weight would pass 2^8
+      bool grow = false;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float m = fmaxf(fmaxf(sc[0][2 * j], sc[0][2 * j + 1]), fmaxf(sc[1][2 * j], sc[1][2 * j + 1]));
-        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
-        m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
-        corr[j] = 1.f;
-        if (m > top[j]) {
-          moved = true;
-          const float next = m * c2;
-          corr[j] = top[j] == -INFINITY ? 0.f : fast_exp2(mc[j] - next);
-          top[j] = m;
-          mc[j] = next;
-        }
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) grow |= fmaxf(sc[n][e], sc[n][2 + e]) > thr[n][e];
+      if (__any_sync(0xFFFFFFFFu, grow)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float m = fmaxf(sc[n][e], sc[n][2 + e]);
+            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
+            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
+            m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+            if (m > thr[n][e]) {
+              const float next = -m * c2q[n][e];
+              const float corr = thr[n][e] == -INFINITY ? 0.f : fast_exp2(next - refn[n][e]);
+              refn[n][e] = next;
+              thr[n][e] = fmaxf((8.f - next) / c2q[n][e], -3.0e38f);       // finite: -inf means that nothing was seen yet
+              sum[n][e] *= corr;
+#pragma unroll
+              for (int i = 0; i < D / 16; ++i) { acc[n][i][e] *= corr; acc[n][i][2 + e] *= corr; }
+            }
+          }
       }
-      if (__any_sync(0xFFFFFFFFu, moved)) {
+      uint32_t pf[NT][2];
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          acc[i][0] *= corr[0]; acc[i][1] *= corr[0];
-          acc[i][2] *= corr[1]; acc[i][3] *= corr[1];
-        }
-        sum[0] *= corr[0];
-        sum[1] *= corr[1];
-      }
-      uint32_t pf[4];
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        float p[4];
+      for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[e] = fast_exp2(fmaf(sc[n][e], c2, -mc[e >> 1]));
-          sum[e >> 1] += p[e];
-          // a scale of a position that is not seen may be anything
-          if (Q) p[e] = partial && p[e] == 0.f ? 0.f : p[e] * vs[n][e & 1];
-          sc[n][e] = p[e];
+          sc[n][e] = fast_exp2(fmaf(sc[n][e], c2q[n][e & 1], refn[n][e & 1]));
+          sum[n][e & 1] += sc[n][e];
         }
-        pf[2 * n] = pack_bf16x2(p[0], p[1]);
-        pf[2 * n + 1] = pack_bf16x2(p[2], p[3]);
-      }
-      // values
-      const uint32_t sv = st + C::kTileBytes;
-      if (Q) {
-        const uint32_t row = kw * 16 + (lane & 15);
+        if (Q) {
+          float p[4];
 #pragma unroll
-        for (int c = 0; c < D / 16; c += 2) {
-          uint32_t w[4];
-          ldsm4t(sv + swizzled<C::kSpan>(row, c + (lane >> 4)), w);
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const uint32_t x = w[2 * u], y = w[2 * u + 1];
-            mma16816(acc[2 * (c + u)], pf, e4m3_to_bf16x2(__byte_perm(x, 0, 0x2404)), e4m3_to_bf16x2(__byte_perm(y, 0, 0x2404)));
-            mma16816(acc[2 * (c + u) + 1], pf, e4m3_to_bf16x2(__byte_perm(x, 0, 0x3414)), e4m3_to_bf16x2(__byte_perm(y, 0, 0x3414)));
-          }
-        }
-      } else {
-        const uint32_t row = kw * 16 + (lane & 15);
-        // bf16 values of positions that a row does not see are multiplied by a weight of zero, which only finite
-        // ones survive: those past the end are cleared, and where the tile's own chunk or a window cuts it, values
-        // that are not finite are taken out and added by hand to the rows that do see them
-        uint32_t keep[2] = {0xFFFFFFFFu, 0xFFFFFFFFu};
-        bool odd = false;
-        if (partial) {
-#pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            const int32_t pos = pos0 + n * 8 + (int32_t)t4 * 2;
-            keep[n] = (pos < seq.len ? 0xFFFFu : 0u) | (pos + 1 < seq.len ? 0xFFFF0000u : 0u);
-          }
-        }
-#pragma unroll
-        for (int c = 0; c < D / 8; c += 2) {
-          uint32_t w[4];
-          ldsm4t(sv + (c >> 3) * (kKvTile * 128) + swizzled<128>(row, (c & 7) + (lane >> 4)), w);
+          for (int e = 0; e < 4; ++e) p[e] = sc[n][e] * vs[e >> 1];
           if (partial) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              w[i] &= keep[i & 1];
-              if (not_finite_bf16x2(w[i])) {
-                odd = true;
-                if ((w[i] & 0x7F80u) == 0x7F80u) w[i] &= 0xFFFF0000u;
-                if ((w[i] & 0x7F800000u) == 0x7F800000u) w[i] &= 0xFFFFu;
+            for (int e = 0; e < 4; ++e) p[e] = sc[n][e] == 0.f ? 0.f : p[e];      // a scale of a position that is not seen may be anything
+          }
+          const float m0 = fmaxf(p[0], p[2]), m1 = fmaxf(p[1], p[3]);
+          if (__any_sync(0xFFFFFFFFu, m0 > lim[n][0] || m1 > lim[n][1])) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              float m = e ? m1 : m0;
+              m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
+              m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
+              m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
+              const uint32_t b = min(max(__float_as_uint(m) >> 23, 1u), 253u);
+              const float next = __uint_as_float((254u - b) << 23);
+              if (m > lim[n][e] && (ei[n][e] == 0.f || next < ei[n][e])) {
+                const float corr = ei[n][e] == 0.f ? 0.f : next / ei[n][e];
+                ei[n][e] = next;
+                lim[n][e] = 256.f / next;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) { acc[n][i][e] *= corr; acc[n][i][2 + e] *= corr; }
               }
             }
           }
-          mma16816(acc[c], pf, w[0], w[1]);
-          mma16816(acc[c + 1], pf, w[2], w[3]);
+          pf[n][0] = transpose8(pack_f16x2(p[0] * ei[n][0], p[1] * ei[n][1]));
+          pf[n][1] = transpose8(pack_f16x2(p[2] * ei[n][0], p[3] * ei[n][1]));
+        } else {
+          pf[n][0] = transpose8(pack_bf16x2(sc[n][0], sc[n][1]));
+          pf[n][1] = transpose8(pack_bf16x2(sc[n][2], sc[n][3]));
+        }
+      }
+      // outputs: columns lane / 4, + 8 of 16 (codes: 2 (lane / 4), + 1) x rows 2t, 2t + 1
+      if (Q) {
+#pragma unroll
+        for (int c = 0; c < D / 16; c += 2) {
+          uint32_t w[4];
+          ldsm4t(sv + swizzled<C::kSpan>(lane & 15, c + (lane >> 4)), w);
+          if (partial) {      // a weight of zero must not meet a NaN code: 0x7F becomes 0x7E (its row's scale makes it NaN again)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) w[u] -= (((w[u] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7;
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t x = __byte_perm(w[2 * u], 0, 0x3120), y = __byte_perm(w[2 * u + 1], 0, 0x3120);
+            const uint32_t f[4] = {codes_to_f16x2(x), codes_hi_to_f16x2(x), codes_to_f16x2(y), codes_hi_to_f16x2(y)};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma16816<true>(acc[n][c + u], f, pf[n][0], pf[n][1]);
+          }
+        }
+      } else {
+        const uint32_t row = (lane & 7) + ((lane >> 4) << 3);
+        // bf16 values of positions that a row does not see are multiplied by a weight of zero, which only finite
+        // ones survive: those past the end are cleared, and where the chunk itself or a window cuts the tile, values
+        // that are not finite are taken out and added by hand to the rows that do see them
+        uint32_t keep[2];
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int32_t pos = pos0 + e * 8 + (int32_t)t4 * 2;
+          keep[e] = (pos < seq.len ? 0xFFFFu : 0u) | (pos + 1 < seq.len ? 0xFFFF0000u : 0u);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          uint32_t w[4];
+          ldsm4t(sv + (i >> 2) * 2048 + swizzled<128>(row, (i & 3) * 2 + ((lane >> 3) & 1)), w);
+          if (partial) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              w[e] &= keep[e >> 1];
+              if (not_finite_bf16x2(w[e])) {
+                odd = true;
+                if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
+                if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
+              }
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma16816<false>(acc[n][i], w, pf[n][0], pf[n][1]);
         }
         if (partial && __any_sync(0xFFFFFFFFu, odd)) {
-          const char* vals = gen + stage * C::kStageBytes + C::kTileBytes;
-#pragma unroll
-          for (int key = 0; key < 16; ++key) {
-            const int from = (int)(lane & ~3u) + ((key & 7) >> 1);
-            const float p0 = __shfl_sync(0xFFFFFFFFu, sc[key >> 3][key & 1], from);
-            const float p1 = __shfl_sync(0xFFFFFFFFu, sc[key >> 3][2 + (key & 1)], from);
-            const int32_t pos = pos0 + key;
-            if (pos >= seq.len) continue;
-            const uint32_t vr = kw * 16 + key;
+          const char* vals = gen + (warp * C::kSlots + slot) * C::kSlotBytes + C::kPartBytes;
 #pragma unroll 1
-            for (int c = 0; c < D / 8; ++c) {
-              const uint32_t v = *reinterpret_cast<const uint32_t*>(vals + (c >> 3) * (kKvTile * 128) + swizzled<128>(vr, c & 7) + t4 * 4);
-              if (!not_finite_bf16x2(v)) continue;
-              const float x = bf16_lo(v), y = bf16_hi(v);
-              const bool ox = (v & 0x7F80u) == 0x7F80u, oy = (v & 0x7F800000u) == 0x7F800000u;
+          for (int key = 0; key < 16; ++key) {
+            const int32_t pos = pos0 + key;
+            const int from = (key & 7) * 4 + (int)t4;
 #pragma unroll
-              for (int cc = 0; cc < D / 8; ++cc)
-                if (cc == c) {
-                  if (pos <= hi[0] && pos >= lo[0]) { if (ox) acc[cc][0] += p0 * x; if (oy) acc[cc][1] += p0 * y; }
-                  if (pos <= hi[1] && pos >= lo[1]) { if (ox) acc[cc][2] += p1 * x; if (oy) acc[cc][3] += p1 * y; }
+            for (int n = 0; n < NT; ++n) {
+              float p[2];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float x = __shfl_sync(0xFFFFFFFFu, sc[n][e], from), y = __shfl_sync(0xFFFFFFFFu, sc[n][2 + e], from);
+                p[e] = key < 8 ? x : y;
+              }
+#pragma unroll
+              for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                  const uint32_t d = i * 16 + half * 8 + r8;
+                  const uint32_t v = *reinterpret_cast<const uint16_t*>(vals + (d >> 6) * 2048 + swizzled<128>(key, (d >> 3) & 7) + (d & 7) * 2);
+                  if ((v & 0x7F80u) != 0x7F80u) continue;
+#pragma unroll
+                  for (int e = 0; e < 2; ++e) {
+                    const int32_t up = sees_to(n * 8 + 2 * t4 + e);
+                    if (pos < seq.len && pos <= up && !(a.window && up != 0x7FFFFFFF && pos <= up - (int32_t)a.window)) acc[n][i][2 * half + e] += p[e] * __uint_as_float(v << 16);
+                  }
                 }
             }
           }
         }
       }
+      // the slot is read: the tile kSlots on may come
       __syncwarp();
-      if (lane == 0) bar_arrive(empty + 8 * stage);
+      if (requested < n_tiles) request(requested++);
+      copies_commit();
     }
 
-    // ---- join the four warps of these query rows, in order ----------------------------------------
+    // ---- join the four warps of the block, in order -------------------------------------------------
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      sum[j] += __shfl_xor_sync(0xFFFFFFFFu, sum[j], 1);
-      sum[j] += __shfl_xor_sync(0xFFFFFFFFu, sum[j], 2);
-      if (t4 == 0) warp_ml[(mt * 4 + kw) * 16 + r8 + 8 * j] = make_float2(top[j] == -INFINITY ? -INFINITY : mc[j], sum[j]);
-    }
-    asm volatile("bar.sync 1, %0;" ::"n"(32 * C::kWarps) : "memory");
-    float all_m[2], all_l[2], mine[2];
+    for (int n = 0; n < NT; ++n)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      float2 ml[4];
-      all_m[j] = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        ml[w] = warp_ml[(mt * 4 + w) * 16 + r8 + 8 * j];
-        all_m[j] = fmaxf(all_m[j], ml[w].x);
+      for (int e = 0; e < 2; ++e) {
+        sum[n][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[n][e], 4);
+        sum[n][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[n][e], 8);
+        sum[n][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[n][e], 16);
+        if (r8 == 0) warp_ml[warp * C::kRows + n * 8 + 2 * t4 + e] = make_float2(thr[n][e] == -INFINITY ? -INFINITY : -refn[n][e], sum[n][e]);
       }
-      all_l[j] = 0.f;
-      mine[j] = 0.f;
+    __syncthreads();
+    float mine[NT][2];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float f = ml[w].x == -INFINITY ? 0.f : fast_exp2(ml[w].x - all_m[j]);
-        all_l[j] += ml[w].y * f;
-        if (w == (int)kw) mine[j] = f;
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, warp_ml[w * C::kRows + n * 8 + 2 * t4 + e].x);
+        mine[n][e] = thr[n][e] == -INFINITY ? 1.f : fast_exp2(-refn[n][e] - m);      // (nothing seen: zeros, or NaN)
+        if (Q) mine[n][e] = ei[n][e] == 0.f ? mine[n][e] : mine[n][e] / ei[n][e];
       }
-    }
-    float* buf = join + mt * (C::kRegs * 32) + lane;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      if (w == (int)kw) {
+    for (uint32_t w = 0; w < 4; ++w) {
+      if (w == warp) {
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float x = acc[i][e] * mine[e >> 1];
-            if (w > 0) x += buf[(i * 4 + e) * 32];
-            if (w < 3) buf[(i * 4 + e) * 32] = x;
-            acc[i][e] = x;
-          }
+          for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t d = Q ? i * 16 + 2 * r8 + (e >> 1) : i * 16 + r8 + 8 * (e >> 1);
+              float* at = join + (n * 8 + 2 * t4 + (e & 1)) * C::kPitch + d;
+              const float x = acc[n][i][e] * mine[n][e & 1];
+              *at = w == 0 ? x : *at + x;
+            }
       }
-      asm volatile("bar.sync 1, %0;" ::"n"(32 * C::kWarps) : "memory");
+      __syncthreads();
     }
 
     // ---- result: whole items directly, cut ones through the workspace ------------------------------
+    // a thread owns four columns of every (512 / D)-th row
+    constexpr uint32_t kStep = 512 / D;
+    const uint32_t d4 = (tid % (D / 4)) * 4, row_first = tid / (D / 4);
     const bool whole = item0 >= begin && item1 <= end;
-    if (!whole && kw == 3) {
-      float* part = a.partials + (size_t)(2 * blockIdx.x + (item0 >= begin ? 1 : 0)) * C::kPartFloats + mt * (C::kRegs * 32 + 32);
+    auto total_of = [&](uint32_t r, float& m, float& l) {
+      m = -INFINITY;
+      l = 0.f;
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i)
+      for (int w = 0; w < 4; ++w) m = fmaxf(m, warp_ml[w * C::kRows + r].x);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) __stcg(part + (i * 4 + e) * 32 + lane, acc[i][e]);
-      if (t4 == 0) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          __stcg(part + C::kRegs * 32 + r8 + 8 * j, all_m[j]);
-          __stcg(part + C::kRegs * 32 + 16 + r8 + 8 * j, all_l[j]);
+      for (int w = 0; w < 4; ++w) {
+        const float2 ml = warp_ml[w * C::kRows + r];
+        l += ml.x == -INFINITY ? ml.y : ml.y * fast_exp2(ml.x - m);
+      }
+    };
+    auto write_row = [&](uint32_t r, float4 o, float m, float l) {
+      const uint32_t i = r / a.group, head = (uint32_t)h * a.group + r - i * a.group;
+      const uint64_t token = (uint64_t)(seq.row0 + (int32_t)i);
+      const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+      *reinterpret_cast<uint2*>(a.out + token * a.o_token + head * a.o_head + d4 * 2) =
+          make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+      if (a.lse && d4 == 0) a.lse[token * a.n_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    };
+    if (whole) {
+      for (uint32_t r = row_first; r < n_rows; r += kStep) {
+        float m, l;
+        total_of(r, m, l);
+        write_row(r, *reinterpret_cast<const float4*>(join + r * C::kPitch + d4), m, l);
+      }
+    } else {
+      float* part = a.partials + (size_t)(2 * blockIdx.x + (item0 >= begin ? 1 : 0)) * C::kPartFloats;
+      for (uint32_t r = row_first; r < n_rows; r += kStep) {
+        float m, l;
+        total_of(r, m, l);
+        __stcg(reinterpret_cast<float4*>(part + r * D + d4), *reinterpret_cast<const float4*>(join + r * C::kPitch + d4));
+        if (d4 == 0) {
+          __stcg(part + C::kRows * D + r, l == 0.f ? -INFINITY : m);
+          __stcg(part + C::kRows * D + C::kRows + r, l);
         }
       }
       __threadfence();
-    }
-    bool mine_to_write = whole && kw == 3;
-    uint32_t i0 = 0, i1 = D / 8;
-    if (!whole) {
-      asm volatile("bar.sync 1, %0;" ::"n"(32 * C::kWarps) : "memory");
+      __syncthreads();
       const uint32_t first = (uint32_t)(item0 / per), count = (uint32_t)((item1 - 1) / per) - first + 1;
       if (tid == 0) {
         __threadfence();
         s_last = atomicAdd(a.counters + first, 1u) == count - 1;
         if (s_last) a.counters[first] = 0;
       }
-      asm volatile("bar.sync 1, %0;" ::"n"(32 * C::kWarps) : "memory");
+      __syncthreads();
       if (s_last) {
-        // every block's part is there: each warp joins a quarter of its rows' columns
         __threadfence();
-        mine_to_write = true;
-        i0 = kw * (D / 32);
-        i1 = i0 + D / 32;
-        auto part_of = [&](uint32_t p) {
-          return a.partials + (size_t)(2 * (first + p) + (p == 0 ? 1 : 0)) * C::kPartFloats + mt * (C::kRegs * 32 + 32);
-        };
-        all_m[0] = all_m[1] = -INFINITY;
-        for (uint32_t p = 0; p < count; ++p)
-#pragma unroll
-          for (int j = 0; j < 2; ++j) all_m[j] = fmaxf(all_m[j], __ldcg(part_of(p) + C::kRegs * 32 + r8 + 8 * j));
-        float o[D / 32][4] = {};
-        all_l[0] = all_l[1] = 0.f;
-#pragma unroll 2
-        for (uint32_t p = 0; p < count; ++p) {
-          const float* part = part_of(p);
-          float f[2];
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float m = __ldcg(part + C::kRegs * 32 + r8 + 8 * j);
-            f[j] = m == -INFINITY ? 0.f : fast_exp2(m - all_m[j]);
-            all_l[j] += f[j] * __ldcg(part + C::kRegs * 32 + 16 + r8 + 8 * j);
+        auto part_of = [&](uint32_t p) { return a.partials + (size_t)(2 * (first + p) + (p == 0 ? 1 : 0)) * C::kPartFloats; };
+        for (uint32_t r = row_first; r < n_rows; r += kStep) {
+          float m = -INFINITY, l = 0.f;
+#pragma unroll 8
+          for (uint32_t p = 0; p < count; ++p) m = fmaxf(m, __ldcg(part_of(p) + C::kRows * D + r));
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+          for (uint32_t p = 0; p < count; ++p) {
+            const float* src = part_of(p);
+            const float mp = __ldcg(src + C::kRows * D + r), lp = __ldcg(src + C::kRows * D + C::kRows + r);
+            const float4 x = __ldcg(reinterpret_cast<const float4*>(src + r * D + d4));
+            const float f = mp == -INFINITY ? (lp == 0.f ? 0.f : NAN) : fast_exp2(mp - m);
+            l += f * lp;
+            o.x += f * x.x; o.y += f * x.y; o.z += f * x.z; o.w += f * x.w;
           }
-#pragma unroll
-          for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[i][e] += f[e >> 1] * __ldcg(part + ((i0 + i) * 4 + e) * 32 + lane);
+          write_row(r, o, m, l);
         }
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if ((uint32_t)i / (D / 32) == kw) acc[i][e] = o[i % (D / 32)][e];
       }
     }
-    if (mine_to_write) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        if (token[j] < 0) continue;
-        const float inv = all_l[j] > 0.f ? 1.f / all_l[j] : all_l[j] == 0.f ? 0.f : NAN;
-        char* dst = a.out + (uint64_t)token[j] * a.o_token + head[j] * a.o_head;
-#pragma unroll
-        for (uint32_t i = 0; i < D / 8; i += 2) {
-          if (i < i0 || i >= i1) continue;
-          if (Q) {
-            *reinterpret_cast<uint2*>(dst + (i * 8 + 4 * t4) * 2) =
-                make_uint2(pack_bf16x2(acc[i][2 * j] * inv, acc[i + 1][2 * j] * inv), pack_bf16x2(acc[i][2 * j + 1] * inv, acc[i + 1][2 * j + 1] * inv));
-          } else {
-            *reinterpret_cast<uint32_t*>(dst + (i * 8 + 2 * t4) * 2) = pack_bf16x2(acc[i][2 * j] * inv, acc[i][2 * j + 1] * inv);
-            *reinterpret_cast<uint32_t*>(dst + (i * 8 + 8 + 2 * t4) * 2) = pack_bf16x2(acc[i + 1][2 * j] * inv, acc[i + 1][2 * j + 1] * inv);
-          }
-        }
-        if (a.lse && i0 == 0 && t4 == 0)
-          a.lse[(uint64_t)token[j] * a.n_heads + head[j]] = all_l[j] == 0.f ? -INFINITY : (all_m[j] + log2f(all_l[j])) * kLn2;
-      }
-    }
+    __syncthreads();       // the join buffer is free again
   }
 }
 

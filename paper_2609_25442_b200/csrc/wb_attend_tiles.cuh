@@ -58,8 +58,6 @@ struct TilesCfg {
 // The warp that issues products stays converged: every lane computes the same descriptors (so that they live in uniform
 // registers) and only the leader's instruction is let through.  Issued from a branch that one lane takes, each product costs
 // about 80 clocks of moves into uniform registers, more than the product itself.
-__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
-__device__ __forceinline__ int32_t uniform(int32_t x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
 __device__ __forceinline__ void tc_commit(uint32_t bar, uint32_t leader) {
   asm volatile("{ .reg .pred e; setp.ne.u32 e, %1, 0; @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0]; }"
                ::"r"(bar), "r"(leader) : "memory");
@@ -719,10 +717,9 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             const int32_t where = page < 0 ? (int32_t)a.c.n_pages : page;      // outside the cache: zeros
 #pragma unroll
             for (uint32_t kv = 0; kv < 2; ++kv) {
-              const uint32_t q = 2 * jg + kv, ring = Q ? C::kRaws : C::kSlots, slot = q % ring;
-              const uint32_t bar = (Q ? raw_full : full) + 8 * slot;
+              const uint32_t q = 2 * jg + kv, ring = Q ? C::kRaws : C::kSlots, slot = q % ring, sc = q % C::kScaleSlots;
+              const uint32_t bar = (Q ? raw_full : full) + 8 * slot, sbar = scale_full + 8 * sc;
               if (q >= ring) ok = wait_or_give_up((Q ? raw_empty : empty) + 8 * slot, (q / ring + 1) & 1, ok, a.error);
-              const uint32_t sc = q % C::kScaleSlots;
               if (Q && q >= C::kScaleSlots) ok = wait_or_give_up(scale_empty + 8 * sc, (q / C::kScaleSlots + 1) & 1, ok, a.error);
               const uint32_t dst = base + (Q ? C::kOffRaw + slot * C::kRawBytes : C::kOffSlots + slot * C::kSlotBytes);
               if (lane < pieces) {
@@ -731,16 +728,16 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
                 for (uint32_t e = 0; e < C::kRowSpans; ++e)
                   load_box(dst + e * (kKeys * C::kRowSpan) + r0 * C::kRowSpan, kv ? &map_v : &map_k, (int32_t)(e * 64), (int32_t)in_page, (int32_t)w.h, where, bar);
                 if (Q && page >= 0) {
-                  bar_arrive_tx(scale_full + 8 * sc, a.box_rows * 4);
+                  bar_arrive_tx(sbar, a.box_rows * 4);
                   load_bulk(base + C::kOffScale + (sc * kKeys + r0) * 4, (kv ? a.c.v_scale : a.c.k_scale) + ((uint64_t)page * hk + w.h) * a.c.page_size + in_page,
-                            a.box_rows * 4, scale_full + 8 * sc);
+                            a.box_rows * 4, sbar);
                 } else if (Q) {
                   for (uint32_t e = 0; e < a.box_rows; ++e) reinterpret_cast<float*>(smem + C::kOffScale)[sc * kKeys + r0 + e] = 0.f;
-                  bar_arrive(scale_full + 8 * sc);
+                  bar_arrive(sbar);
                 }
               } else {
                 bar_arrive(bar);
-                if (Q) bar_arrive(scale_full + 8 * sc);
+                if (Q) bar_arrive(sbar);
               }
             }
           }

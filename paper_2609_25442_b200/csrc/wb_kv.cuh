@@ -20,7 +20,7 @@ struct wb_kv {
 
 namespace wbi {
 
-constexpr uint32_t kKvTile = 64;   // cache rows per load tile of the attention kernels
+constexpr uint32_t kKvTile = 64;   // cache rows of a tile of the row kernel, and at most in a box
 
 struct KvView {
   char* k;
