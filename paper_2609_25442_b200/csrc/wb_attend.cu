@@ -1,5 +1,6 @@
 // Attention of a chunk of new tokens over the paged cache.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstring>
 
@@ -15,6 +16,37 @@ constexpr uint32_t kHeaderBytes = 256;
 constexpr uint32_t kMaxRows = 32;                       // of wb_attend_rows_kernel
 constexpr uint32_t kMaxRowBlocks = 3 * kNumSMs;
 
+// A kernel's dynamic shared memory is raised once per device to the most that it may ask for; with `regs`, the kernel has to have been
+// compiled to that many registers and no static shared memory.  Returns an error only where it cannot run at all.
+template <typename K> cudaError_t prepare_kernel(K kernel, uint32_t most, int regs, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  cudaFuncAttributes f;
+  if ((e = cudaFuncGetAttributes(&f, kernel)) != cudaSuccess) return e;
+  if (regs && (f.numRegs != regs || f.sharedSizeBytes != 0)) return cudaErrorInvalidConfiguration;
+  most = std::min<uint32_t>(most, 232448 - (uint32_t)f.sharedSizeBytes);
+  if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most)) != cudaSuccess) return e;
+  done.fetch_or(bit, std::memory_order_release);
+  return cudaSuccess;
+}
+
+// A joining kernel is set up while the kernel before it still runs, and waits for that one's end itself.
+cudaError_t launch_join(void (*kernel)(AttendArgs), dim3 grid, uint32_t threads, const AttendArgs& a, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 template <int D, bool Q, int NT>
 cudaError_t launch_rows(const AttendArgs& a, cudaStream_t stream) {
   using C = RowsCfg<D, Q, NT>;
@@ -23,10 +55,13 @@ cudaError_t launch_rows(const AttendArgs& a, cudaStream_t stream) {
   // every block gets the same share of the tiles, so the grid is what fits at once (with thousands of sequences the table of
   // prefix sums takes the place of a block)
   const uint32_t per_sm = std::min<uint32_t>(C::kBlocksPerSm, (uint32_t)(kSmemPerSm / (smem + 2048)));
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = prepare_kernel(kernel, 232448, 0, done);
   if (e != cudaSuccess) return e;
-  kernel<<<kNumSMs * std::max(1u, per_sm), C::kThreads, smem, stream>>>(a);
-  return cudaPeekAtLastError();
+  const uint32_t grid = kNumSMs * std::max(1u, per_sm);
+  kernel<<<grid, C::kThreads, smem, stream>>>(a);
+  if ((e = cudaPeekAtLastError()) != cudaSuccess) return e;
+  return launch_join(wb_attend_join_rows_kernel<D, NT>, dim3(grid, 2 * NT), 256, a, stream);
 }
 
 template <int D, bool Q>
@@ -40,12 +75,10 @@ template <int D, bool Q>
 cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_rows, cudaStream_t stream) {
   using C = TilesCfg<D, Q>;
   auto kernel = wb_attend_tiles_kernel<D, Q>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmemBytes);
-  if (e != cudaSuccess) return e;
   // the softmax warps wait for registers that the others give back: the launch has to have them
-  cudaFuncAttributes f;
-  if ((e = cudaFuncGetAttributes(&f, kernel)) != cudaSuccess) return e;
-  if (f.numRegs != C::kLaunchRegs || f.sharedSizeBytes != 0) return cudaErrorInvalidConfiguration;
+  static std::atomic<uint64_t> done{0};
+  cudaError_t e = prepare_kernel(kernel, C::kSmemBytes, C::kLaunchRegs, done);
+  if (e != cudaSuccess) return e;
   for (uint32_t s0 = 0; s0 < all.b.n_seqs; s0 += C::kMaxSeqs) {
     AttendArgs a = all;
     a.b.n_seqs = std::min(C::kMaxSeqs, all.b.n_seqs - s0);
@@ -54,22 +87,13 @@ cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_r
     a.b.kv_len += s0;
     kernel<<<kNumSMs, C::kThreads, C::kSmemBytes, stream>>>(a, kv->map_k, kv->map_v, skip_rows);
     if ((e = cudaPeekAtLastError()) != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(kNumSMs, kQRows / 32);
-    cfg.blockDim = dim3(256);
-    cfg.stream = stream;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // set up while the kernel before still runs
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    if ((e = cudaLaunchKernelEx(&cfg, wb_attend_join_kernel<D>, a)) != cudaSuccess) return e;
+    if ((e = launch_join(wb_attend_join_kernel<D>, dim3(kNumSMs, kQRows / 32), 256, a, stream)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
 
 
-constexpr uint32_t kCounterBytes = (kMaxRowBlocks * 4 + 255) / 256 * 256, kCutBytes = (kNumSMs * sizeof(CutItem) + 255) / 256 * 256;
+constexpr uint32_t kCutBytes = (kMaxRowBlocks * sizeof(CutItem) + 255) / 256 * 256;
 template <int D> constexpr size_t partial_bytes() {
   return (size_t)2 * 4 * std::max({kMaxRowBlocks * RowsCfg<D, true, 2>::kPartFloats, 2 * kNumSMs * RowsCfg<D, true, 4>::kPartFloats,
                                    kNumSMs * TilesCfg<D, false>::kPartFloats});
@@ -79,7 +103,7 @@ template <int D> constexpr size_t partial_bytes() {
 
 extern "C" size_t wb_kv_attend_workspace_bytes(const wb_kv* kv, uint32_t n_heads, uint32_t n_seqs) {
   if (!kv || !n_heads || n_seqs > WB_KV_MAX_SEQS) return 0;
-  return kHeaderBytes + kCounterBytes + kCutBytes + (kv->d.head_dim == 128 ? partial_bytes<128>() : partial_bytes<64>());
+  return kHeaderBytes + kCutBytes + (kv->d.head_dim == 128 ? partial_bytes<128>() : partial_bytes<64>());
 }
 
 extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* q, uint32_t n_heads,
@@ -107,9 +131,8 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   a.window = window;
   a.box_rows = kv->box_rows;
   a.error = (uint32_t*)workspace;
-  a.counters = (uint32_t*)((char*)workspace + kHeaderBytes);
-  a.cuts = (char*)workspace + kHeaderBytes + kCounterBytes;
-  a.partials = (float*)((char*)workspace + kHeaderBytes + kCounterBytes + kCutBytes);
+  a.cuts = (char*)workspace + kHeaderBytes;
+  a.partials = (float*)((char*)workspace + kHeaderBytes + kCutBytes);
   const bool e = kv->d.dtype == WB_E4M3;
   const cudaStream_t st = (cudaStream_t)stream;
   const uint64_t rows = (uint64_t)batch->max_new * a.group;

@@ -16,9 +16,14 @@ struct AttendArgs {
   uint32_t n_heads, group, window;
   uint32_t box_rows;
   uint32_t* error;                              // workspace: first word
-  uint32_t* counters;                           // row kernel: one per block, for the cut item that begins in it; zero between calls
-  char* cuts;                                   // CutItem of every block of the tile kernel
+  char* cuts;                                   // CutItem of every block
   float* partials;
+};
+
+// What a joining kernel reads of the item that is cut first in a block.
+struct CutItem {
+  uint32_t parts;          // 0: none
+  uint32_t s, h, rb;       // sequence, kv head, row block; for the row kernel: first row of the step's tensors, kv head, rows
 };
 
 constexpr float kLn2 = 0.69314718055994531f;

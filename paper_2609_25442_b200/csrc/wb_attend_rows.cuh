@@ -16,8 +16,8 @@
 //     four codes, and the kernel was bound by them: 115 us where this takes WB_T_DEC8.)
 //   - The running maximum and the f16 exponent move only when a weight would pass 2^8, checked without any exchange: one vote.
 //   - Work is cut evenly over the SMs whatever the lengths: all (sequence, kv head) items form one line of tiles, every block
-//     takes the same number of consecutive tiles, and an item that crosses blocks is joined by the block that finishes it
-//     last, in the order of the tiles (so results do not depend on timing).
+//     takes the same number of consecutive tiles, and a second kernel joins the items that cross blocks, in the order of the
+//     tiles (so results do not depend on timing).
 #pragma once
 #include "wb_attend.cuh"
 
@@ -36,7 +36,8 @@ struct RowsCfg {
   static constexpr uint32_t kScaleBytes = Q ? 128 : 0;                       // 16 scales of keys and of values
   static constexpr uint32_t kRows = 8 * NT;                                  // query rows
   static constexpr uint32_t kPitch = D + 4;                                  // floats; keeps the join free of bank conflicts
-  static constexpr uint32_t kJoinBytes = kRows * kPitch * 4;
+  static constexpr uint32_t kBuffers = NT == 4 ? 1 : 2;                      // of the join
+  static constexpr uint32_t kJoinBytes = kBuffers * kRows * kPitch * 4;
   static constexpr uint32_t kBlocksPerSm = NT == 4 || !Q ? 2 : 3;
   static constexpr uint32_t kThreads = 128;
   static constexpr uint32_t kPartFloats = kRows * D + 2 * kRows;             // one partial: outputs, maxima, sums
@@ -104,14 +105,11 @@ __device__ __forceinline__ bool not_finite_bf16x2(uint32_t w) {
   return ((w & 0x7F80u) == 0x7F80u) | ((w & 0x7F800000u) == 0x7F800000u);
 }
 
-// A warp's place in the line of tiles for its loads: sequence s, kv head h, tile j of the item's nt; its 16 rows of that
-// tile are slots [slot, slot + 16) of the table's entry `entry`.
-struct LoadWalk {
-  uint32_t s, entry, slot, entry0, slot0;
-  int32_t h, j, nt, left;  // left: positions from here to the end of the sequence
-  int32_t left0;
-  const int32_t* row;      // of the page table
-  int32_t page;            // -1: none
+// Where a warp's 16 rows of a tile are: slots [slot, slot + 16) of kv head h in a page, as the table has it (checked when used;
+// h is -1 if the position lies past the sequence or the table).
+struct TilePlace {
+  int32_t page, h;
+  uint32_t slot;
 };
 
 template <int D, bool Q, int NT>
@@ -127,7 +125,6 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   float2* const warp_ml = reinterpret_cast<float2*>(join + C::kJoinBytes / 4);        // [warp][row]
   int32_t* const cum = reinterpret_cast<int32_t*>(warp_ml + 4 * C::kRows);
   __shared__ int32_t scan_tmp[4];
-  __shared__ uint32_t s_last;
   __shared__ float down_of[C::kRows];      // what undoes the scaling of a row's query
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t4 = lane & 3, r8 = lane >> 2;
 
@@ -166,62 +163,51 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   const int32_t total = cum[n_seqs];
   const int32_t per = (total + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
   const int32_t begin = min((int32_t)blockIdx.x * per, total), end = min(begin + per, total);
+  CutItem* const cut_item = reinterpret_cast<CutItem*>(a.cuts) + blockIdx.x;
+  if (tid == 0) cut_item->parts = 0;
   if (begin >= end) return;
 
-  uint32_t s = 0;
-  {
-    uint32_t hi = n_seqs;                // cum[s] <= begin < cum[hi]
-    while (hi - s > 1) {
-      const uint32_t mid = (s + hi) >> 1;
-      if (cum[mid] <= begin) s = mid; else hi = mid;
+  // the sequence of tile t
+  auto find = [&](int32_t t) {
+    uint32_t lo = 0, hi = n_seqs;        // cum[lo] <= t < cum[hi]
+    while (hi - lo > 1) {
+      const uint32_t mid = (lo + hi) >> 1;
+      if (cum[mid] <= t) lo = mid; else hi = mid;
     }
-    while (cum[s + 1] <= begin) ++s;
-  }
+    while (cum[lo + 1] <= t) ++lo;
+    return lo;
+  };
 
   // ---- loads: the warp's 16 rows of a tile ------------------------------------------------------------
-  LoadWalk lw = {};
-  const uint32_t step_entry = kKvTile / a.c.page_size, step_slot = kKvTile % a.c.page_size;
-  auto enter_seq = [&]() {
-    const KvSeq q = attend_seq(a.b, lw.s);
-    const int32_t pos = first_position(q, a.window) / (int32_t)kKvTile * (int32_t)kKvTile + (int32_t)(warp * 16);
-    lw.nt = (cum[lw.s + 1] - cum[lw.s]) / (int32_t)hk;
-    lw.entry0 = (uint32_t)pos / a.c.page_size;
-    lw.slot0 = (uint32_t)pos % a.c.page_size;
-    lw.left0 = q.len - pos;
-    lw.row = a.b.table + (uint64_t)lw.s * a.b.table_stride;
-  };
-  auto enter_item = [&]() {
-    lw.j = 0;
-    lw.entry = lw.entry0;
-    lw.slot = lw.slot0;
-    lw.left = lw.left0;
-  };
-  auto fetch_page = [&]() {
-    lw.page = -1;
-    if (lw.left > 0 && lw.entry < a.b.table_stride) {
-      const int32_t x = __ldg(lw.row + lw.entry);
-      lw.page = (uint32_t)x < a.c.n_pages ? x : -1;
+  // Lane i looks tile 32 n + i of the block up, 16 tiles before the first of the 32 is requested, so that neither the search nor
+  // the table's latency is on the way of a request.
+  auto look_up = [&](uint32_t k0) {
+    TilePlace x = {-1, -1, 0};
+    const int32_t t = begin + (int32_t)(k0 + lane);
+    if (t < end) {
+      const uint32_t s = find(t);
+      const KvSeq q = attend_seq(a.b, s);
+      const int32_t nt = (cum[s + 1] - cum[s]) / (int32_t)hk, local = t - cum[s], h = local / nt;
+      const uint32_t pos = (uint32_t)(first_position(q, a.window) / (int32_t)kKvTile + local - h * nt) * kKvTile + warp * 16;
+      const uint32_t entry = pos / a.c.page_size;
+      x.slot = pos - entry * a.c.page_size;
+      if (pos < (uint32_t)q.len && entry < a.b.table_stride) {
+        x.h = h;
+        x.page = __ldg(a.b.table + (uint64_t)s * a.b.table_stride + entry);
+      }
     }
+    return x;
   };
-  lw.s = s;
-  enter_seq();
-  enter_item();
-  lw.h = (begin - cum[s]) / lw.nt;
-  lw.j = begin - cum[s] - lw.h * lw.nt;
-  {
-    const uint32_t pos = lw.entry0 * a.c.page_size + lw.slot0 + (uint32_t)lw.j * kKvTile;
-    lw.entry = pos / a.c.page_size;
-    lw.slot = pos % a.c.page_size;
-    lw.left -= lw.j * (int32_t)kKvTile;
-  }
-  fetch_page();
-  // Requests tile number k of the block and steps on; the next tile's page is looked up now, for the next call.  The 16 rows are
-  // one contiguous piece of keys and one of values, so a lane's copies are at fixed distances from two addresses.
+  TilePlace place = look_up(0), later = {-1, -1, 0};
+  // Requests tile number k of the block.  The 16 rows are one contiguous piece of keys and one of values, so a lane's copies
+  // are at fixed distances from two addresses.
   const uint32_t warp_slots = base + warp * C::kSlots * C::kSlotBytes;
   auto request = [&](uint32_t k) {
     const uint32_t slot = k % C::kSlots, at = warp_slots + slot * C::kSlotBytes;
-    const bool live = lw.page >= 0;
-    const uint64_t row = live ? (uint64_t)(uint32_t)lw.page * a.c.page_stride + (uint32_t)lw.h * a.c.head_stride + lw.slot * D : 0;
+    const uint32_t page = (uint32_t)__shfl_sync(0xFFFFFFFFu, place.page, k & 31), in_page = __shfl_sync(0xFFFFFFFFu, place.slot, k & 31);
+    const int32_t h = __shfl_sync(0xFFFFFFFFu, place.h, k & 31);
+    const bool live = h >= 0 && page < a.c.n_pages;
+    const uint64_t row = live ? (uint64_t)page * a.c.page_stride + (uint32_t)h * a.c.head_stride + in_page * D : 0;
     const char* src_k = a.c.k + row * C::kElem + lane * 16;
     const char* src_v = a.c.v + row * C::kElem + lane * 16;
     const uint32_t bytes = live ? 16 : 0;                                   // a page that does not exist reads as zeros
@@ -234,29 +220,64 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     }
     if (Q) {
       const float* scales = lane < 16 ? a.c.k_scale : a.c.v_scale;
-      const uint64_t sr = live ? ((uint64_t)(uint32_t)lw.page * hk + (uint32_t)lw.h) * a.c.page_size + lw.slot + (lane & 15) : 0;
+      const uint64_t sr = live ? ((uint64_t)page * hk + (uint32_t)h) * a.c.page_size + in_page + (lane & 15) : 0;
       copy4(base + kScaleBase + (warp * C::kSlots + slot) * C::kScaleBytes + lane * 4, scales + sr, live ? 4 : 0);
     }
-    if (begin + (int32_t)k + 1 < end) {
-      if (++lw.j == lw.nt) {
-        if (++lw.h == (int32_t)hk) {
-          lw.h = 0;
-          do ++lw.s; while (cum[lw.s + 1] == cum[lw.s]);
-          enter_seq();
+    if ((k & 31) == 15) later = look_up((k | 31) + 1);
+    if ((k & 31) == 31) place = later;
+  };
+  // ---- an item and its queries --------------------------------------------------------------------------
+  // query fragments: rows lane / 4 of every group of 8 (32 rows: one group per warp, shared through the join buffer)
+  constexpr bool kShared = NT == 4;
+  constexpr int kGroups = kShared ? 1 : NT;
+  struct Item {
+    uint32_t s, n_rows;
+    int32_t h, tile0, i0, i1, row0, len, n_new;      // i0, i1: its tiles in the line
+  };
+  auto enter = [&](Item& x, int32_t t) {
+    while (cum[x.s + 1] <= t) ++x.s;
+    const KvSeq q = attend_seq(a.b, x.s);
+    const int32_t nt = (cum[x.s + 1] - cum[x.s]) / (int32_t)hk;
+    x.tile0 = first_position(q, a.window) / (int32_t)kKvTile;
+    x.h = (t - cum[x.s]) / nt;
+    x.i0 = cum[x.s] + x.h * nt;
+    x.i1 = x.i0 + nt;
+    x.n_rows = (uint32_t)q.n_new * a.group;
+    x.row0 = q.row0;
+    x.len = q.len;
+    x.n_new = q.n_new;
+  };
+  uint32_t qf[kGroups][D / 16][2];
+  const uint32_t group_inv = (65536 + a.group - 1) / a.group;      // r / group = r * group_inv >> 16 for r < 64
+  auto fetch_queries = [&](const Item& x) {
+#pragma unroll
+    for (int n = 0; n < kGroups; ++n) {
+      const uint32_t r = (kShared ? warp : n) * 8 + r8;
+      const bool in = r < x.n_rows;
+      const uint32_t i = in ? r * group_inv >> 16 : 0;
+      const char* src = a.q + (uint64_t)(x.row0 + (int32_t)i) * a.q_token + ((uint32_t)x.h * a.group + (in ? r - i * a.group : 0)) * a.q_head;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        uint2 w = make_uint2(0, 0);
+        if (in) {
+          if (Q) {   // the k index of an instruction is permuted alike in both operands: four adjacent codes per lane
+            w = __ldg(reinterpret_cast<const uint2*>(src + ks * 32 + t4 * 8));
+          } else {
+            w.x = __ldg(reinterpret_cast<const uint32_t*>(src + ks * 32 + t4 * 4));
+            w.y = __ldg(reinterpret_cast<const uint32_t*>(src + ks * 32 + 16 + t4 * 4));
+          }
         }
-        enter_item();
-      } else {
-        lw.entry += step_entry;
-        lw.slot += step_slot;
-        if (lw.slot >= a.c.page_size) {
-          lw.slot -= a.c.page_size;
-          ++lw.entry;
-        }
-        lw.left -= (int32_t)kKvTile;
+        qf[n][ks][0] = w.x;
+        qf[n][ks][1] = w.y;
       }
-      fetch_page();
     }
   };
+
+  // the first item's queries are on their way before the cache's tiles crowd the memory
+  Item it = {};
+  it.s = find(begin);
+  enter(it, begin);
+  fetch_queries(it);
   const uint32_t n_tiles = (uint32_t)(end - begin);
   uint32_t requested = 0;
   for (; requested < C::kSlots; ++requested) {
@@ -269,42 +290,19 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   uint32_t k = 0;
   int32_t t = begin;
   while (t < end) {
-    while (cum[s + 1] <= t) ++s;
-    const KvSeq seq = attend_seq(a.b, s);
-    const int32_t tile0 = first_position(seq, a.window) / (int32_t)kKvTile;
-    const int32_t nt = (cum[s + 1] - cum[s]) / (int32_t)hk;
-    const int32_t h = (t - cum[s]) / nt, item0 = cum[s] + h * nt, item1 = item0 + nt, stop = min(end, item1);
-    const uint32_t n_rows = (uint32_t)seq.n_new * a.group;
-    const int32_t first_hi = seq.len - seq.n_new, last_lo = a.window ? seq.len - (int32_t)a.window : 0;
-
-    // query fragments: rows lane / 4 of every group of 8 (32 rows: one group per warp, shared through the join buffer)
-    constexpr bool kShared = NT == 4;
-    uint32_t qf[kShared ? 1 : NT][D / 16][2];
+    const Item cur = it;
+    const int32_t stop = min(end, cur.i1);
+    const uint32_t n_rows = cur.n_rows;
+    const int32_t first_hi = cur.len - cur.n_new, last_lo = a.window ? cur.len - (int32_t)a.window : 0;
     float c2q[NT][2];                     // the softmax scale (of the scaled queries) of rows 2t, 2t + 1
+    if (Q) {
 #pragma unroll
-    for (int n = 0; n < (kShared ? 1 : NT); ++n) {
-      const uint32_t r = (kShared ? warp : n) * 8 + r8;
-      const bool in = r < n_rows;
-      const uint32_t i = in ? r / a.group : 0;
-      const char* src = a.q + (uint64_t)(seq.row0 + (int32_t)i) * a.q_token + ((uint32_t)h * a.group + (in ? r - i * a.group : 0)) * a.q_head;
-      uint32_t big = 0;
+      for (int n = 0; n < kGroups; ++n) {
+        uint32_t big = 0;
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        uint32_t x = 0, y = 0;
-        if (in) {
-          if (Q) {   // the k index of an instruction is permuted alike in both operands: four adjacent codes per lane
-            const uint2 w = __ldg(reinterpret_cast<const uint2*>(src + ks * 32 + t4 * 8));
-            x = w.x; y = w.y;
-          } else {
-            x = __ldg(reinterpret_cast<const uint32_t*>(src + ks * 32 + t4 * 4));
-            y = __ldg(reinterpret_cast<const uint32_t*>(src + ks * 32 + 16 + t4 * 4));
-          }
-        }
-        if (Q) big = max(max(max(x & 0x7FFFu, (x >> 16) & 0x7FFFu), max(y & 0x7FFFu, (y >> 16) & 0x7FFFu)), big);
-        qf[n][ks][0] = x;
-        qf[n][ks][1] = y;
-      }
-      if (Q) {
+        for (int ks = 0; ks < D / 16; ++ks)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) big = max(max(qf[n][ks][b] & 0x7FFFu, (qf[n][ks][b] >> 16) & 0x7FFFu), big);
         big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 1));
         big = max(big, __shfl_xor_sync(0xFFFFFFFFu, big, 2));
         // 2^(7 - exponent): an exponent field of e becomes 134; what is not finite stays so
@@ -315,7 +313,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
           for (int b = 0; b < 2; ++b) qf[n][ks][b] = pack_f16x2(bf16_lo(qf[n][ks][b]) * up, bf16_hi(qf[n][ks][b]) * up);
         if (kShared) {
-          if (t4 == 0) down_of[r] = down;
+          if (t4 == 0) down_of[warp * 8 + r8] = down;
         } else {
           c2q[n][0] = c2 * __shfl_sync(0xFFFFFFFFu, down, t4 * 8);
           c2q[n][1] = c2 * __shfl_sync(0xFFFFFFFFu, down, t4 * 8 + 4);
@@ -347,7 +345,6 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       }
     };
     // how far row r sees; a row that is none sees everything
-    const uint32_t group_inv = (65536 + a.group - 1) / a.group;      // r / group = r * group_inv >> 16 for r < 64
     auto sees_to = [&](uint32_t r) { return r < n_rows ? first_hi + (int32_t)(r * group_inv >> 16) : 0x7FFFFFFF; };
 
     float acc[NT][D / 16][4];
@@ -371,7 +368,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       copies_wait<C::kSlots - 1>();
       __syncwarp();
       const uint32_t sk = base + (warp * C::kSlots + slot) * C::kSlotBytes, sv = sk + C::kPartBytes;
-      const int32_t pos0 = (tile0 + t - item0) * (int32_t)kKvTile + (int32_t)(warp * 16);
+      const int32_t pos0 = (cur.tile0 + t - cur.i0) * (int32_t)kKvTile + (int32_t)(warp * 16);
       // scores: keys lane / 4, + 8 (registers 0 1, 2 3) x rows 2t, 2t + 1
       float sc[NT][4];
 #pragma unroll
@@ -446,7 +443,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
               const float next = -m * c2q[n][e];
               const float corr = thr[n][e] == -INFINITY ? 0.f : fast_exp2(next - refn[n][e]);
               refn[n][e] = next;
-              thr[n][e] = fmaxf((8.f - next) / c2q[n][e], -3.0e38f);       // finite: -inf means that nothing was seen yet
+              thr[n][e] = fmaxf(m + __fdividef(8.f, c2q[n][e]), -3.0e38f);       // finite: -inf means that nothing was seen yet
               sum[n][e] *= corr;
 #pragma unroll
               for (int i = 0; i < D / 16; ++i) { acc[n][i][e] *= corr; acc[n][i][2 + e] *= corr; }
@@ -477,12 +474,12 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
               m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 4));
               m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
               m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
-              const uint32_t b = min(max(__float_as_uint(m) >> 23, 1u), 253u);
-              const float next = __uint_as_float((254u - b) << 23);
-              if (m > lim[n][e] && (ei[n][e] == 0.f || next < ei[n][e])) {
-                const float corr = ei[n][e] == 0.f ? 0.f : next / ei[n][e];
-                ei[n][e] = next;
-                lim[n][e] = 256.f / next;
+              const uint32_t b = min(max(__float_as_uint(m) >> 23, 1u), 246u), old = __float_as_uint(lim[n][e]) >> 23;
+              if (m > lim[n][e] && b + 8 > old) {
+                // 2^(old - new); from nothing (old = 0) there is nothing to scale
+                const float corr = old == 0 ? 0.f : __uint_as_float((uint32_t)max(127 + (int32_t)old - (int32_t)(b + 8), 0) << 23);
+                ei[n][e] = __uint_as_float((254u - b) << 23);
+                lim[n][e] = __uint_as_float((b + 8) << 23);
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) { acc[n][i][e] *= corr; acc[n][i][2 + e] *= corr; }
               }
@@ -523,7 +520,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int32_t pos = pos0 + e * 8 + (int32_t)t4 * 2;
-          keep[e] = (pos < seq.len ? 0xFFFFu : 0u) | (pos + 1 < seq.len ? 0xFFFF0000u : 0u);
+          keep[e] = (pos < cur.len ? 0xFFFFu : 0u) | (pos + 1 < cur.len ? 0xFFFF0000u : 0u);
         }
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
@@ -567,7 +564,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
                   for (int e = 0; e < 2; ++e) {
                     const int32_t up = sees_to(n * 8 + 2 * t4 + e);
-                    if (pos < seq.len && pos <= up && !(a.window && up != 0x7FFFFFFF && pos <= up - (int32_t)a.window)) acc[n][i][2 * half + e] += p[e] * __uint_as_float(v << 16);
+                    if (pos < cur.len && pos <= up && !(a.window && up != 0x7FFFFFFF && pos <= up - (int32_t)a.window)) acc[n][i][2 * half + e] += p[e] * __uint_as_float(v << 16);
                   }
                 }
             }
@@ -578,6 +575,11 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       __syncwarp();
       if (requested < n_tiles) request(requested++);
       copies_commit();
+    }
+
+    if (t < end) {         // the next item's queries arrive during the join
+      enter(it, t);
+      fetch_queries(it);
     }
 
     // ---- join the four warps of the block, in order -------------------------------------------------
@@ -600,11 +602,12 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
         for (int w = 0; w < 4; ++w) m = fmaxf(m, warp_ml[w * C::kRows + n * 8 + 2 * t4 + e].x);
         mine[n][e] = thr[n][e] == -INFINITY ? 1.f : fast_exp2(-refn[n][e] - m);      // (nothing seen: zeros, or NaN)
-        if (Q) mine[n][e] = ei[n][e] == 0.f ? mine[n][e] : mine[n][e] / ei[n][e];
+        if (Q && ei[n][e] != 0.f) mine[n][e] *= lim[n][e] * (1.f / 256.f);
       }
 #pragma unroll
-    for (uint32_t w = 0; w < 4; ++w) {
-      if (w == warp) {
+    for (uint32_t round = 0; round < 4 / C::kBuffers; ++round) {
+      if (round == warp / C::kBuffers) {
+        float* const buf = join + warp % C::kBuffers * (C::kRows * C::kPitch);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -612,9 +615,9 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t d = Q ? i * 16 + 2 * r8 + (e >> 1) : i * 16 + r8 + 8 * (e >> 1);
-              float* at = join + (n * 8 + 2 * t4 + (e & 1)) * C::kPitch + d;
+              float* at = buf + (n * 8 + 2 * t4 + (e & 1)) * C::kPitch + d;
               const float x = acc[n][i][e] * mine[n][e & 1];
-              *at = w == 0 ? x : *at + x;
+              *at = round == 0 ? x : *at + x;
             }
       }
       __syncthreads();
@@ -624,7 +627,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     // a thread owns four columns of every (512 / D)-th row
     constexpr uint32_t kStep = 512 / D;
     const uint32_t d4 = (tid % (D / 4)) * 4, row_first = tid / (D / 4);
-    const bool whole = item0 >= begin && item1 <= end;
+    const bool whole = cur.i0 >= begin && cur.i1 <= end;
     auto total_of = [&](uint32_t r, float& m, float& l) {
       m = -INFINITY;
       l = 0.f;
@@ -636,9 +639,17 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         l += ml.x == -INFINITY ? ml.y : ml.y * fast_exp2(ml.x - m);
       }
     };
+    auto joined = [&](uint32_t r) {
+      float4 x = *reinterpret_cast<const float4*>(join + r * C::kPitch + d4);
+      if (C::kBuffers == 2) {
+        const float4 y = *reinterpret_cast<const float4*>(join + (C::kRows + r) * C::kPitch + d4);
+        x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+      }
+      return x;
+    };
     auto write_row = [&](uint32_t r, float4 o, float m, float l) {
-      const uint32_t i = r / a.group, head = (uint32_t)h * a.group + r - i * a.group;
-      const uint64_t token = (uint64_t)(seq.row0 + (int32_t)i);
+      const uint32_t i = r * group_inv >> 16, head = (uint32_t)cur.h * a.group + r - i * a.group;
+      const uint64_t token = (uint64_t)(cur.row0 + (int32_t)i);
       const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
       *reinterpret_cast<uint2*>(a.out + token * a.o_token + head * a.o_head + d4 * 2) =
           make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
@@ -648,51 +659,86 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       for (uint32_t r = row_first; r < n_rows; r += kStep) {
         float m, l;
         total_of(r, m, l);
-        write_row(r, *reinterpret_cast<const float4*>(join + r * C::kPitch + d4), m, l);
+        write_row(r, joined(r), m, l);
       }
     } else {
-      float* part = a.partials + (size_t)(2 * blockIdx.x + (item0 >= begin ? 1 : 0)) * C::kPartFloats;
+      float* part = a.partials + (size_t)(2 * blockIdx.x + (cur.i0 >= begin ? 1 : 0)) * C::kPartFloats;
       for (uint32_t r = row_first; r < n_rows; r += kStep) {
         float m, l;
         total_of(r, m, l);
-        __stcg(reinterpret_cast<float4*>(part + r * D + d4), *reinterpret_cast<const float4*>(join + r * C::kPitch + d4));
+        __stcg(reinterpret_cast<float4*>(part + r * D + d4), joined(r));
         if (d4 == 0) {
           __stcg(part + C::kRows * D + r, l == 0.f ? -INFINITY : m);
           __stcg(part + C::kRows * D + C::kRows + r, l);
         }
       }
-      __threadfence();
-      __syncthreads();
-      const uint32_t first = (uint32_t)(item0 / per), count = (uint32_t)((item1 - 1) / per) - first + 1;
-      if (tid == 0) {
-        __threadfence();
-        s_last = atomicAdd(a.counters + first, 1u) == count - 1;
-        if (s_last) a.counters[first] = 0;
-      }
-      __syncthreads();
-      if (s_last) {
-        __threadfence();
-        auto part_of = [&](uint32_t p) { return a.partials + (size_t)(2 * (first + p) + (p == 0 ? 1 : 0)) * C::kPartFloats; };
-        for (uint32_t r = row_first; r < n_rows; r += kStep) {
-          float m = -INFINITY, l = 0.f;
-#pragma unroll 8
-          for (uint32_t p = 0; p < count; ++p) m = fmaxf(m, __ldcg(part_of(p) + C::kRows * D + r));
-          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-          for (uint32_t p = 0; p < count; ++p) {
-            const float* src = part_of(p);
-            const float mp = __ldcg(src + C::kRows * D + r), lp = __ldcg(src + C::kRows * D + C::kRows + r);
-            const float4 x = __ldcg(reinterpret_cast<const float4*>(src + r * D + d4));
-            const float f = mp == -INFINITY ? (lp == 0.f ? 0.f : NAN) : fast_exp2(mp - m);
-            l += f * lp;
-            o.x += f * x.x; o.y += f * x.y; o.z += f * x.z; o.w += f * x.w;
-          }
-          write_row(r, o, m, l);
-        }
-      }
+      if (tid == 0 && cur.i0 >= begin) *cut_item = CutItem{(uint32_t)((cur.i1 - 1) / per - cur.i0 / per) + 1, (uint32_t)cur.row0, (uint32_t)cur.h, n_rows};
     }
     __syncthreads();       // the join buffer is free again
   }
+}
+
+// Joins the items that blocks' shares cut: block (x, y) takes four rows of the item that is cut first in block x.  A kernel of its
+// own: the last block to finish an item would have to find that out (a fence and an atomic) and read all parts alone, 7 us of a
+// single token's 16 where this takes WB_T_JOIN.  A warp joins every eighth part, and the warps' results are joined in order.
+template <int D, int NT>
+__global__ void __launch_bounds__(256) wb_attend_join_rows_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr uint32_t kRows = 8 * NT, kPart = kRows * D + 2 * kRows;
+  constexpr uint32_t kLanes = D / 4, kAtOnce = 32 / kLanes, kG = 4 / kAtOnce;      // a lane owns four columns of kG rows
+  __shared__ float4 sums[8][4][kLanes];
+  __shared__ float2 ml[8][4];
+  const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, c = lane % kLanes, r0 = blockIdx.y * 4;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const CutItem it = reinterpret_cast<const CutItem*>(a.cuts)[blockIdx.x];       // (parts, first row, kv head, rows)
+  if (r0 >= it.rb || !it.parts) return;
+  const float* const parts = a.partials + (size_t)2 * blockIdx.x * kPart;
+  float4 o[kG];
+  float m[kG], l[kG];
+#pragma unroll
+  for (uint32_t g = 0; g < kG; ++g) {
+    o[g] = make_float4(0.f, 0.f, 0.f, 0.f);
+    m[g] = -INFINITY;
+    l[g] = 0.f;
+  }
+#pragma unroll 4
+  for (uint32_t p = warp; p < it.parts; p += 8) {
+    const float* src = parts + (size_t)(2 * p + (p == 0 ? 1 : 0)) * kPart;
+#pragma unroll
+    for (uint32_t g = 0; g < kG; ++g) {
+      const uint32_t r = min(r0 + g * kAtOnce + lane / kLanes, it.rb - 1);
+      const float mp = src[kRows * D + r], lp = src[kRows * D + kRows + r], next = fmaxf(m[g], mp);
+      const float4 x = *reinterpret_cast<const float4*>(src + r * D + c * 4);
+      const float f = m[g] == -INFINITY ? 1.f : fast_exp2(m[g] - next), h = mp == -INFINITY ? 1.f : fast_exp2(mp - next);   // (nothing seen: zeros, or NaN)
+      o[g].x = o[g].x * f + x.x * h; o[g].y = o[g].y * f + x.y * h; o[g].z = o[g].z * f + x.z * h; o[g].w = o[g].w * f + x.w * h;
+      l[g] = l[g] * f + lp * h;
+      m[g] = next;
+    }
+  }
+#pragma unroll
+  for (uint32_t g = 0; g < kG; ++g) {
+    sums[warp][g * kAtOnce + lane / kLanes][c] = o[g];
+    if (c == 0) ml[warp][g * kAtOnce + lane / kLanes] = make_float2(m[g], l[g]);
+  }
+  __syncthreads();
+  const uint32_t i = tid / kLanes, r = r0 + i;      // now a thread owns four columns of one row
+  if (i >= 4 || r >= it.rb) return;
+  float top = -INFINITY, all = 0.f;
+  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int w = 0; w < 8; ++w) top = fmaxf(top, ml[w][i].x);
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    const float2 part = ml[w][i];
+    const float f = part.x == -INFINITY ? 1.f : fast_exp2(part.x - top);
+    const float4 y = sums[w][i][c % kLanes];
+    all += part.y * f;
+    x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
+  }
+  const float inv = all > 0.f ? 1.f / all : all == 0.f ? 0.f : NAN;
+  const uint32_t token = r / a.group, head = it.h * a.group + r - token * a.group;
+  const uint64_t row = (uint64_t)it.s + token;
+  *reinterpret_cast<uint2*>(a.out + row * a.o_token + head * a.o_head + c * 8) = make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
+  if (a.lse && c == 0) a.lse[row * a.n_heads + head] = all == 0.f ? -INFINITY : (top + log2f(all)) * kLn2;
 }
 
 }  // namespace wbi

@@ -168,12 +168,6 @@ __device__ __forceinline__ Cuts cuts_of(int32_t i0, int32_t i1, int32_t per) {
   return Cuts{lo - 1, max(0, hi - lo + 1)};
 }
 
-// What the joining kernel reads of the item that is cut first in a block.
-struct CutItem {
-  uint32_t parts;          // 0: none
-  uint32_t s, h, rb;
-};
-
 // Where a block is in the line of tiles; every warp walks it alike.
 struct Walk {
   uint32_t s, h, rb, n_rb;

@@ -20,8 +20,7 @@ _DTYPE = {torch.float32: wb.WB_F32, torch.bfloat16: wb.WB_BF16, torch.float8_e4m
 _E4M3 = torch.float8_e4m3fn
 
 
-def _stream(device: torch.device) -> int:
-    return torch.cuda.current_stream(device).cuda_stream
+_stream = torch._C._cuda_getCurrentRawStream      # of a device index; torch.cuda.current_stream builds an object first
 
 
 def _require(ok: bool, what: str) -> None:
@@ -30,18 +29,20 @@ def _require(ok: bool, what: str) -> None:
 
 
 def _ints(t: torch.Tensor, name: str, device: torch.device) -> torch.Tensor:
-    _require(t.dtype == torch.int32 and t.device == device, f"{name}: an int32 tensor on {device} is needed")
+    if t.dtype != torch.int32 or t.device != device:
+        raise ValueError(f"{name}: an int32 tensor on {device} is needed")
     return t
 
 
 def _heads(t: torch.Tensor, name: str, n_tokens: int, heads: int, dim: int, device: torch.device) -> wb.wb_heads:
     """A step's tensor [tokens, heads, dim] with contiguous rows, as the C ABI takes it."""
-    _require(t.dim() == 3 and t.shape[0] == n_tokens and t.shape[1] == heads and t.shape[2] == dim,
-             f"{name}: shape {tuple(t.shape)}, expected {(n_tokens, heads, dim)}")
-    _require(t.device == device and t.dtype in _DTYPE, f"{name}: {t.dtype} on {t.device}")
+    dtype = _DTYPE.get(t.dtype)
+    if t.shape != (n_tokens, heads, dim) or t.device != device or dtype is None:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {(n_tokens, heads, dim)} on {device}")
     st, sh, se = t.stride()
-    _require(se == 1 and (st >= 0 and sh >= 0), f"{name}: rows must be contiguous")
-    return wb.wb_heads(t.data_ptr(), _DTYPE[t.dtype], 0, st, sh)
+    if se != 1 or st < 0 or sh < 0:
+        raise ValueError(f"{name}: rows must be contiguous")
+    return wb.wb_heads(t.data_ptr(), dtype, 0, st, sh)
 
 
 class KvBatch:
@@ -94,6 +95,7 @@ class KvCache:
                      "scales: contiguous fp32 [n_pages, n_kv_heads, page_size]")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.device = k.device
+        self._index = k.device.index
         self._kv = wb.Kv(wb.wb_kv_desc(_DTYPE[k.dtype], self.n_kv_heads, self.head_dim, self.page_size, self.n_pages,
                                        k.stride(0), k.stride(1), k.data_ptr(), v.data_ptr(),
                                        k_scale.data_ptr() if k_scale is not None else None,
@@ -112,7 +114,7 @@ class KvCache:
         """Append the new tokens' keys and values (bf16 or fp32, [n_tokens, n_kv_heads, head_dim])."""
         a = _heads(k, "k", batch.n_tokens, self.n_kv_heads, self.head_dim, self.device)
         b = _heads(v, "v", batch.n_tokens, self.n_kv_heads, self.head_dim, self.device)
-        self._kv.write(batch._for(self), a, b, _stream(self.device))
+        self._kv.write(batch._for(self), a, b, _stream(self._index))
 
     def read(self, batch: KvBatch, dtype: torch.dtype = torch.bfloat16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
         """Keys and values of the batch's positions, [n_tokens, n_kv_heads, head_dim] each."""
@@ -120,25 +122,26 @@ class KvCache:
         k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device))
         a = _heads(k, "out[0]", *shape, self.device)
         b = _heads(v, "out[1]", *shape, self.device)
-        self._kv.read(batch._for(self), a, b, _stream(self.device))
+        self._kv.read(batch._for(self), a, b, _stream(self._index))
         return k, v
 
     def attend(self, batch: KvBatch, q: torch.Tensor, *, workspace: "AttendWorkspace", scale: Optional[float] = None,
                window: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
         """Attention of the new tokens' queries (bf16, [n_tokens, n_heads, head_dim]) over the cache, causal at the
         sequences' ends; window > 0 limits a query to that many latest positions.  Returns (out, lse)."""
-        _require(q.dim() == 3, "q: [n_tokens, n_heads, head_dim]")
-        n, h = batch.n_tokens, int(q.shape[1])
+        if q.dim() != 3:
+            raise ValueError("q: [n_tokens, n_heads, head_dim]")
+        n, h = batch.n_tokens, q.shape[1]
         a = _heads(q, "q", n, h, self.head_dim, self.device)
         if out is None:
             out = torch.empty((n, h, self.head_dim), dtype=torch.bfloat16, device=self.device)
         if lse is None:
             lse = torch.empty((n, h), dtype=torch.float32, device=self.device)
-        _require(lse.shape == (n, h) and lse.dtype == torch.float32 and lse.is_contiguous() and lse.device == self.device,
-                 "lse: contiguous fp32 [n_tokens, n_heads]")
+        elif lse.shape != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != self.device:
+            raise ValueError("lse: contiguous fp32 [n_tokens, n_heads]")
         b = _heads(out, "out", n, h, self.head_dim, self.device)
         self._kv.attend(batch._for(self), a, h, b, lse.data_ptr(), self.head_dim ** -0.5 if scale is None else scale, window,
-                        workspace.buffer.data_ptr(), workspace.bytes, _stream(self.device))
+                        workspace.pointer, workspace.bytes, _stream(self._index))
         return out, lse
 
 
@@ -149,6 +152,7 @@ class AttendWorkspace:
         self.bytes = cache._kv.attend_workspace_bytes(n_heads, n_seqs)
         _require(self.bytes > 0, f"no workspace for {n_heads} heads and {n_seqs} sequences over this cache")
         self.buffer = torch.zeros(self.bytes, dtype=torch.uint8, device=cache.device)
+        self.pointer = self.buffer.data_ptr()
 
 
 def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tokens: torch.Tensor, draft_start: torch.Tensor,
@@ -159,16 +163,19 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
     uniform [n_drafts], draft_start [n_seqs + 1], race [n_seqs, vocab] (Exp(1) variates).  Returns (accepted [n_seqs],
     tokens [n_seqs, max_drafts + 1], -1 beyond the drawn token), int32."""
     dev = target.device
-    n, vocab, total = int(draft_start.shape[0]) - 1, int(target.shape[1]), int(draft_tokens.shape[0])
-    _require(target.is_cuda and target.dim() == 2 and n >= 0 and target.shape[0] == total + n and target.stride(1) == 1,
-             "target: [n_drafts + n_seqs, vocab] with contiguous rows on a CUDA device")
-    _require(target.dtype in (torch.float32, torch.bfloat16), f"probabilities of {target.dtype}: float32 or bfloat16")
-    _require(draft is None or (draft.shape == (total, vocab) and draft.dtype == target.dtype and draft.device == dev and draft.stride(1) == 1),
-             "draft: [n_drafts, vocab] of the target's type")
-    _require(uniform.shape == (total,) and uniform.dtype == torch.float32 and uniform.device == dev and uniform.is_contiguous(),
-             "uniform: fp32 [n_drafts]")
-    _require(race.shape == (n, vocab) and race.dtype == torch.float32 and race.device == dev and race.stride(1) == 1, "race: fp32 [n_seqs, vocab]")
-    _require(draft_tokens.is_contiguous() and draft_start.is_contiguous(), "draft_tokens, draft_start: contiguous")
+    n, vocab, total = draft_start.shape[0] - 1, target.shape[1], draft_tokens.shape[0]
+    if not target.is_cuda or target.dim() != 2 or n < 0 or target.shape[0] != total + n or target.stride(1) != 1:
+        raise ValueError("target: [n_drafts + n_seqs, vocab] with contiguous rows on a CUDA device")
+    if target.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"probabilities of {target.dtype}: float32 or bfloat16")
+    if draft is not None and (draft.shape != (total, vocab) or draft.dtype != target.dtype or draft.device != dev or draft.stride(1) != 1):
+        raise ValueError("draft: [n_drafts, vocab] of the target's type")
+    if uniform.shape != (total,) or uniform.dtype != torch.float32 or uniform.device != dev or not uniform.is_contiguous():
+        raise ValueError("uniform: fp32 [n_drafts]")
+    if race.shape != (n, vocab) or race.dtype != torch.float32 or race.device != dev or race.stride(1) != 1:
+        raise ValueError("race: fp32 [n_seqs, vocab]")
+    if not draft_tokens.is_contiguous() or not draft_start.is_contiguous():
+        raise ValueError("draft_tokens, draft_start: contiguous")
     _ints(draft_tokens, "draft_tokens", dev)
     _ints(draft_start, "draft_start", dev)
     accepted = torch.empty(n, dtype=torch.int32, device=dev)
@@ -178,5 +185,5 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
                                           None if none else draft.data_ptr(), max(target.stride(0), vocab),
                                           0 if none else max(draft.stride(0), vocab), max(race.stride(0), vocab),
                                           draft_tokens.data_ptr(), draft_start.data_ptr(), uniform.data_ptr(), race.data_ptr(),
-                                          accepted.data_ptr(), tokens.data_ptr()), _stream(dev))
+                                          accepted.data_ptr(), tokens.data_ptr()), _stream(dev.index))
     return accepted, tokens
