@@ -53,54 +53,85 @@ __device__ __forceinline__ void store8(char* p, const float* x) {
   }
 }
 
-// Where the block's tokens live: page and slot of each, page -1 for one that has no place.
+// Where the block's tokens live: page and slot of each, page -1 for one that has no place.  One warp: it finds the first token's
+// sequence by a 32-way search (a load per factor of 32, where a search per token would be five), and the others' by counting
+// the starts that follow.
 __device__ __forceinline__ void place_tokens(const KvView& c, const KvBatch& b, uint32_t t0, uint32_t n, int2* place) {
-  for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
-    const int32_t row = (int32_t)(t0 + i);
-    const uint32_t s = kv_seq_of_row(b, row);
-    const KvSeq q = kv_seq(b, s);
-    const int32_t at = row - q.row0;
-    const int32_t pos = q.len - q.n_new + at;
-    const bool in = at >= 0 && at < q.n_new;
-    const int32_t page = in ? kv_page(b, c.n_pages, c.page_size, s, pos) : -1;
-    place[i] = make_int2(page, page < 0 ? 0 : pos % (int32_t)c.page_size);
+  if (threadIdx.x < 32) {
+    const uint32_t lane = threadIdx.x;
+    const int32_t first = (int32_t)t0, row = (int32_t)(t0 + lane);
+    uint32_t lo = 0, hi = b.n_seqs;                     // new_start[lo] <= first < new_start[hi]
+    while (hi - lo > 1) {
+      const uint32_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+      const bool before = at < hi && (lane == 0 || __ldg(b.new_start + at) <= first);
+      const uint32_t k = 31 - __clz(__ballot_sync(0xFFFFFFFFu, before));
+      lo += k * step;
+      hi = min(hi, lo + step);
+    }
+    // sequences after the first that start within the block's tokens
+    uint32_t s = lo;
+    if (n > 1 && b.n_seqs > 1) {
+      const uint32_t next = lo + 1 + lane;
+      const int32_t start = next < b.n_seqs ? __ldg(b.new_start + next) : 0x7FFFFFFF;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) s += __shfl_sync(0xFFFFFFFFu, start, j) <= row;
+      if (s == lo + 32) s = kv_seq_of_row(b, row);      // more than 32 of them (most without tokens)
+    }
+    if (lane < n) {
+      const KvSeq q = kv_seq(b, s);
+      const int32_t at = row - q.row0, pos = q.len - q.n_new + at;
+      const int32_t page = at >= 0 && at < q.n_new ? kv_page(b, c.n_pages, c.page_size, s, pos) : -1;
+      place[lane] = make_int2(page, page < 0 ? 0 : pos % (int32_t)c.page_size);
+    }
   }
   __syncthreads();
 }
 
-// step tensor -> cache.  A row is D / 8 lanes wide; its maximum is found across them.
+// step tensor -> cache.  A thread has 32 elements of a row, as four pieces of 8 (D / 32 pieces apart, so that the threads of a row
+// read and write whole sectors): with so few threads to a row its maximum takes two exchanges at most, and the two exact divisions
+// of its scale are shared by 32 elements (16 threads to a row, 8 elements each: 42 us where this takes WB_T_WRITE).
 template <int D, bool F32, bool Q>
 __global__ void __launch_bounds__(kRowThreads)
 wb_kv_write_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {
-  constexpr uint32_t LANES = D / 8, ROWS = kRowThreads / LANES;
+  constexpr uint32_t LANES = D / 32, ROWS = kRowThreads / LANES;
   __shared__ int2 place[kTokensPerBlock];
   const uint32_t t0 = blockIdx.x * per_block, n = min(per_block, b.n_tokens - t0);
-  place_tokens(c, b, t0, n, place);
-  const uint32_t lane = threadIdx.x % LANES, per_token = 2 * c.n_kv_heads;
-  const uint32_t total = n * per_token, padded = (total + ROWS - 1) / ROWS * ROWS;
-#pragma unroll 4
-  for (uint32_t r = threadIdx.x / LANES; r < padded; r += ROWS) {
+  const uint32_t lane = threadIdx.x % LANES, per_token = 2 * c.n_kv_heads, total = n * per_token;
+  bool placed = false;
+  for (uint32_t r = threadIdx.x / LANES; r < (total + ROWS - 1) / ROWS * ROWS; r += ROWS) {
     const bool in = r < total;
-    const uint32_t i = in ? r / per_token : 0, w = in ? r - i * per_token : 0;
+    const uint32_t tok = in ? r / per_token : 0, w = in ? r - tok * per_token : 0;
     const bool is_v = w >= c.n_kv_heads;
-    const uint32_t h = is_v ? w - c.n_kv_heads : w;
-    const int2 at = place[i];
-    const bool live = in && at.x >= 0;
+    const uint32_t h = w - (is_v ? c.n_kv_heads : 0);
     const Rows& src = is_v ? v : k;
-    float x[8];
+    const char* from = src.data + (uint64_t)(t0 + tok) * src.token_stride + h * src.head_stride + lane * (F32 ? 32 : 16);
+    float x[4][8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    if (live) load8<F32>(src.data + (t0 + i) * src.token_stride + h * src.head_stride + lane * (F32 ? 32 : 16), x);
+    for (uint32_t j = 0; j < 4; ++j) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[j][e] = 0.f;
+      if (in) load8<F32>(from + j * (LANES * (F32 ? 32 : 16)), x[j]);
+    }
+    if (!placed) {                 // the rows are on their way meanwhile
+      place_tokens(c, b, t0, n, place);
+      placed = true;
+    }
+    const int2 at = place[tok];
+    const bool live = in && at.x >= 0;
     char* base = is_v ? c.v : c.k;
-    const uint64_t off = (uint64_t)at.x * c.page_stride + h * c.head_stride + (uint32_t)at.y * D + lane * 8;
+    const uint64_t off = (uint64_t)(uint32_t)at.x * c.page_stride + h * c.head_stride + (uint32_t)at.y * D + lane * 8;
     if (!Q) {
-      if (live) store8<false>(base + off * 2, x);
+      if (live)
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) store8<false>(base + (off + j * (LANES * 8)) * 2, x[j]);
       continue;
     }
     // magnitudes are compared as unsigned patterns, so that a NaN wins and makes the whole row NaN
     uint32_t m = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+    for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[j][e]) & 0x7FFFFFFFu);
 #pragma unroll
     for (uint32_t d = LANES / 2; d; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
     const float amax = __uint_as_float(m);
@@ -112,18 +143,25 @@ wb_kv_write_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {
     }
     if (!isfinite(inv)) {   // 448 / amax overflows (or is NaN): divide instead
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = __fdiv_rn(x[e], scale);
+      for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[j][e] = __fdiv_rn(x[j][e], scale);
       inv = 1.f;
     }
     if (live) {
-      uint2 codes;
-      codes.x = pack_e4m3x2(x[0] * inv, x[1] * inv) | (uint32_t)pack_e4m3x2(x[2] * inv, x[3] * inv) << 16;
-      codes.y = pack_e4m3x2(x[4] * inv, x[5] * inv) | (uint32_t)pack_e4m3x2(x[6] * inv, x[7] * inv) << 16;
-      __stcs(reinterpret_cast<uint2*>(base + off), codes);
-      if (lane == 0) (is_v ? c.v_scale : c.k_scale)[((uint64_t)at.x * c.n_kv_heads + h) * c.page_size + at.y] = scale;
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) {
+        uint2 codes;
+        codes.x = pack_e4m3x2(x[j][0] * inv, x[j][1] * inv) | (uint32_t)pack_e4m3x2(x[j][2] * inv, x[j][3] * inv) << 16;
+        codes.y = pack_e4m3x2(x[j][4] * inv, x[j][5] * inv) | (uint32_t)pack_e4m3x2(x[j][6] * inv, x[j][7] * inv) << 16;
+        *reinterpret_cast<uint2*>(base + off + j * (LANES * 8)) = codes;
+      }
+      if (lane == 0) (is_v ? c.v_scale : c.k_scale)[((uint64_t)(uint32_t)at.x * c.n_kv_heads + h) * c.page_size + at.y] = scale;
     }
   }
 }
+
+constexpr uint32_t kAhead = 4;      // rows whose loads a thread has in flight
 
 // cache -> step tensor
 template <int D, bool F32, bool Q>
@@ -134,41 +172,64 @@ wb_kv_read_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {
   const uint32_t t0 = blockIdx.x * per_block, n = min(per_block, b.n_tokens - t0);
   place_tokens(c, b, t0, n, place);
   const uint32_t lane = threadIdx.x % LANES, per_token = 2 * c.n_kv_heads, total = n * per_token;
-#pragma unroll 4
-  for (uint32_t r = threadIdx.x / LANES; r < total; r += ROWS) {
-    const uint32_t i = r / per_token, w = r - i * per_token;
-    const bool is_v = w >= c.n_kv_heads;
-    const uint32_t h = is_v ? w - c.n_kv_heads : w;
-    const int2 at = place[i];
-    const char* base = is_v ? c.v : c.k;
-    float x[8];
+  for (uint32_t r0 = threadIdx.x / LANES; r0 < total; r0 += kAhead * ROWS) {
+    uint4 raw[kAhead];
+    float scale[kAhead];
+    uint32_t tok[kAhead], which[kAhead];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    if (at.x >= 0) {
-      const uint64_t off = (uint64_t)at.x * c.page_stride + h * c.head_stride + (uint32_t)at.y * D + lane * 8;
-      if (Q) {
-        const uint2 codes = __ldcs(reinterpret_cast<const uint2*>(base + off));
-        const float s = __ldg((is_v ? c.v_scale : c.k_scale) + ((uint64_t)at.x * c.n_kv_heads + h) * c.page_size + at.y);
-        const uint32_t q[2] = {codes.x, codes.y};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 f = unpack_e4m3x2((uint16_t)(q[e >> 1] >> (16 * (e & 1))));
-          x[2 * e] = f.x * s;
-          x[2 * e + 1] = f.y * s;
+    for (uint32_t u = 0; u < kAhead; ++u) {
+      const uint32_t r = min(r0 + u * ROWS, total - 1);      // (the last rows may be read again, not written)
+      tok[u] = r / per_token;
+      which[u] = r - tok[u] * per_token;
+      const bool is_v = which[u] >= c.n_kv_heads;
+      const uint32_t h = which[u] - (is_v ? c.n_kv_heads : 0);
+      const int2 at = place[tok[u]];
+      raw[u] = make_uint4(0, 0, 0, 0);
+      scale[u] = 0.f;
+      if (at.x >= 0) {
+        const char* src = (is_v ? c.v : c.k) + ((uint64_t)(uint32_t)at.x * c.page_stride + h * c.head_stride + (uint32_t)at.y * D + lane * 8) * (Q ? 1 : 2);
+        if (Q) {
+          const uint2 x = __ldcs(reinterpret_cast<const uint2*>(src));
+          raw[u].x = x.x;
+          raw[u].y = x.y;
+          scale[u] = __ldg((is_v ? c.v_scale : c.k_scale) + ((uint64_t)(uint32_t)at.x * c.n_kv_heads + h) * c.page_size + at.y);
+        } else {
+          raw[u] = __ldcs(reinterpret_cast<const uint4*>(src));
         }
-      } else {
-        load8<false>(base + off * 2, x);
       }
     }
-    const Rows& dst = is_v ? v : k;
-    store8<F32>(dst.data + (t0 + i) * dst.token_stride + h * dst.head_stride + lane * (F32 ? 32 : 16), x);
+#pragma unroll
+    for (uint32_t u = 0; u < kAhead; ++u) {
+      if (r0 + u * ROWS >= total) continue;
+      const bool is_v = which[u] >= c.n_kv_heads;
+      const Rows& dst = is_v ? v : k;
+      char* to = dst.data + (uint64_t)(t0 + tok[u]) * dst.token_stride + (which[u] - (is_v ? c.n_kv_heads : 0)) * dst.head_stride + lane * (F32 ? 32 : 16);
+      if (!Q && !F32) {
+        __stcs(reinterpret_cast<uint4*>(to), raw[u]);
+        continue;
+      }
+      float x[8];
+      const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (Q) {
+          const float2 f = unpack_e4m3x2((uint16_t)(w[e >> 1] >> (16 * (e & 1))));
+          x[2 * e] = f.x * scale[u];
+          x[2 * e + 1] = f.y * scale[u];
+        } else {
+          x[2 * e] = bf16_lo(w[e]);
+          x[2 * e + 1] = bf16_hi(w[e]);
+        }
+      }
+      store8<F32>(to, x);
+    }
   }
 }
 
 template <bool WRITE, int D, bool F32, bool Q>
 void launch_rows(const KvView& c, const KvBatch& b, const Rows& k, const Rows& v, cudaStream_t stream) {
-  // as many tokens per block as leave eight blocks for every SM
-  const uint32_t per = std::min(kTokensPerBlock, std::max(1u, b.n_tokens / (kNumSMs * 8)));
+  // as many tokens per block as leave eight blocks for every SM (four where they are read: measured best of 4, 8, 16)
+  const uint32_t per = std::min(kTokensPerBlock, std::max(1u, b.n_tokens / (kNumSMs * (WRITE ? 8 : 4))));
   const uint32_t grid = (b.n_tokens + per - 1) / per;
   if (WRITE) wb_kv_write_kernel<D, F32, Q><<<grid, kRowThreads, 0, stream>>>(c, b, k, v, per);
   else wb_kv_read_kernel<D, F32, Q><<<grid, kRowThreads, 0, stream>>>(c, b, k, v, per);

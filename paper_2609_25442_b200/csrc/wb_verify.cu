@@ -11,6 +11,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "wb_kv.cuh"
@@ -20,36 +21,82 @@ using namespace wbi;
 
 namespace {
 
-constexpr uint32_t kVerifyThreads = 512;
-
 __device__ __forceinline__ float prob(const float* p, uint64_t i) { return __ldg(p + i); }
 __device__ __forceinline__ float prob(const uint16_t* p, uint64_t i) { return __uint_as_float((uint32_t)__ldg(p + i) << 16); }
-
 __device__ __forceinline__ uint64_t key_max(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
-// Scores are positive, so their bits order as they do; a larger complement is a lower index.
-__device__ __forceinline__ uint64_t race_key(float w, float e, uint32_t v, uint64_t best) {
-  if (!(w > 0.f)) return best;
-  const float score = __fdiv_rn(w, e);
-  if (!(score >= 0.f)) return best;     // a NaN or negative race variate takes no part
-  return key_max(best, (uint64_t)__float_as_uint(score) << 32 | (uint32_t)~v);
+
+// The best of a thread so far: its key (score bits above the complemented index; scores are positive, so their bits order as they
+// do, and a larger complement is a lower index), and the score a little lowered: a candidate whose weight does not exceed that
+// times its race variate cannot win, and is spared the division (all but about ln n of n candidates).
+struct Best {
+  uint64_t key = 0;                     // below every key: no weight is positive
+  float bar = 0.f;
+  __device__ __forceinline__ void offer(float w, float e, uint32_t v) {
+    if (!(w > 0.f) || !(w > bar * e)) return;
+    const float score = __fdiv_rn(w, e);
+    if (!(score >= 0.f)) return;        // a NaN or negative race variate takes no part
+    key = key_max(key, (uint64_t)__float_as_uint(score) << 32 | (uint32_t)~v);
+    bar = fmaxf(bar, score * 0.999999f);
+  }
+};
+
+// Eight probabilities from a 16-byte boundary.
+__device__ __forceinline__ void load8(const float* p, float* x) {
+  const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const uint16_t* p, float* x) {
+  const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
 }
 
-// mode 0: w = p; 1: w = max(p - q, 0); 2: w = p except for index `skip`
-template <typename T>
-__device__ __forceinline__ uint64_t race_range(const T* p, const T* q, const float* e, uint32_t v0, uint32_t v1, uint32_t skip, int mode) {
-  uint64_t best = 0;                    // below every key: no weight is positive
-  for (uint32_t v = v0 + threadIdx.x; v < v1; v += kVerifyThreads) {
-    float w = prob(p, v);
-    if (mode == 1) w -= prob(q, v);
-    if (mode == 2 && v == skip) w = 0.f;
-    best = race_key(w, __ldg(e + v), v, best);
+// w = p, or max(p - q, 0) where there is a q; index `skip` has none.  Rows that start on 16-byte boundaries are read eight
+// elements at a time; others element by element, four in flight.
+template <typename T, bool SUB, uint32_t kVerifyThreads>
+__device__ __forceinline__ Best race_range(const T* p, const T* q, const float* e, uint32_t v0, uint32_t v1, uint32_t skip) {
+  Best best;
+  uint32_t v = v0;
+  if ((((uintptr_t)(p + v0) | (uintptr_t)(e + v0) | (SUB ? (uintptr_t)(q + v0) : 0)) & 15u) == 0) {
+    const uint32_t whole = v0 + (v1 - v0) / 8 * 8;
+    for (v = v0 + threadIdx.x * 8; v < whole; v += kVerifyThreads * 8) {
+      float x[8], y[8], z[8];
+      load8(p + v, x);
+      load8(e + v, z);
+      if (SUB) load8(q + v, y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float w = SUB ? x[i] - y[i] : x[i];
+        if (v + i == skip) w = 0.f;
+        best.offer(w, z[i], v + i);
+      }
+    }
+    v = whole;
+  }
+  for (v += threadIdx.x; v < v1; v += 4 * kVerifyThreads) {
+    float x[4], y[4], z[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t at = min(v + i * kVerifyThreads, v1 - 1);
+      x[i] = prob(p, at);
+      z[i] = __ldg(e + at);
+      if (SUB) y[i] = prob(q, at);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t at = v + i * kVerifyThreads;
+      float w = SUB ? x[i] - y[i] : x[i];
+      if (at >= v1 || at == skip) w = 0.f;
+      best.offer(w, z[i], at);
+    }
   }
   return best;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kVerifyThreads) wb_verify_kernel(wb_verify_args a) {
+template <typename T, uint32_t kVerifyThreads>
+__global__ void __launch_bounds__(kVerifyThreads, 1024 / kVerifyThreads) wb_verify_kernel(wb_verify_args a) {
   cg::cluster_group cluster = cg::this_cluster();
   const uint32_t rank = cluster.block_rank(), size = cluster.num_blocks(), s = blockIdx.x / size;
   __shared__ uint64_t warp_best[kVerifyThreads / 32];
@@ -59,6 +106,10 @@ __global__ void __launch_bounds__(kVerifyThreads) wb_verify_kernel(wb_verify_arg
   const int32_t count = min(min(max(__ldg(a.draft_start + s + 1), start), (int32_t)a.n_drafts) - start, (int32_t)a.max_drafts);
   const T* target = reinterpret_cast<const T*>(a.target) + (uint64_t)(start + (int32_t)s) * a.target_stride;
   const T* draft = a.draft ? reinterpret_cast<const T*>(a.draft) + (uint64_t)start * a.draft_stride : nullptr;
+  const float* e = a.race + (uint64_t)s * a.race_stride;
+  const uint32_t share = ((a.vocab + size - 1) / size + 7) / 8 * 8, v0 = min(rank * share, a.vocab), v1 = min(v0 + share, a.vocab);
+  // the race is needed whatever is accepted: it comes into the second-level cache while that is found out
+  for (uint32_t v = v0 + threadIdx.x * 32; v < v1; v += kVerifyThreads * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(e + v));
   if (threadIdx.x < 32) {
     int accepted = 0;
     for (int i0 = 0; i0 < count; i0 += 32) {
@@ -84,12 +135,10 @@ __global__ void __launch_bounds__(kVerifyThreads) wb_verify_kernel(wb_verify_arg
   const T* p = target + (uint64_t)accepted * a.target_stride;
   const T* q = rejected && draft ? draft + (uint64_t)accepted * a.draft_stride : nullptr;
   const uint32_t skip = rejected && !draft ? (uint32_t)__ldg(a.draft_tokens + start + accepted) : 0xFFFFFFFFu;
-  const float* e = a.race + (uint64_t)s * a.race_stride;
-  const uint32_t share = (a.vocab + size - 1) / size, v0 = min(rank * share, a.vocab), v1 = min(v0 + share, a.vocab);
-  int mode = !rejected ? 0 : q ? 1 : 2;
+  int mode = !rejected ? 0 : q ? 1 : 2;      // w = p; max(p - q, 0); p except for index `skip`
   uint64_t best;
   for (;;) {
-    best = race_range<T>(p, q, e, v0, v1, skip, mode);
+    best = mode == 1 ? race_range<T, true, kVerifyThreads>(p, q, e, v0, v1, 0xFFFFFFFFu).key : race_range<T, false, kVerifyThreads>(p, nullptr, e, v0, v1, mode == 2 ? skip : 0xFFFFFFFFu).key;
 #pragma unroll
     for (int d = 16; d; d >>= 1) best = key_max(best, __shfl_xor_sync(0xFFFFFFFFu, best, d));
     if ((threadIdx.x & 31) == 0) warp_best[threadIdx.x >> 5] = best;
@@ -116,9 +165,19 @@ __global__ void __launch_bounds__(kVerifyThreads) wb_verify_kernel(wb_verify_arg
   }
 }
 
-template <typename T>
-wb_status launch_verify(const wb_verify_args& a, cudaStream_t stream) {
-  const uint32_t size = 8;
+template <typename T, uint32_t kVerifyThreads>
+wb_status launch_verify(const wb_verify_args& a, uint32_t size, cudaStream_t stream) {
+  auto kernel = wb_verify_kernel<T, kVerifyThreads>;
+  if (size > 8) {
+    static std::atomic<uint64_t> allowed{0};      // a bit per device
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (!(allowed.load(std::memory_order_acquire) & bit)) {
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
+      allowed.fetch_or(bit, std::memory_order_release);
+    }
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(a.n_seqs * size);
   cfg.blockDim = dim3(kVerifyThreads);
@@ -129,8 +188,17 @@ wb_status launch_verify(const wb_verify_args& a, cudaStream_t stream) {
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, wb_verify_kernel<T>, a) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
+  if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
   return WB_OK;
+}
+
+// Up to 18 sequences get 16 blocks of 512 threads each (not a portable cluster size, but every B200's): 7.9 us for one sequence of
+// 151936, where 256 threads take 8.5.  More get as many blocks of 256 threads, at most 8, as fit at once, four on an SM: 192
+// sequences of 128256 take 45 us with 2 blocks each, 51 with 4, and 57 with 3, which leave holes in the groups of SMs.
+template <typename T> wb_status launch_verify_of(const wb_verify_args& a, cudaStream_t stream) {
+  const uint32_t fit = kNumSMs * 4 / std::min<uint32_t>(a.n_seqs, kNumSMs * 4);
+  if (fit >= 32) return launch_verify<T, 512>(a, 16, stream);
+  return launch_verify<T, 256>(a, fit == 3 ? 2 : std::min(fit, 8u), stream);
 }
 
 }  // namespace
@@ -150,5 +218,5 @@ extern "C" wb_status wb_verify_drafts(const wb_verify_args* args, void* stream) 
   if (((uintptr_t)a.target | (uintptr_t)a.draft) % e || ((uintptr_t)a.race | (uintptr_t)a.uniform | (uintptr_t)a.draft_tokens |
       (uintptr_t)a.draft_start | (uintptr_t)a.accepted | (uintptr_t)a.tokens) % 4)
     return WB_ERR_INVALID_ARG;
-  return a.dtype == WB_F32 ? launch_verify<float>(a, (cudaStream_t)stream) : launch_verify<uint16_t>(a, (cudaStream_t)stream);
+  return a.dtype == WB_F32 ? launch_verify_of<float>(a, (cudaStream_t)stream) : launch_verify_of<uint16_t>(a, (cudaStream_t)stream);
 }

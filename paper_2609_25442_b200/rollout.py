@@ -96,6 +96,9 @@ class KvCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.device = k.device
         self._index = k.device.index
+        self._scale = self.head_dim ** -0.5
+        # new_empty of these allocates results without looking a device and a type up again
+        self._like = {t: torch.empty(0, dtype=t, device=k.device) for t in (torch.float32, torch.bfloat16)}
         self._kv = wb.Kv(wb.wb_kv_desc(_DTYPE[k.dtype], self.n_kv_heads, self.head_dim, self.page_size, self.n_pages,
                                        k.stride(0), k.stride(1), k.data_ptr(), v.data_ptr(),
                                        k_scale.data_ptr() if k_scale is not None else None,
@@ -119,9 +122,17 @@ class KvCache:
     def read(self, batch: KvBatch, dtype: torch.dtype = torch.bfloat16, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None):
         """Keys and values of the batch's positions, [n_tokens, n_kv_heads, head_dim] each."""
         shape = (batch.n_tokens, self.n_kv_heads, self.head_dim)
-        k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=self.device), torch.empty(shape, dtype=dtype, device=self.device))
-        a = _heads(k, "out[0]", *shape, self.device)
-        b = _heads(v, "out[1]", *shape, self.device)
+        if out is None:
+            if dtype not in self._like:
+                raise ValueError(f"rows of {dtype}: float32 or bfloat16")
+            k, v = self._like[dtype].new_empty((2, *shape)).unbind(0)
+            step = self.n_kv_heads * self.head_dim
+            a = wb.wb_heads(k.data_ptr(), _DTYPE[dtype], 0, step, self.head_dim)
+            b = wb.wb_heads(v.data_ptr(), _DTYPE[dtype], 0, step, self.head_dim)
+        else:
+            k, v = out
+            a = _heads(k, "out[0]", *shape, self.device)
+            b = _heads(v, "out[1]", *shape, self.device)
         self._kv.read(batch._for(self), a, b, _stream(self._index))
         return k, v
 
@@ -134,13 +145,15 @@ class KvCache:
         n, h = batch.n_tokens, q.shape[1]
         a = _heads(q, "q", n, h, self.head_dim, self.device)
         if out is None:
-            out = torch.empty((n, h, self.head_dim), dtype=torch.bfloat16, device=self.device)
+            out = self._like[torch.bfloat16].new_empty((n, h, self.head_dim))
+            b = wb.wb_heads(out.data_ptr(), wb.WB_BF16, 0, h * self.head_dim, self.head_dim)
+        else:
+            b = _heads(out, "out", n, h, self.head_dim, self.device)
         if lse is None:
-            lse = torch.empty((n, h), dtype=torch.float32, device=self.device)
+            lse = self._like[torch.float32].new_empty((n, h))
         elif lse.shape != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != self.device:
             raise ValueError("lse: contiguous fp32 [n_tokens, n_heads]")
-        b = _heads(out, "out", n, h, self.head_dim, self.device)
-        self._kv.attend(batch._for(self), a, h, b, lse.data_ptr(), self.head_dim ** -0.5 if scale is None else scale, window,
+        self._kv.attend(batch._for(self), a, h, b, lse.data_ptr(), self._scale if scale is None else scale, window,
                         workspace.pointer, workspace.bytes, _stream(self._index))
         return out, lse
 
@@ -178,8 +191,8 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
         raise ValueError("draft_tokens, draft_start: contiguous")
     _ints(draft_tokens, "draft_tokens", dev)
     _ints(draft_start, "draft_start", dev)
-    accepted = torch.empty(n, dtype=torch.int32, device=dev)
-    tokens = torch.empty((n, max_drafts + 1), dtype=torch.int32, device=dev)
+    accepted = draft_start.new_empty(n)
+    tokens = draft_start.new_empty((n, max_drafts + 1))
     none = draft is None or total == 0
     wb.wb_verify_drafts(wb.wb_verify_args(n, vocab, max_drafts, _DTYPE[target.dtype], total, 0, target.data_ptr(),
                                           None if none else draft.data_ptr(), max(target.stride(0), vocab),
