@@ -477,24 +477,18 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               unpack2(mul2(pack2(x[c + 2], x[c + 3]), f.y), x[c + 2], x[c + 3]);
             }
           }
-          // masks, in groups of columns that some row of the warp does not see
-          if (pos0 + (int32_t)kKeys - 1 > warp_hi) {
-            const int32_t h1 = x0.hi - pos0, w1 = warp_hi - pos0;
+          // masks: a bit per column for both ends at once, in groups of columns that some row of the warp does not see whole
+          // (a comparison and a selection per column and end took 1.1 us of the step)
+          if (pos0 + (int32_t)kKeys - 1 > warp_hi || pos0 < warp_lo) {
+            const int32_t h1 = x0.hi - pos0 + 1, l1 = x0.lo - pos0;
 #pragma unroll
-            for (int c = 0; c < 128; c += 16)
-              if (c + 15 > w1) {
+            for (int c = 0; c < 128; c += 32) {
+              if (pos0 + c + 31 <= warp_hi && pos0 + c >= warp_lo) continue;
+              const int32_t up = min(max(h1 - c, 0), 32), low = min(max(l1 - c, 0), 32);
+              const uint32_t bits = (uint32_t)((1ull << up) - 1) & ~(uint32_t)((1ull << low) - 1);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[c + e] = c + e > h1 ? -INFINITY : x[c + e];
-              }
-          }
-          if (pos0 < warp_lo) {
-            const int32_t l1 = x0.lo - pos0, w1 = warp_lo - pos0;
-#pragma unroll
-            for (int c = 0; c < 128; c += 16)
-              if (c < w1) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[c + e] = c + e < l1 ? -INFINITY : x[c + e];
-              }
+              for (int e = 0; e < 32; ++e) x[c + e] = bits & 1u << e ? x[c + e] : -INFINITY;
+            }
           }
           float m4[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
