@@ -283,26 +283,37 @@ __device__ __forceinline__ RowOf row_of(const AttendArgs& a, const Walk& w, uint
   return x;
 }
 
-// The row's query into shared memory, swizzled as the products read it.
+// The queries of a warp's 32 rows into shared memory, swizzled as the products read them; lane i knows row i.  Eight lanes copy 128
+// bytes of a row together (a thread copying its own row would touch a line per thread and load).
 template <int D>
-__device__ __forceinline__ void load_query(const AttendArgs& a, char* tile, uint32_t row, const RowOf& x) {
-  const uint4* src = reinterpret_cast<const uint4*>(a.q + (uint64_t)x.tok * a.q_token + x.head * a.q_head);
+__device__ __forceinline__ void copy_queries(const AttendArgs& a, uint32_t tile, uint32_t row0, const RowOf& x) {
+  const uint32_t lane = threadIdx.x & 31, c = lane & 7;
+  const uint64_t mine = (uint64_t)(a.q + (uint64_t)x.tok * a.q_token + x.head * a.q_head);
 #pragma unroll
-  for (uint32_t c = 0; c < D / 8; ++c) {
-    const uint4 y = x.in ? __ldg(src + c) : make_uint4(0, 0, 0, 0);
-    *reinterpret_cast<uint4*>(tile + (c >> 3) * (kKeys * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) = y;
+  for (uint32_t i = 0; i < 8; ++i) {
+    const uint32_t from = i * 4 + (lane >> 3), row = row0 + from;
+    const uint64_t src = __shfl_sync(0xFFFFFFFFu, mine, from);
+    const uint32_t bytes = __shfl_sync(0xFFFFFFFFu, (uint32_t)x.in, from) ? 16 : 0;      // a row that is none: zeros
+#pragma unroll
+    for (uint32_t sp = 0; sp < D / 64; ++sp)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tile + sp * (kKeys * 128) + row * 128 + ((c ^ (row & 7)) << 4)),
+                   "l"(src + sp * 128 + c * 16), "r"(bytes) : "memory");
   }
+}
+__device__ __forceinline__ void queries_arrived() {
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  fence_async();
 }
 
 // One cache row of a value tile: cleared if it lies past the end; else its values that are not finite are taken out, and the
-// flag is raised first, so that whoever finds them gone finds the flag.
+// flag is raised first, so that whoever finds them gone finds the flag.  True if anything was written.
 template <int D>
-__device__ __forceinline__ void clear_values(char* tile, uint32_t row, bool past, volatile uint32_t* flag) {
+__device__ __forceinline__ bool clear_values(char* tile, uint32_t row, bool past, volatile uint32_t* flag) {
   char* v = tile + row * 128;
   if (past) {
 #pragma unroll
     for (uint32_t c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(v + (c >> 3) * (kKeys * 128) + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
-    return;
+    return true;
   }
   bool odd = false;
 #pragma unroll
@@ -313,7 +324,7 @@ __device__ __forceinline__ void clear_values(char* tile, uint32_t row, bool past
                           ((y.w & 0x7FFF7FFFu) + 0x00800080u)) & 0x80008000u;
     odd |= any != 0;
   }
-  if (!odd) return;
+  if (!odd) return false;
   *flag = 1;
   __threadfence_block();
   for (uint32_t c = 0; c < D / 2; ++c) {
@@ -323,6 +334,7 @@ __device__ __forceinline__ void clear_values(char* tile, uint32_t row, bool past
     if ((y & 0x7F800000u) == 0x7F800000u) y &= 0xFFFFu;
     *at = y;
   }
+  return true;
 }
 
 
@@ -424,8 +436,9 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       bool ok = true;
       Walk w = walk_to(a, cum, skip_rows, begin);
       RowOf x0 = row_of(a, w, i * 128 + row);
-      load_query<D>(a, smem + i * C::kSlotBytes, row, x0);
-      fence_async();
+      const uint32_t q_tile = base + i * C::kSlotBytes, warp_row = (warp & 3) * 32;
+      copy_queries<D>(a, q_tile, warp_row, x0);
+      queries_arrived();
       bar_arrive(q_full);
       for (int32_t t = begin; t < end; ++item) {
         const int32_t item1 = w.item0 + w.blk.n, stop = min(end, item1), from = t;
@@ -438,6 +451,14 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         const int32_t warp_hi = __shfl_sync(0xFFFFFFFFu, x0.hi, 0), warp_lo = a.window ? __shfl_sync(0xFFFFFFFFu, x0.lo, 31) : 0;
         const bool takes_part = i == 0 || n_rows > w.rb * kQRows + 128;
         if (tid == 0) misc[8 + (item + 5) % 8] = 0;     // that of three items ago; nobody is five items ahead
+        Walk w2 = w;                                // the next item, once this one's last scores are there
+        RowOf x2 = x0;
+        // the scores of this item are done with: the next one's queries take their place while its last weights are computed
+        auto prepare_next = [&]() {
+          walk_on(w2, a, cum, skip_rows);
+          x2 = row_of(a, w2, i * 128 + row);
+          copy_queries<D>(a, q_tile, warp_row, x2);
+        };
         float mref = -INFINITY;                     // the maximum that the weights are relative to, times c2
         uint64_t sum2[2] = {0, 0};
         for (bool first = true; t < stop; ++t, ++jg, first = false) {
@@ -457,8 +478,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             // values past the end, and values that are not finite, must not meet weights of zero
             const uint32_t vq = 2 * jg + 1, slot = vq % C::kSlots;
             ok = wait_or_give_up(full + 8 * slot, (vq / C::kSlots) & 1, ok, a.error);
-            clear_values<D>(smem + C::kOffSlots + slot * C::kSlotBytes, row, pos0 + (int32_t)row >= w.seq.len, misc + 8 + item % 8);
-            fence_async();
+            if (clear_values<D>(smem + C::kOffSlots + slot * C::kSlotBytes, row, pos0 + (int32_t)row >= w.seq.len, misc + 8 + item % 8)) fence_async();
           }
           float x[128];
           ok = wait_or_give_up(s_full + 8 * i, js & 1, ok, a.error);
@@ -466,6 +486,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           tc_after();
 #pragma unroll
           for (int c = 0; c < 128; c += 32) tm_load32(tm_s + c, reinterpret_cast<uint32_t*>(x) + c);
+          if (t + 1 == stop && stop < end) prepare_next();
           tm_wait_load();
           if (Q) {
             ok = wait_or_give_up(scale_ready + 8 * sk, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
@@ -560,14 +581,9 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             bar_arrive(scale_empty + 8 * sv);
           }
         }
-        // the scores of this item are done with: the next one's queries take their place while its last product runs
-        Walk w2 = w;
-        RowOf x2 = x0;
         if (t < end) {
-          walk_on(w2, a, cum, skip_rows);
-          x2 = row_of(a, w2, i * 128 + row);
-          load_query<D>(a, smem + i * C::kSlotBytes, row, x2);
-          fence_async();
+          if (!takes_part) prepare_next();
+          queries_arrived();
           bar_arrive(q_full);
         }
         // ---- outputs ---------------------------------------------------------------------------------
