@@ -669,11 +669,14 @@ wb_status wb_kv_read(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* 
  * slots and unused parts of pages hold does not matter (NaN included).  q and out are bf16;
  * n_heads is a multiple of n_kv_heads, n_heads / n_kv_heads at most 64, and scale is positive and finite.
  * workspace: wb_kv_attend_workspace_bytes device bytes, 256-byte aligned, zeroed once by the caller
- * before its first use; it carries nothing from call to call, and calls that may overlap need one each. */
+ * before its first use; it carries no results from call to call, and calls that may overlap need one each. */
 wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* q, uint32_t n_heads,
                        const wb_heads* out, float* lse, float scale, uint32_t window, void* workspace,
                        size_t workspace_bytes, void* cuda_stream);
 size_t wb_kv_attend_workspace_bytes(const wb_kv* kv, uint32_t n_heads, uint32_t n_seqs);
+/* Waits for the stream and reports whether a kernel that used the workspace gave up waiting inside (every wait is
+ * bounded, so that a lost signal cannot hang the GPU): WB_ERR_CUDA, and its results are not to be used. */
+wb_status wb_kv_attend_check(const void* workspace, void* cuda_stream);
 
 /* Verification of drafted tokens.  Sequence b drafted K = draft_start[b+1] - draft_start[b] tokens
  * x_0 .. x_{K-1} (K may be 0; at most max_drafts count), which are entries draft_start[b] + i of draft_tokens.

@@ -112,7 +112,7 @@ EXPORTS = [
     "wb_plan_num_ckpts", "wb_plan_ckpt_ids", "wb_plan_qbucket_bytes", "wb_absmax", "wb_bucket_quantize",
     "wb_bucket_dequantize", "wb_transfer_rounds_fp8", "wb_pack_fp8", "wb_unpack_fp8", "wb_transfer_rounds_fp8_fused",
     "wb_diff2_nonzeros", "wb_diff2_nonzeros_batch", "wb_diff2_batch_scratch_bytes", "wb_diff2_recombine", "wb_diff2_chunk_pass", "wb_diff2_chunk_scratch_bytes", "wb_scan_slices", "wb_route_account", "wb_wait_probe", "wb_plan_check_replicas", "wb_launches_per_call", "wb_status_str", "wb_version",
-    "wb_kv_open", "wb_kv_free", "wb_kv_write", "wb_kv_read", "wb_kv_attend", "wb_kv_attend_workspace_bytes", "wb_verify_drafts",
+    "wb_kv_open", "wb_kv_free", "wb_kv_write", "wb_kv_read", "wb_kv_attend", "wb_kv_attend_workspace_bytes", "wb_kv_attend_check", "wb_verify_drafts",
 ]
 
 _lib: Optional[C.CDLL] = None
@@ -187,6 +187,7 @@ def load() -> C.CDLL:
     lib.wb_kv_attend.argtypes = [vp, vp, vp, C.c_uint32, vp, vp, C.c_float, C.c_uint32, vp, sz, vp]
     lib.wb_kv_attend_workspace_bytes.argtypes = [vp, C.c_uint32, C.c_uint32]
     lib.wb_kv_attend_workspace_bytes.restype = sz
+    lib.wb_kv_attend_check.argtypes = [vp, vp]
     lib.wb_verify_drafts.argtypes = [vp, vp]
     lib.wb_launches_per_call.restype = C.c_int
     lib.wb_status_str.argtypes = [C.c_int]
@@ -571,6 +572,11 @@ class Kv:
                workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
         _check(_lib.wb_kv_attend(self.handle, C.byref(batch), C.byref(q), n_heads, C.byref(out), lse_ptr, scale, window,
                                  workspace_ptr, workspace_bytes, stream), "wb_kv_attend")
+
+
+def wb_kv_attend_check(workspace_ptr: int, stream: int = 0) -> None:
+    load()
+    _check(_lib.wb_kv_attend_check(workspace_ptr, stream), "wb_kv_attend_check")
 
 
 def wb_verify_drafts(args: wb_verify_args, stream: int = 0) -> None:

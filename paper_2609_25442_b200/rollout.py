@@ -167,6 +167,10 @@ class AttendWorkspace:
         self.buffer = torch.zeros(self.bytes, dtype=torch.uint8, device=cache.device)
         self.pointer = self.buffer.data_ptr()
 
+    def check(self) -> None:
+        """Waits for the current stream; raises if a kernel that used this workspace gave up waiting inside."""
+        wb.wb_kv_attend_check(self.pointer, _stream(self.buffer.device.index))
+
 
 def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tokens: torch.Tensor, draft_start: torch.Tensor,
                   uniform: torch.Tensor, race: torch.Tensor, *, max_drafts: int):

@@ -106,7 +106,9 @@ class Case:
 
 def attend(case, q, window=0, **kw):
     ws = rollout.AttendWorkspace(case.cache, case.heads, len(case.lens))
-    return case.cache.attend(case.batch, q, workspace=ws, window=window, **kw)
+    result = case.cache.attend(case.batch, q, workspace=ws, window=window, **kw)
+    ws.check()
+    return result
 
 
 # ---- write and read ------------------------------------------------------------------------------

@@ -140,6 +140,15 @@ def test_verify_refuses(kw, name):
     assert e.value.name == name
 
 
+@pytest.mark.parametrize("ws", [None, A + 8])
+def test_attend_check_refuses(ws):
+    assert wb.STATUS_NAMES[wb.load().wb_kv_attend_check(ws, None)] == "WB_ERR_INVALID_ARG"
+
+
+def test_workspace_of_nothing():
+    assert wb.load().wb_kv_attend_workspace_bytes(None, 4, 1) == 0
+
+
 def test_verify_refuses_null():
     assert wb.STATUS_NAMES[wb.load().wb_verify_drafts(None, None)] == "WB_ERR_INVALID_ARG"
 
