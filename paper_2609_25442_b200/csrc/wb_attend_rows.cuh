@@ -348,16 +348,16 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     auto sees_to = [&](uint32_t r) { return r < n_rows ? first_hi + (int32_t)(r * group_inv >> 16) : 0x7FFFFFFF; };
 
     float acc[NT][D / 16][4];
-    // what the weights are relative to (log2, negated), the score above which it moves, sums; 2^-(f16 exponent), the weight
-    // above which it moves
-    float refn[NT][2], thr[NT][2], sum[NT][2], ei[NT][2], lim[NT][2];
+    // the score that the weights are relative to, the score above which it moves, sums; 2^-(f16 exponent), the weight
+    // above which it moves.  (Differences are formed before they are scaled: scores of any finite size give weights of 1 and less.)
+    float ref[NT][2], thr[NT][2], sum[NT][2], ei[NT][2], lim[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) acc[n][i][0] = acc[n][i][1] = acc[n][i][2] = acc[n][i][3] = 0.f;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        refn[n][e] = 0.f;
+        ref[n][e] = 0.f;
         thr[n][e] = -INFINITY;
         sum[n][e] = ei[n][e] = lim[n][e] = 0.f;
       }
@@ -440,9 +440,8 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
             m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 8));
             m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, 16));
             if (m > thr[n][e]) {
-              const float next = -m * c2q[n][e];
-              const float corr = thr[n][e] == -INFINITY ? 0.f : fast_exp2(next - refn[n][e]);
-              refn[n][e] = next;
+              const float corr = thr[n][e] == -INFINITY ? 0.f : fast_exp2((ref[n][e] - m) * c2q[n][e]);
+              ref[n][e] = m;
               thr[n][e] = fmaxf(m + __fdividef(8.f, c2q[n][e]), -3.0e38f);       // finite: -inf means that nothing was seen yet
               sum[n][e] *= corr;
 #pragma unroll
@@ -455,7 +454,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          sc[n][e] = fast_exp2(fmaf(sc[n][e], c2q[n][e & 1], refn[n][e & 1]));
+          sc[n][e] = fast_exp2((sc[n][e] - ref[n][e & 1]) * c2q[n][e & 1]);
           sum[n][e & 1] += sc[n][e];
         }
         if (Q) {
@@ -590,7 +589,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         sum[n][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[n][e], 4);
         sum[n][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[n][e], 8);
         sum[n][e] += __shfl_xor_sync(0xFFFFFFFFu, sum[n][e], 16);
-        if (r8 == 0) warp_ml[warp * C::kRows + n * 8 + 2 * t4 + e] = make_float2(thr[n][e] == -INFINITY ? -INFINITY : -refn[n][e], sum[n][e]);
+        if (r8 == 0) warp_ml[warp * C::kRows + n * 8 + 2 * t4 + e] = make_float2(thr[n][e] == -INFINITY ? -INFINITY : __fmul_rn(ref[n][e], c2q[n][e]), sum[n][e]);
       }
     __syncthreads();
     float mine[NT][2];
@@ -601,7 +600,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         float m = -INFINITY;
 #pragma unroll
         for (int w = 0; w < 4; ++w) m = fmaxf(m, warp_ml[w * C::kRows + n * 8 + 2 * t4 + e].x);
-        mine[n][e] = thr[n][e] == -INFINITY ? 1.f : fast_exp2(-refn[n][e] - m);      // (nothing seen: zeros, or NaN)
+        mine[n][e] = thr[n][e] == -INFINITY ? 1.f : fast_exp2(__fmul_rn(ref[n][e], c2q[n][e]) - m);      // (nothing seen: zeros, or NaN; the product is rounded, as m was)
         if (Q && ei[n][e] != 0.f) mine[n][e] *= lim[n][e] * (1.f / 256.f);
       }
 #pragma unroll

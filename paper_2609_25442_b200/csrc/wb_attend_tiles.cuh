@@ -459,7 +459,9 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           x2 = row_of(a, w2, i * 128 + row);
           copy_queries<D>(a, q_tile, warp_row, x2);
         };
-        float mref = -INFINITY;                     // the maximum that the weights are relative to, times c2
+        // the score that the weights are relative to (differences are formed before they are scaled: scores of any finite size
+        // give weights of 2^8 and less), and that above which it moves
+        float ref = 0.f, limit = -INFINITY;
         uint64_t sum2[2] = {0, 0};
         for (bool first = true; t < stop; ++t, ++jg, first = false) {
           const uint32_t sk = (2 * jg) % C::kScaleSlots, sv = sk + 1;
@@ -518,14 +520,15 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             for (int e = 0; e < 4; ++e) m4[e] = max3(m4[e], x[c + 2 * e], x[c + 2 * e + 1]);
           m4[0] = max3(m4[0], x[124], x[125]);
           m4[1] = max3(m4[1], x[126], x[127]);
-          const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * c2;
-          const bool grow = m > mref + 8.f;
+          const float m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+          const bool grow = m > limit;
           // the step's commit covered the previous product, so nothing writes the outputs now
           if (__any_sync(0xFFFFFFFFu, grow)) {
             float corr = 1.f;
             if (grow) {
-              corr = mref == -INFINITY ? 0.f : fast_exp2(mref - m);
-              mref = m;
+              corr = limit == -INFINITY ? 0.f : fast_exp2((ref - m) * c2);
+              ref = m;
+              limit = fmaxf(m + __fdividef(8.f, c2), -3.0e38f);      // finite: -inf means that nothing was seen yet
             }
             const uint64_t corr2 = pack2(corr, corr);
             sum2[0] = mul2(sum2[0], corr2);
@@ -543,7 +546,6 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             }
           }
           if (Q) ok = wait_or_give_up(scale_ready + 8 * sv, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
-          const float ref = mref == -INFINITY ? 0.f : mref;
           const uint64_t c22 = pack2(c2, c2), ref2 = pack2(-ref, -ref);
           const uint32_t vscales = base + C::kOffScale + sv * (kKeys * 4);
 #pragma unroll
@@ -557,7 +559,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
                 float u, v;
-                unpack2(fma2(pack2(x[c + 2 * k], x[c + 2 * k + 1]), c22, ref2), u, v);
+                unpack2(mul2(add2(pack2(x[c + 2 * k], x[c + 2 * k + 1]), ref2), c22), u, v);
                 const uint64_t y = pack2(fast_exp2(u), fast_exp2(v));
                 sum2[k] = add2(sum2[k], y);
                 unpack2(Q ? mul2(y, k ? f.y : f.x) : y, u, v);
@@ -629,9 +631,9 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           }
           if (cuts.n == 0) {
             if (x0.in && a.lse)
-              a.lse[(uint64_t)x0.tok * a.n_heads + x0.head] = l == 0.f ? -INFINITY : (mref + log2f(l)) * kLn2;
+              a.lse[(uint64_t)x0.tok * a.n_heads + x0.head] = l == 0.f ? -INFINITY : (ref * c2 + log2f(l)) * kLn2;
           } else {
-            part[D * 128] = l == 0.f ? -INFINITY : mref;
+            part[D * 128] = l == 0.f ? -INFINITY : ref * c2;
             part[D * 128 + 128] = l;
             if (tid == 0 && w.item0 >= begin) *cut_item = CutItem{(uint32_t)cuts.n + 1, w.s, w.h, w.rb};
           }

@@ -445,3 +445,116 @@ def test_verify_corner_distributions():
         wa, wt = orc.verify(p[2 * b:2 * b + 2], q[b:b + 1], tokens[b:b + 1], uniform[b:b + 1], race[b], 1)
         assert a[b] == wa and np.array_equal(out[b], wt), (b, out[b], wt)
     assert out[0][0] == 0 and list(out[1]) == [77, 500] and out[2][0] == 11 and out[3][0] == 0
+
+
+@pytest.mark.parametrize("n,ks,vocab", [(19, 2, 300), (40, 1, 4100), (150, 3, 129), (700, 1, 65)])
+def test_verify_many_sequences(n, ks, vocab):
+    """Batches at which a sequence gets 8, 4 and 2 blocks, and one."""
+    rng = np.random.default_rng(n)
+    counts = rng.integers(0, ks + 1, n)
+    starts, total = np.concatenate([[0], np.cumsum(counts)]), int(counts.sum())
+    p = rng.dirichlet(np.ones(vocab), total + n).astype(np.float32)
+    q = rng.dirichlet(np.ones(vocab), total).astype(np.float32)
+    tokens, uniform = rng.integers(0, vocab, total), rng.random(total).astype(np.float32)
+    race = rng.exponential(size=(n, vocab)).astype(np.float32)
+    a, out = run_verify(torch.tensor(p, device=DEV), torch.tensor(q, device=DEV), tokens, starts, uniform, torch.tensor(race, device=DEV), ks)
+    for b in range(n):
+        s, e = starts[b], starts[b + 1]
+        wa, wt = orc.verify(p[s + b:e + b + 1], q[s:e], tokens[s:e], uniform[s:e], race[b], ks)
+        assert a[b] == wa and np.array_equal(out[b], wt), b
+
+
+# ---- large batches ---------------------------------------------------------------------------------
+def mixed_batch(n, most_new, seed):
+    rng = np.random.default_rng(seed)
+    lens = [int(x) for x in rng.integers(0, 40, n)]
+    new = [min(int(rng.integers(0, most_new + 1)), x) if i % 7 else 0 for i, x in enumerate(lens)]
+    lens[:60] = [0] * 60                           # a run of empty sequences, longer than any group the kernels look at
+    new[:60] = [0] * 60
+    return lens, new
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("n,most_new,heads", [(1100, 1, 4), (4096, 1, 2), (300, 4, 16)])
+def test_many_sequences(dtype, n, most_new, heads):
+    lens, new = mixed_batch(n, most_new, n)
+    c = Case(lens, new, heads, 2, 64, 16, dtype, seed=n)
+    k, v = c.rows()
+    c.cache.write(c.whole, k, v)
+    rk, _ = c.cache.read(c.whole, dtype=torch.float32)
+    grid = k.float().abs().amax(-1, keepdim=True) * (2.0 ** -4 if dtype == E4M3 else 0.0)
+    assert bool(((rk - k.float()).abs() <= grid).all())
+    q = c.queries()
+    out, lse = attend(c, q)
+    c.check_attend(q, out, lse)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+def test_many_prompts(dtype):
+    """More sequences than one launch of the kernel for long chunks takes, among ones that the other kernel takes."""
+    lens, new = mixed_batch(620, 12, 3)
+    c = Case(lens, new, 10, 2, 64, 16, dtype, seed=7)
+    k, v = c.rows()
+    c.cache.write(c.whole, k, v)
+    q = c.queries()
+    out, lse = attend(c, q)
+    c.check_attend(q, out, lse)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("group,new", [(8, 1), (9, 1), (16, 1), (17, 1), (32, 1), (33, 1), (64, 1), (1, 8), (1, 9), (1, 33), (2, 16), (2, 64), (2, 65), (4, 64), (1, 257)])
+def test_row_counts(dtype, group, new):
+    """Rows at the borders between the kernels and between their tiles."""
+    c = Case([300, 70], [new, min(new, 70)], group, 1, 128, 32, dtype, seed=group * 1000 + new)
+    k, v = c.rows()
+    c.cache.write(c.whole, k, v)
+    q = c.queries()
+    out, lse = attend(c, q)
+    c.check_attend(q, out, lse)
+
+
+def test_queries_of_very_different_size():
+    """E4M3 caches: a row's products do not depend on its neighbours' magnitudes, nor on subnormal or zero queries."""
+    c = Case([200, 150], [1, 60], 8, 2, 128, 16, E4M3, seed=12)
+    k, v = c.rows()
+    c.cache.write(c.whole, k, v)
+    q = c.queries()
+    size = torch.tensor([1.0, 2.0 ** 60, 2.0 ** -60, 0.0, 2.0 ** -130, 3.0, 2.0 ** -20, 100.0], device=DEV)
+    q = (q.float() * size[None, :, None]).to(torch.bfloat16)
+    out, lse = attend(c, q, scale=2.0 ** -10)
+    for h in range(8):
+        one = q.clone()
+        one[:, [x for x in range(8) if x != h]] = 0
+        got, l = attend(c, one, scale=2.0 ** -10)
+        assert torch.equal(got[:, h], out[:, h]) and torch.equal(l[:, h], lse[:, h])
+    small = [0, 2, 3, 4, 5, 6, 7]
+    t = 0
+    for s, (kk, vv) in enumerate(c.values_of()):
+        n = c.new[s]
+        want, wl, mag = orc.attend(q[t:t + n].float().cpu().numpy(), kk, vv, n, 2.0 ** -10)
+        assert (np.abs(out[t:t + n].float().cpu().numpy() - want) <= out_bound(want, mag))[:, small].all()
+        assert (np.abs(lse[t:t + n].cpu().numpy() - wl)[:, small] <= 1e-4).all()
+        t += n
+
+
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_row_scales_of_very_different_size(new):
+    """E4M3 caches: neighbouring rows whose value scales differ by up to 2^30, in either order."""
+    c = Case([400], [new], 4, 2, 64, 16, E4M3, seed=13)
+    k, v = c.rows()
+    size = 2.0 ** torch.tensor(np.random.default_rng(3).integers(-15, 16, 400), dtype=torch.float32, device=DEV)
+    v = v.float() * size[:, None, None]
+    c.cache.write(c.whole, k.float(), v)
+    q = c.queries()
+    out, lse = attend(c, q)
+    (kk, vv), = c.values_of()
+    want, wl, mag = orc.attend(q.float().cpu().numpy(), kk, vv, new, 64 ** -0.5)
+    # the ordinary bound, and the weights' own range: a term below 2^-14 of the row's largest one is off by up to 2^-25 of that
+    # (times the largest value of a code), 400 terms in all
+    top = np.abs(vv).max() * 400 * 2.0 ** -24
+    assert (np.abs(out.float().cpu().numpy() - want) <= out_bound(want, mag) + top).all()
+
+
+# ---- the host's refusals, where there is a driver to open a cache with -------------------------------------------
+from test_rollout_host import (kv, test_attend_refuses, test_calls_refuse_batches, test_calls_refuse_tensors,  # noqa: E402,F401
+                               test_rows_of_two_types_are_refused)
