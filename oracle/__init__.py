@@ -23,6 +23,10 @@ Pins (see tests marked "not gpu"):
                           in exact rationals, torch's CPU float8_e4m3fn table and cast inside the
                           finite range, brute-force nearest-even over all codes incl. every
                           midpoint, saturation and NaN table, scale rule and round-trip bound.
+  rollout.attend / verify / quantize_row
+                          (the rollout step's operators; not in the paper) one key gives its value, windows
+                          equal cut keys, empty rows; emitted tokens follow the target's distribution; rows
+                          quantise as tensors do.
   The order of payloads inside a transfer bucket and the rule that picks which trainer
   replica supplies a replicated element are planner choices the paper does not fix:
   parity unpinned by the paper, checked only against the directory the library reports

@@ -1,4 +1,10 @@
-// Attention of a chunk of new tokens over the paged cache.
+// Attention of a chunk of new tokens over the paged cache: which kernel takes a sequence, and the launches.
+//
+// Two kernels share a batch by the sequences' rows (new tokens x query heads per kv head): up to 32 rows the cache's bytes are the
+// bound, and a kernel that streams them through the legacy matrix instructions does it at the copy's bandwidth (one token, 4 rows:
+// 178 us for 1.1 GB; the tile kernel, which fills 128 rows whatever there are, needs the tensor core's time for all of them, 0.6 us per
+// 64 cache rows and SM against 0.3 that the bytes take); beyond, the products are, and they need the tensor memory's kernel (64 tokens
+// of 4 heads over 16384 positions: 56 us).  Both are launched where a batch may hold both kinds; each leaves the other's alone.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -117,6 +123,9 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < wb_kv_attend_workspace_bytes(kv, n_heads, batch->n_seqs))
     return WB_ERR_INVALID_ARG;
   if (!batch->n_tokens || !batch->n_seqs) return WB_OK;
+  // the kernels count tiles in 31 bits
+  const uint64_t group = n_heads / kv->d.n_kv_heads, row_blocks = (uint64_t)batch->n_tokens * group / kQRows + batch->n_seqs;
+  if (row_blocks * (batch->max_len / kKvTile + 2) * kv->d.n_kv_heads > 0x7FFFFFFFull) return WB_ERR_INVALID_ARG;
   AttendArgs a;
   a.c = kv_view(kv);
   a.b = kv_batch(batch);
