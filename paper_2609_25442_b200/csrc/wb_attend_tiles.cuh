@@ -457,7 +457,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         // rows of a warp are in the order of their tokens: its first row sees the least far, its last row's window begins last
         const int32_t warp_hi = __shfl_sync(0xFFFFFFFFu, x0.hi, 0), warp_lo = a.window ? __shfl_sync(0xFFFFFFFFu, x0.lo, 31) : 0;
         const bool takes_part = i == 0 || n_rows > w.rb * kQRows + 128;
-        if (tid == 0) misc[8 + (item + 5) % 8] = 0;     // that of three items ago; nobody is five items ahead
+        if (tid == 0) misc[8 + (item + 5) % 8] = 0;     // that of three items ago: the other tile is at most one behind, nobody five ahead
         Walk w2 = w;                                // the next item, once this one's last scores are there
         RowOf x2 = x0;
         // the scores of this item are done with: the next one's queries take their place while its last weights are computed
@@ -593,6 +593,9 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         if (t < end) {
           if (!takes_part) prepare_next();
           queries_arrived();
+          // Neither tile's warps get an item ahead of the other's: a tile that takes no part in an item has nothing to wait for, and
+          // its arrivals for the items after would stand in for the other's.
+          asm volatile("bar.sync 1, 256;" ::: "memory");
           bar_arrive(q_full);
         }
         // ---- outputs ---------------------------------------------------------------------------------
@@ -711,8 +714,8 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           }
           if (t < t_end) walk_on(w, a, cum, skip_rows);
         }
-        // the last commit arrives before the block ends
-        (void)wait_or_give_up(empty + 8 * ((2 * jg - 1) % C::kSlots), ((2 * jg - 1) / C::kSlots) & 1, ok, a.error);
+        // the last commit arrives before the block ends (waited for even after a wait that gave up)
+        (void)wait_or_give_up(empty + 8 * ((2 * jg - 1) % C::kSlots), ((2 * jg - 1) / C::kSlots) & 1, true, a.error);
         __syncwarp();
       } else if (warp == 9) {
         // ---- cache tiles: one lane per page piece ------------------------------------------------------
@@ -756,6 +759,12 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           }
           if (t < end) walk_on(w, a, cum, skip_rows);
         }
+        // every load lands before the block ends, also where the others gave up waiting and left some unread
+        const uint32_t n = 2 * jg, ring = Q ? C::kRaws : C::kSlots;
+        for (uint32_t q = n > ring ? n - ring : 0; q < n; ++q) (void)wait_or_give_up((Q ? raw_full : full) + 8 * (q % ring), (q / ring) & 1, true, a.error);
+        if (Q)
+          for (uint32_t q = n > C::kScaleSlots ? n - C::kScaleSlots : 0; q < n; ++q)
+            (void)wait_or_give_up(scale_full + 8 * (q % C::kScaleSlots), (q / C::kScaleSlots) & 1, true, a.error);
       }
     } else if (Q) {
       // ---- codes -> bf16: one thread per cache row -------------------------------------------------------

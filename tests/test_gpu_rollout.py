@@ -502,6 +502,43 @@ def test_many_prompts(dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("dim,most", [(64, 300), (128, 700), (128, 100)])
+def test_blocks_of_one_tile(dtype, dim, most):
+    """Many items in a row of at most 128 query rows, of which a block of the kernel for long chunks uses one of its two tiles,
+    with larger ones in between."""
+    rng = np.random.default_rng(most)
+    n = 90
+    new = [int(x) for x in rng.integers(9, 33, n)]
+    new[::11] = [70] * len(new[::11])
+    lens = [max(a, int(x)) for a, x in zip(new, rng.integers(20, most, n))]
+    c = Case(lens, new, 32, 8, dim, 16, dtype, seed=most)
+    k, v = c.rows()
+    c.cache.write(c.whole, k, v)
+    q = c.queries()
+    first, lse = attend(c, q)
+    for _ in range(3):
+        again, l = attend(c, q)
+        assert torch.equal(first, again) and torch.equal(lse, l)
+    # the oracle over a few of the sequences; the others against fp32 torch on the values that the cache holds
+    t = 0
+    for s, (kk, vv) in enumerate(c.values_of()):
+        m = new[s]
+        if s % 15 == 0:
+            want, wl, mag = orc.attend(q[t:t + m].float().cpu().numpy(), kk, vv, m, dim ** -0.5)
+            want, mag, wl = torch.tensor(want, device=DEV), torch.tensor(mag, device=DEV), torch.tensor(wl, device=DEV)
+        else:
+            kt, vt = (torch.tensor(x, device=DEV).double().repeat_interleave(4, 0) for x in (kk, vv))
+            z = torch.einsum("thd,hld->thl", q[t:t + m].double(), kt) * dim ** -0.5
+            pos = torch.arange(lens[s], device=DEV)
+            z.masked_fill_(pos[None, None] > (torch.arange(m, device=DEV) + lens[s] - m)[:, None, None], -math.inf)
+            w = torch.softmax(z, -1)
+            want, mag, wl = torch.einsum("thl,hld->thd", w, vt), torch.einsum("thl,hld->thd", w, vt.abs()), torch.logsumexp(z, -1)
+        assert bool(((first[t:t + m].double() - want).abs() <= 2.0 ** -8 * (1 + 2.0 ** -6) * (want.abs() + mag) + 1e-6).all()), s
+        assert bool(((lse[t:t + m] - wl).abs() <= 1e-4).all()), s
+        t += m
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
 @pytest.mark.parametrize("group,new", [(8, 1), (9, 1), (16, 1), (17, 1), (32, 1), (33, 1), (64, 1), (1, 8), (1, 9), (1, 33), (2, 16), (2, 64), (2, 65), (4, 64), (1, 257)])
 def test_row_counts(dtype, group, new):
     """Rows at the borders between the kernels and between their tiles."""
