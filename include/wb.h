@@ -628,7 +628,8 @@ void wb_kv_free(wb_kv* kv);
  * bounds on a sequence's new tokens and on kv_len (they size the launch; a loose max_len only costs
  * blocks that end at once, results beyond a max_new that is too small are not computed).  A position
  * that the table does not cover, or whose page is not in [0, n_pages), is not written, reads as zeros
- * and is attended over as zeros: table entries past a sequence's last page may hold anything. */
+ * and is attended over as zeros: table entries past a sequence's last page may hold anything.  The arrays are
+ * read more than once: they must not change while a call that was given them runs. */
 typedef struct {
   uint32_t n_seqs;            /* at most WB_KV_MAX_SEQS                                            */
   uint32_t n_tokens;          /* rows of the step's tensors                                        */

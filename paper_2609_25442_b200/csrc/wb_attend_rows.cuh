@@ -246,7 +246,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     x.h = (t - cum[x.s]) / nt;
     x.i0 = cum[x.s] + x.h * nt;
     x.i1 = x.i0 + nt;
-    x.n_rows = (uint32_t)q.n_new * a.group;
+    x.n_rows = min((uint32_t)q.n_new * a.group, C::kRows);
     x.row0 = q.row0;
     x.len = q.len;
     x.n_new = q.n_new;

@@ -89,12 +89,12 @@ __device__ __forceinline__ void place_tokens(const KvView& c, const KvBatch& b, 
 
 // step tensor -> cache.  A thread has 32 elements of a row, as four pieces of 8 (D / 32 pieces apart, so that the threads of a row
 // read and write whole sectors): with so few threads to a row its maximum takes two exchanges at most, and the two exact divisions
-// of its scale are shared by 32 elements (16 threads to a row, 8 elements each: 42 us for 14.9 thousand
-// tokens of 8 heads of 128 where this takes 19.6, 4.3 TB/s).
+// of its scale are shared by 32 elements (16 threads to a row, 8 elements each: 42 us for 13.4 thousand
+// tokens of 8 heads of 128 where this takes 17.7, 4.7 TB/s).
 template <int D, bool F32, bool Q>
-__global__ void __launch_bounds__(kRowThreads)
+__global__ void __launch_bounds__(kRowThreads, F32 ? 4 : 6)
 wb_kv_write_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {
-  constexpr uint32_t LANES = D / 32, ROWS = kRowThreads / LANES;
+  constexpr uint32_t LANES = D / 32, ROWS = kRowThreads / LANES, N = F32 ? 2 : 1;      // N 16-byte loads for 8 elements
   __shared__ int2 place[kTokensPerBlock];
   const uint32_t t0 = blockIdx.x * per_block, n = min(per_block, b.n_tokens - t0);
   const uint32_t lane = threadIdx.x % LANES, per_token = 2 * c.n_kv_heads, total = n * per_token;
@@ -105,14 +105,13 @@ wb_kv_write_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {
     const bool is_v = w >= c.n_kv_heads;
     const uint32_t h = w - (is_v ? c.n_kv_heads : 0);
     const Rows& src = is_v ? v : k;
-    const char* from = src.data + (uint64_t)(t0 + tok) * src.token_stride + h * src.head_stride + lane * (F32 ? 32 : 16);
-    float x[4][8];
+    const char* from = src.data + (uint64_t)(t0 + tok) * src.token_stride + h * src.head_stride + lane * (16 * N);
+    uint4 raw[4][N];               // as loaded: the rows wait in half the registers that their values would take
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
+    for (uint32_t j = 0; j < 4; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[j][e] = 0.f;
-      if (in) load8<F32>(from + j * (LANES * (F32 ? 32 : 16)), x[j]);
-    }
+      for (uint32_t i = 0; i < N; ++i)
+        raw[j][i] = in ? __ldcs(reinterpret_cast<const uint4*>(from + j * (LANES * 16 * N)) + i) : make_uint4(0, 0, 0, 0);
     if (!placed) {                 // the rows are on their way meanwhile
       place_tokens(c, b, t0, n, place);
       placed = true;
@@ -124,15 +123,40 @@ wb_kv_write_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {
     if (!Q) {
       if (live)
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) store8<false>(base + (off + j * (LANES * 8)) * 2, x[j]);
+        for (uint32_t j = 0; j < 4; ++j) {
+          uint4 y = raw[j][0];
+          if (F32)
+            y = make_uint4(pack_bf16x2(__uint_as_float(raw[j][0].x), __uint_as_float(raw[j][0].y)), pack_bf16x2(__uint_as_float(raw[j][0].z), __uint_as_float(raw[j][0].w)),
+                           pack_bf16x2(__uint_as_float(raw[j][N - 1].x), __uint_as_float(raw[j][N - 1].y)), pack_bf16x2(__uint_as_float(raw[j][N - 1].z), __uint_as_float(raw[j][N - 1].w)));
+          __stcs(reinterpret_cast<uint4*>(base + (off + j * (LANES * 8)) * 2), y);
+        }
       continue;
     }
+    auto value = [&](uint32_t j, int e) {
+      if (F32) {
+        const uint4 q = raw[j][e / 4 % N];
+        return __uint_as_float(e % 4 == 0 ? q.x : e % 4 == 1 ? q.y : e % 4 == 2 ? q.z : q.w);
+      }
+      const uint4 q = raw[j][0];
+      const uint32_t word = e / 2 == 0 ? q.x : e / 2 == 1 ? q.y : e / 2 == 2 ? q.z : q.w;
+      return e & 1 ? bf16_hi(word) : bf16_lo(word);
+    };
     // magnitudes are compared as unsigned patterns, so that a NaN wins and makes the whole row NaN
     uint32_t m = 0;
+    if (F32) {
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j)
+      for (uint32_t j = 0; j < 4; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(x[j][e]) & 0x7FFFFFFFu);
+        for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(value(j, e)) & 0x7FFFFFFFu);
+    } else {
+      uint32_t m2 = 0;             // two at a time
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) {
+        m2 = __vmaxu2(m2, __vmaxu2(raw[j][0].x & 0x7FFF7FFFu, raw[j][0].y & 0x7FFF7FFFu));
+        m2 = __vmaxu2(m2, __vmaxu2(raw[j][0].z & 0x7FFF7FFFu, raw[j][0].w & 0x7FFF7FFFu));
+      }
+      m = max(m2 << 16, m2 & 0xFFFF0000u);
+    }
 #pragma unroll
     for (uint32_t d = LANES / 2; d; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
     const float amax = __uint_as_float(m);
@@ -142,29 +166,27 @@ wb_kv_write_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {
       if (scale == 0.f) scale = __uint_as_float(1u);
       inv = __fdiv_rn(448.f, amax);
     }
-    if (!isfinite(inv)) {   // 448 / amax overflows (or is NaN): divide instead
+    if (!live) continue;
+    const bool divide = !isfinite(inv);       // 448 / amax overflows (or is NaN): divide by the scale instead
 #pragma unroll
-      for (uint32_t j = 0; j < 4; ++j)
+    for (uint32_t j = 0; j < 4; ++j) {
+      uint32_t code[4];
+      if (divide) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[j][e] = __fdiv_rn(x[j][e], scale);
-      inv = 1.f;
-    }
-    if (live) {
+        for (int e = 0; e < 4; ++e) code[e] = pack_e4m3x2(__fdiv_rn(value(j, 2 * e), scale), __fdiv_rn(value(j, 2 * e + 1), scale));
+      } else {
 #pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) {
-        uint2 codes;
-        codes.x = pack_e4m3x2(x[j][0] * inv, x[j][1] * inv) | (uint32_t)pack_e4m3x2(x[j][2] * inv, x[j][3] * inv) << 16;
-        codes.y = pack_e4m3x2(x[j][4] * inv, x[j][5] * inv) | (uint32_t)pack_e4m3x2(x[j][6] * inv, x[j][7] * inv) << 16;
-        *reinterpret_cast<uint2*>(base + off + j * (LANES * 8)) = codes;
+        for (int e = 0; e < 4; ++e) code[e] = pack_e4m3x2(value(j, 2 * e) * inv, value(j, 2 * e + 1) * inv);
       }
-      if (lane == 0) (is_v ? c.v_scale : c.k_scale)[((uint64_t)(uint32_t)at.x * c.n_kv_heads + h) * c.page_size + at.y] = scale;
+      *reinterpret_cast<uint2*>(base + off + j * (LANES * 8)) = make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16);
     }
+    if (lane == 0) (is_v ? c.v_scale : c.k_scale)[((uint64_t)(uint32_t)at.x * c.n_kv_heads + h) * c.page_size + at.y] = scale;
   }
 }
 
 constexpr uint32_t kAhead = 4;      // rows whose loads a thread has in flight
 
-// cache -> step tensor.  100 thousand tokens of 8 heads of 128 from codes to bf16: 65 us, 5.3 TB/s.
+// cache -> step tensor.  56 thousand tokens of 8 heads of 128 from codes to bf16: 65 us, 5.3 TB/s.
 template <int D, bool F32, bool Q>
 __global__ void __launch_bounds__(kRowThreads)
 wb_kv_read_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {
