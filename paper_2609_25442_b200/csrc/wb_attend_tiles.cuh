@@ -17,8 +17,9 @@
 //   - One warp issues all products in the order  QK0 QK1 | PV0 QK0' PV1 QK1' | ..., one requests cache tiles into a
 //     ring of slots (keys, values, keys, ...) by tensor-map loads, a box per page piece and lane.
 //   - E4M3 caches: tiles arrive as codes, four more warps widen them to bf16 slots; the row scales multiply scores and
-//     weights in the softmax, where each is a value of its own.  The widening and the scales cost 700 us where bf16 takes 410:
-//     the ALU pipe serves the softmax and the widening both.
+//     weights in the softmax, where each is a value of its own.  This takes 680 us where bf16 takes 410 (tensor core 34 % busy,
+//     issue slots 43 %, ALU 31 %): the step's chain is a microsecond longer, by the scales' loads, products and barriers, and by the
+//     widening warps' share of the schedulers; 616 us with nothing widened, 530 without scales as well.
 //   - Work is cut as in the kernel for few rows: one line of 128-row tiles over all (sequence, kv head, row block)
 //     items, an equal share for every SM; a second kernel joins the cut items.
 #pragma once
@@ -39,10 +40,10 @@ struct TilesCfg {
   static constexpr uint32_t kSpanBytes = kKeys * 128;              // one span of 128 rows
   static constexpr uint32_t kSlotBytes = kSpans * kSpanBytes;      // a bf16 tile of keys or values
   static constexpr uint32_t kQBytes = 2 * kSlotBytes;
-  static constexpr uint32_t kSlots = Q ? (D == 128 ? 4 : 6) : (D == 128 ? 5 : 10);
+  static constexpr uint32_t kSlots = Q ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 10);
   static constexpr uint32_t kRawBytes = Q ? kKeys * D : 0;         // a tile of codes
-  static constexpr uint32_t kRaws = Q && D == 64 ? 4 : 2;
-  static constexpr uint32_t kScaleSlots = 4;                       // 128 scales each; keys and values in turn
+  static constexpr uint32_t kRaws = Q && D == 64 ? 8 : 4;
+  static constexpr uint32_t kScaleSlots = D == 64 ? 8 : 4;         // 128 scales each; keys and values in turn
   static constexpr uint32_t kRowSpan = D * (Q ? 1 : 2) < 128 ? D * (Q ? 1 : 2) : 128;   // bytes of a row in a box
   static constexpr uint32_t kRowSpans = D * (Q ? 1 : 2) / kRowSpan;
   // the quarter of a row's weights after which their product may start (3: all; measured best of 0, 1, 3)
