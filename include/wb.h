@@ -691,7 +691,7 @@ wb_status wb_kv_attend_check(const void* workspace, void* cuda_stream);
  * emitted tokens are distributed as the target's own.  draft = NULL means a drafter that proposes one
  * token with certainty (q one-hot at x_i).  accepted[b] = a; tokens[b][0 .. a] are the accepted tokens
  * and the drawn one, tokens[b][a + 1 ..] = -1.  Probabilities are fp32 or bf16, rows `*_stride` elements
- * apart; no alignment beyond the element's is needed. */
+ * apart (at least vocab, or 0: all rows are the same one); no alignment beyond the element's is needed. */
 typedef struct {
   uint32_t n_seqs, vocab, max_drafts;
   uint32_t dtype;               /* of target and draft: WB_F32 or WB_BF16                        */

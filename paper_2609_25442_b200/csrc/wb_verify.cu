@@ -211,7 +211,8 @@ extern "C" wb_status wb_verify_drafts(const wb_verify_args* args, void* stream) 
   if (!a.vocab || a.vocab > 0x7FFFFFFFu || a.max_drafts > (1u << 20) || a.n_seqs > (1u << 24) || a.n_drafts > (1u << 30) ||
       a.reserved)
     return WB_ERR_INVALID_ARG;
-  if (a.target_stride < a.vocab || a.race_stride < a.vocab || (a.draft && a.draft_stride < a.vocab)) return WB_ERR_INVALID_ARG;
+  auto bad_pitch = [&](uint64_t pitch) { return pitch && pitch < a.vocab; };       // 0: one row for all
+  if (bad_pitch(a.target_stride) || bad_pitch(a.race_stride) || (a.draft && bad_pitch(a.draft_stride))) return WB_ERR_INVALID_ARG;
   if (!a.n_seqs) return WB_OK;
   if (!a.target || !a.draft_start || !a.race || !a.accepted || !a.tokens) return WB_ERR_INVALID_ARG;
   if (a.n_drafts && (!a.draft_tokens || !a.uniform)) return WB_ERR_INVALID_ARG;

@@ -45,6 +45,16 @@ def _heads(t: torch.Tensor, name: str, n_tokens: int, heads: int, dim: int, devi
     return wb.wb_heads(t.data_ptr(), dtype, 0, st, sh)
 
 
+def _pitch(t: torch.Tensor, name: str) -> int:
+    """Elements from a row of a [rows, n] tensor to the next; 0 where all rows are one (a broadcast)."""
+    step, n = t.stride(0), t.shape[1]
+    if t.shape[0] <= 1:
+        return n                              # says nothing for a single row
+    if 0 < step < n:
+        raise ValueError(f"{name}: rows overlap")
+    return step
+
+
 class KvBatch:
     """One step's sequences: `page_table` [n_seqs, pages] (a position's page), `new_start` [n_seqs + 1] (the rows of a
     sequence's new tokens), `kv_len` [n_seqs] (tokens in the cache after the step), all int32 on the device.
@@ -178,7 +188,7 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
 
     target [n_drafts + n_seqs, vocab], draft [n_drafts, vocab] or None (a drafter that is certain), draft_tokens and
     uniform [n_drafts], draft_start [n_seqs + 1], race [n_seqs, vocab] (Exp(1) variates).  Returns (accepted [n_seqs],
-    tokens [n_seqs, max_drafts + 1], -1 beyond the drawn token), int32."""
+    tokens [n_seqs, max_drafts + 1], -1 beyond the drawn token), int32.  Rows may be one row broadcast with expand."""
     dev = target.device
     n, vocab, total = draft_start.shape[0] - 1, target.shape[1], draft_tokens.shape[0]
     if not target.is_cuda or target.dim() != 2 or n < 0 or target.shape[0] != total + n or target.stride(1) != 1:
@@ -199,8 +209,8 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
     tokens = draft_start.new_empty((n, max_drafts + 1))
     none = draft is None or total == 0
     wb.wb_verify_drafts(wb.wb_verify_args(n, vocab, max_drafts, _DTYPE[target.dtype], total, 0, target.data_ptr(),
-                                          None if none else draft.data_ptr(), max(target.stride(0), vocab),
-                                          0 if none else max(draft.stride(0), vocab), max(race.stride(0), vocab),
+                                          None if none else draft.data_ptr(), _pitch(target, "target"),
+                                          0 if none else _pitch(draft, "draft"), _pitch(race, "race"),
                                           draft_tokens.data_ptr(), draft_start.data_ptr(), uniform.data_ptr(), race.data_ptr(),
                                           accepted.data_ptr(), tokens.data_ptr()), _stream(dev.index))
     return accepted, tokens

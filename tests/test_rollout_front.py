@@ -1,0 +1,69 @@
+"""The torch front of the rollout step without a GPU: what reaches the C call, and what is refused before it.  Tensors lie in
+host memory and claim to be on a GPU; the C call is a recorder, so nothing reads them."""
+import pytest
+import torch
+
+from paper_2609_25442_b200 import rollout
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says it is on cuda:0."""
+    is_cuda = True
+    device = torch.device("cuda", 0)
+
+
+def gpu(t):
+    return t.as_subclass(OnGpu)
+
+
+@pytest.fixture
+def verified(monkeypatch):
+    """The arguments of every wb_verify_drafts call."""
+    calls = []
+    monkeypatch.setattr(rollout, "_stream", lambda index: 0)
+    monkeypatch.setattr(rollout.wb, "wb_verify_drafts", lambda args, stream=0: calls.append(args))
+    return calls
+
+
+def drafts_of(n=2, total=4, vocab=100, **kw):
+    d = dict(target=torch.rand(total + n, vocab), draft=torch.rand(total, vocab), draft_tokens=torch.zeros(total, dtype=torch.int32),
+             draft_start=torch.arange(n + 1, dtype=torch.int32) * (total // n), uniform=torch.rand(total), race=torch.rand(n, vocab))
+    d.update(kw)
+    return {k: v if v is None else gpu(v) for k, v in d.items()}
+
+
+def test_verify_passes_row_pitches_as_they_are(verified):
+    wide = torch.rand(6, 128)
+    rollout.verify_drafts(**drafts_of(target=wide[:, 5:105]), max_drafts=2)
+    assert (verified[0].target_stride, verified[0].draft_stride, verified[0].race_stride) == (128, 100, 100)
+
+
+@pytest.mark.parametrize("name,rows", [("target", 6), ("draft", 4), ("race", 2)])
+def test_verify_shares_one_row_of_a_broadcast_tensor(verified, name, rows):
+    """`row.expand(rows, vocab)` has one row in memory: the kernel must not be told of a pitch of `vocab`."""
+    rollout.verify_drafts(**drafts_of(**{name: torch.rand(1, 100).expand(rows, 100)}), max_drafts=2)
+    strides = {n: getattr(verified[0], n + "_stride") for n in ("target", "draft", "race")}
+    assert strides == {n: 0 if n == name else 100 for n in strides}
+
+
+@pytest.mark.parametrize("name,rows", [("target", 6), ("draft", 4), ("race", 2)])
+def test_verify_refuses_rows_that_overlap(verified, name, rows):
+    with pytest.raises(ValueError, match=name):
+        rollout.verify_drafts(**drafts_of(**{name: torch.rand(1000).as_strided((rows, 100), (60, 1))}), max_drafts=2)
+    assert not verified
+
+
+def test_verify_ignores_the_pitch_of_a_single_row(verified):
+    one = torch.rand(1, 100).as_strided((1, 100), (7, 1))
+    rollout.verify_drafts(**drafts_of(n=1, total=1, draft=one, race=one), max_drafts=2)
+    assert (verified[0].draft_stride, verified[0].race_stride) == (100, 100)
+
+
+def test_c_entry_takes_a_pitch_of_zero():
+    """0 stands for one row; anything else below the vocabulary stays refused."""
+    from test_rollout_host import verify_args
+    from paper_2609_25442_b200 import binding as wb
+    wb.wb_verify_drafts(verify_args(n_seqs=0, target_stride=0, draft_stride=0, race_stride=0))
+    for name in ("target_stride", "draft_stride", "race_stride"):
+        with pytest.raises(wb.WbError):
+            wb.wb_verify_drafts(verify_args(n_seqs=0, **{name: 1}))
