@@ -634,9 +634,9 @@ typedef struct {
   uint32_t n_seqs;            /* at most WB_KV_MAX_SEQS                                            */
   uint32_t n_tokens;          /* rows of the step's tensors                                        */
   uint32_t max_new, max_len;
-  uint32_t table_stride;      /* entries per row of page_table                                     */
-  uint32_t reserved;          /* must be 0                                                         */
-  const int32_t* page_table;  /* device, n_seqs x table_stride                                     */
+  uint32_t table_stride;      /* entries of a row of page_table                                    */
+  uint32_t table_pitch;       /* entries from a row to the next, at least table_stride; 0: table_stride */
+  const int32_t* page_table;  /* device, n_seqs rows                                               */
   const int32_t* new_start;   /* device, n_seqs + 1, non-decreasing, new_start[0] = 0              */
   const int32_t* kv_len;      /* device, n_seqs                                                    */
 } wb_kv_batch;

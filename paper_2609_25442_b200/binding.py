@@ -62,6 +62,9 @@ class wb_kv_batch(C.Structure):
                 ("page_table", C.c_void_p), ("new_start", C.c_void_p), ("kv_len", C.c_void_p)]
 
 
+wb_kv_batch.table_pitch = wb_kv_batch.reserved      # the header's name of the field
+
+
 class wb_heads(C.Structure):
     _fields_ = [("data", C.c_void_p), ("dtype", C.c_uint32), ("reserved", C.c_uint32),
                 ("token_stride", C.c_uint64), ("head_stride", C.c_uint64)]

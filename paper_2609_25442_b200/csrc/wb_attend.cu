@@ -88,7 +88,7 @@ cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_r
   for (uint32_t s0 = 0; s0 < all.b.n_seqs; s0 += C::kMaxSeqs) {
     AttendArgs a = all;
     a.b.n_seqs = std::min(C::kMaxSeqs, all.b.n_seqs - s0);
-    a.b.table += (uint64_t)s0 * a.b.table_stride;
+    a.b.table += (uint64_t)s0 * a.b.table_pitch;
     a.b.new_start += s0;
     a.b.kv_len += s0;
     kernel<<<kNumSMs, C::kThreads, C::kSmemBytes, stream>>>(a, kv->map_k, kv->map_v, skip_rows);

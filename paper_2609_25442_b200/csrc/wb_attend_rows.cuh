@@ -197,7 +197,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       x.slot = pos - entry * a.c.page_size;
       if (pos < (uint32_t)q.len && entry < a.b.table_stride) {
         x.h = h;
-        x.page = __ldg(a.b.table + (uint64_t)s * a.b.table_stride + entry);
+        x.page = __ldg(a.b.table + (uint64_t)s * a.b.table_pitch + entry);
       }
     }
     return x;

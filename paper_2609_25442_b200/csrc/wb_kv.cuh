@@ -41,16 +41,17 @@ struct KvBatch {
   const int32_t* table;
   const int32_t* new_start;
   const int32_t* kv_len;
-  uint32_t n_seqs, n_tokens, table_stride;
+  uint32_t n_seqs, n_tokens, table_stride, table_pitch;
   int32_t max_len;
 };
 
 inline KvBatch kv_batch(const wb_kv_batch* b) {
-  return KvBatch{b->page_table, b->new_start, b->kv_len, b->n_seqs, b->n_tokens, b->table_stride, (int32_t)b->max_len};
+  return KvBatch{b->page_table, b->new_start, b->kv_len, b->n_seqs, b->n_tokens, b->table_stride,
+                 b->table_pitch ? b->table_pitch : b->table_stride, (int32_t)b->max_len};
 }
 
 inline wb_status check_batch(const wb_kv* kv, const wb_kv_batch* b) {
-  if (!kv || !b || b->reserved || b->n_seqs > WB_KV_MAX_SEQS) return WB_ERR_INVALID_ARG;
+  if (!kv || !b || b->n_seqs > WB_KV_MAX_SEQS || (b->table_pitch && b->table_pitch < b->table_stride)) return WB_ERR_INVALID_ARG;
   if (b->n_tokens > 0x7FFFFFFFu || b->max_len > 0x7FFFFFFFu || b->max_new > b->n_tokens) return WB_ERR_INVALID_ARG;
   if (b->n_seqs && (!b->new_start || !b->kv_len || (b->table_stride && !b->page_table))) return WB_ERR_INVALID_ARG;
   // positions are 32-bit: a row of the table covers fewer than 2^31 of them
@@ -97,7 +98,7 @@ __device__ __forceinline__ int32_t kv_page(const KvBatch& b, uint32_t n_pages, u
   if (pos < 0) return -1;
   const uint32_t i = (uint32_t)pos / page_size;
   if (i >= b.table_stride) return -1;
-  const int32_t p = __ldg(b.table + (uint64_t)s * b.table_stride + i);
+  const int32_t p = __ldg(b.table + (uint64_t)s * b.table_pitch + i);
   return (uint32_t)p < n_pages ? p : -1;
 }
 

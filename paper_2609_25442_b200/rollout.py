@@ -58,7 +58,8 @@ def _pitch(t: torch.Tensor, name: str) -> int:
 class KvBatch:
     """One step's sequences: `page_table` [n_seqs, pages] (a position's page), `new_start` [n_seqs + 1] (the rows of a
     sequence's new tokens), `kv_len` [n_seqs] (tokens in the cache after the step), all int32 on the device.
-    `max_new` and `max_len` bound a sequence's new tokens and its length; they size the launches."""
+    `max_new` and `max_len` bound a sequence's new tokens and its length; they size the launches.  The three tensors are used in
+    place (a table may be a slice of a wider one), so a batch can be kept while they are updated."""
 
     def __init__(self, page_table: torch.Tensor, new_start: torch.Tensor, kv_len: torch.Tensor, *, n_tokens: int,
                  max_new: Optional[int] = None, max_len: Optional[int] = None):
@@ -70,16 +71,14 @@ class KvBatch:
         _require(new_start.shape == (self.n_seqs + 1,) and kv_len.dim() == 1 and new_start.is_contiguous() and kv_len.is_contiguous(),
                  "new_start: [n_seqs + 1], kv_len: [n_seqs], contiguous")
         _require(self.n_seqs <= 1 or page_table.shape[1] == 0 or page_table.stride(0) >= page_table.shape[1], "page_table: rows overlap")
-        # the C ABI knows one number for the pages of a row and the pitch of the table
-        if self.n_seqs > 1 and page_table.stride(0) != page_table.shape[1]:
-            page_table = page_table.contiguous()
         self.page_table = _ints(page_table, "page_table", dev)
         self.new_start, self.kv_len = _ints(new_start, "new_start", dev), _ints(kv_len, "kv_len", dev)
         self.device = dev
         most = int(page_table.shape[1]) if max_len is None else None
         self._max_len, self._table_pages = max_len, most
         self.args = wb.wb_kv_batch(self.n_seqs, self.n_tokens, min(self.n_tokens if max_new is None else int(max_new), self.n_tokens),
-                                   0 if max_len is None else int(max_len), int(page_table.shape[1]), 0,
+                                   0 if max_len is None else int(max_len), int(page_table.shape[1]),
+                                   page_table.stride(0) if self.n_seqs > 1 else 0,
                                    self.page_table.data_ptr(), self.new_start.data_ptr(), self.kv_len.data_ptr())
 
     def _for(self, cache: "KvCache") -> wb.wb_kv_batch:

@@ -6,7 +6,7 @@ import torch
 
 from oracle import rollout as orc
 from paper_2609_25442_b200 import rollout
-from test_gpu_rollout import DEV, run_verify
+from test_gpu_rollout import DEV, E4M3, Case, run_verify
 
 pytestmark = pytest.mark.gpu
 
@@ -29,3 +29,35 @@ def test_verify_broadcast_rows(dtype, vocab):
             s, e = starts[b], starts[b + 1]
             wa, wt = orc.verify(pf[s + b:e + b + 1], qf[s:e], tokens[s:e], uniform[s:e], race[0].cpu().numpy(), 4)
             assert a[b] == wa and np.array_equal(out[b], wt), b
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+def test_sliced_table_is_read_in_place(dtype):
+    """A kept batch over a slice of a wider table: pages that are entered later are written, read and attended over, and a
+    neighbouring column is never taken for one of the slice."""
+    lens, new = [70, 40, 33], [70, 3, 33]
+    c = Case(lens, new, 4, 2, 64, 16, dtype, seed=21)
+    width = c.table.shape[1]
+    wide = torch.full((3, width + 5), c.table.max() + 0, dtype=torch.int32, device=DEV)
+    view = wide[:, 2:2 + width]
+    view.fill_(-1)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    lens_t = torch.tensor(lens, **i32)
+    whole = rollout.KvBatch(view, torch.tensor(np.concatenate([[0], np.cumsum(lens)]), **i32), lens_t, n_tokens=sum(lens))
+    step = rollout.KvBatch(view, torch.tensor(np.concatenate([[0], np.cumsum(new)]), **i32), lens_t, n_tokens=sum(new))
+    k, v = c.rows()
+    c.cache.write(whole, k, v)
+    assert bool(c.k.float().isnan().all())               # no page yet
+    view.copy_(torch.tensor(c.table, device=DEV))
+    c.cache.write(whole, k, v)
+    same = [x.clone() for x in c.cache.read(whole, dtype=torch.float32)]
+    assert all(torch.equal(a, b) for a, b in zip(same, c.cache.read(c.whole, dtype=torch.float32)))
+    q = c.queries()
+    ws = rollout.AttendWorkspace(c.cache, 4, 3)
+    out, lse = c.cache.attend(step, q, workspace=ws)
+    ws.check()
+    c.check_attend(q, out, lse)
+    # positions past the slice have no page, whatever stands in the wider table
+    narrow = rollout.KvBatch(wide[:, 2:4], whole.new_start, lens_t, n_tokens=sum(lens))
+    rk, _ = c.cache.read(narrow, dtype=torch.float32)
+    assert torch.equal(rk[:32], same[0][:32]) and bool((rk[32:70] == 0).all()) and torch.equal(rk[70:102], same[0][70:102])

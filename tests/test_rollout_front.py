@@ -67,3 +67,27 @@ def test_c_entry_takes_a_pitch_of_zero():
     for name in ("target_stride", "draft_stride", "race_stride"):
         with pytest.raises(wb.WbError):
             wb.wb_verify_drafts(verify_args(n_seqs=0, **{name: 1}))
+
+
+def batch_of(table, **kw):
+    n = table.shape[0]
+    ints = lambda x: torch.tensor(x, dtype=torch.int32)
+    return rollout.KvBatch(table, ints(list(range(n + 1))), ints([5] * n), n_tokens=n, max_new=1, max_len=40, **kw)
+
+
+@pytest.mark.parametrize("cut", [slice(0, 3), slice(2, 5), slice(7, 8)])
+def test_batch_uses_a_sliced_table_in_place(cut):
+    """The kernels see later changes of a sliced table, as they do of a whole one, of new_start and of kv_len."""
+    big = torch.full((4, 8), -1, dtype=torch.int32)
+    b = batch_of(big[:, cut])
+    assert b.args.page_table == big.data_ptr() + 4 * cut.start
+    assert (b.args.table_stride, b.args.table_pitch) == (cut.stop - cut.start, 8)
+    one = batch_of(big[1:2, cut])
+    assert (one.args.page_table, one.args.table_stride) == (big.data_ptr() + 4 * (8 + cut.start), cut.stop - cut.start)
+
+
+def test_batch_refuses_tables_whose_rows_overlap_or_are_not_contiguous():
+    big = torch.zeros(4, 8, dtype=torch.int32)
+    for table in (big[:1].expand(4, 8), torch.zeros(30, dtype=torch.int32).as_strided((4, 8), (4, 1)), big[:, ::2], big.t()[:4]):
+        with pytest.raises(ValueError, match="page_table"):
+            batch_of(table)
