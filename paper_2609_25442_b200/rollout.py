@@ -82,6 +82,8 @@ class KvBatch:
                                    self.page_table.data_ptr(), self.new_start.data_ptr(), self.kv_len.data_ptr())
 
     def _for(self, cache: "KvCache") -> wb.wb_kv_batch:
+        if self.device != cache.device:
+            raise ValueError(f"batch on {self.device}, cache on {cache.device}")
         if self._max_len is None:                       # the table's capacity bounds every length
             self.args.max_len = self._table_pages * cache.page_size
         return self.args
@@ -151,6 +153,8 @@ class KvCache:
         sequences' ends; window > 0 limits a query to that many latest positions.  Returns (out, lse)."""
         if q.dim() != 3:
             raise ValueError("q: [n_tokens, n_heads, head_dim]")
+        if workspace.device != self.device:
+            raise ValueError(f"workspace on {workspace.device}, cache on {self.device}")
         n, h = batch.n_tokens, q.shape[1]
         a = _heads(q, "q", n, h, self.head_dim, self.device)
         if out is None:
@@ -174,7 +178,7 @@ class AttendWorkspace:
         self.bytes = cache._kv.attend_workspace_bytes(n_heads, n_seqs)
         _require(self.bytes > 0, f"no workspace for {n_heads} heads and {n_seqs} sequences over this cache")
         self.buffer = torch.zeros(self.bytes, dtype=torch.uint8, device=cache.device)
-        self.pointer = self.buffer.data_ptr()
+        self.pointer, self.device = self.buffer.data_ptr(), cache.device
 
     def check(self) -> None:
         """Waits for the current stream; raises if a kernel that used this workspace gave up waiting inside."""

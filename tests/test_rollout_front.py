@@ -91,3 +91,58 @@ def test_batch_refuses_tables_whose_rows_overlap_or_are_not_contiguous():
     for table in (big[:1].expand(4, 8), torch.zeros(30, dtype=torch.int32).as_strided((4, 8), (4, 1)), big[:, ::2], big.t()[:4]):
         with pytest.raises(ValueError, match="page_table"):
             batch_of(table)
+
+
+# ---- a cache that is not there: calls are recorded ------------------------------------------------------------------
+class Recorder:
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *args: self.calls.append((name, args))
+
+
+@pytest.fixture
+def cache(monkeypatch):
+    """A bf16 cache of 8 pages x 2 heads x 16 slots x 64 on cuda:0 without memory."""
+    monkeypatch.setattr(rollout, "_stream", lambda index: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    c = rollout.KvCache.__new__(rollout.KvCache)
+    c.n_pages, c.n_kv_heads, c.page_size, c.head_dim = 8, 2, 16, 64
+    c.device, c._index, c._scale, c._kv = torch.device("cuda", 0), 0, 0.125, Recorder()
+    c._like = {t: gpu(torch.empty(0, dtype=t)) for t in (torch.float32, torch.bfloat16)}
+    return c
+
+
+def gpu_batch(n=2, on=gpu, **kw):
+    ints = lambda x: on(torch.tensor(x, dtype=torch.int32))
+    d = dict(page_table=ints([[0, 1]] * n), new_start=ints(list(range(n + 1))), kv_len=ints([5] * n), n_tokens=n, max_new=1, max_len=32)
+    d.update(kw)
+    return rollout.KvBatch(**d)
+
+
+def workspace(device=torch.device("cuda", 0)):
+    w = rollout.AttendWorkspace.__new__(rollout.AttendWorkspace)
+    w.bytes, w.pointer, w.device = 1 << 30, 1 << 20, device
+    return w
+
+
+def all_calls(cache, batch, ws=None, **kw):
+    rows, q = gpu(torch.zeros(batch.n_tokens, 2, 64, dtype=torch.bfloat16)), gpu(torch.zeros(batch.n_tokens, 4, 64, dtype=torch.bfloat16))
+    return [lambda: cache.write(batch, rows, rows), lambda: cache.read(batch), lambda: cache.attend(batch, q, workspace=ws or workspace(), **kw)]
+
+
+def test_calls_reach_the_library(cache):
+    for f in all_calls(cache, gpu_batch()):
+        f()
+    assert [name for name, _ in cache._kv.calls] == ["write", "read", "attend"]
+
+
+def test_batches_and_workspaces_of_another_device_are_refused(cache):
+    """Index arrays in host memory, or a workspace elsewhere, are pointers that the kernels must not get."""
+    for f in all_calls(cache, gpu_batch(on=lambda t: t)):
+        with pytest.raises(ValueError, match="batch"):
+            f()
+    with pytest.raises(ValueError, match="workspace"):
+        all_calls(cache, gpu_batch(), workspace(torch.device("cuda", 1)))[2]()
+    assert not cache._kv.calls
