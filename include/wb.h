@@ -589,7 +589,8 @@ wb_status wb_scan_slices(const wb_diff2_entry* nz, size_t n, uint64_t rows, uint
  * paged cache, wb_kv_attend lets the new tokens attend over everything the cache holds of their
  * sequence, wb_kv_read copies rows back out, and wb_verify_drafts accepts or rejects the tokens a
  * drafter proposed.  All calls are asynchronous on the given stream, allocate nothing, copy
- * nothing between host and device, and can be captured in a CUDA graph.
+ * nothing between host and device, and can be captured in a CUDA graph.  They launch on the current device, which has to
+ * be the one that holds their memory.
  *
  * The cache.  Keys and values each live in n_pages pages of page_size slots; the rows (head_dim
  * elements) of one (page, head) are contiguous: slot s of head h in page p starts at element
@@ -617,7 +618,8 @@ typedef struct {
 typedef struct wb_kv wb_kv;
 
 /* Validates a cache's description and encodes its tensor maps (host memory only; nothing of the
- * cache is read or written).  The handle stays valid while the cache's memory does. */
+ * cache is read or written).  The handle stays valid while the cache's memory does.  It belongs to the device that is
+ * current here, where the cache's memory has to be: calls from another current device are refused. */
 wb_status wb_kv_open(const wb_kv_desc* desc, wb_kv** out);
 void wb_kv_free(wb_kv* kv);
 

@@ -331,6 +331,11 @@ extern "C" wb_status wb_kv_open(const wb_kv_desc* d, wb_kv** out) {
   if (!kv) return WB_ERR_OOM;
   kv->d = *d;
   kv->box_rows = std::gcd(d->page_size, kKvTile);
+  if (cudaGetDevice(&kv->device) != cudaSuccess) {
+    (void)cudaGetLastError();
+    delete kv;
+    return WB_ERR_CUDA;
+  }
   if (!encode_map(kv->d, d->k, kv->box_rows, &kv->map_k) || !encode_map(kv->d, d->v, kv->box_rows, &kv->map_v)) {
     delete kv;
     return WB_ERR_CUDA;

@@ -16,6 +16,7 @@ struct wb_kv {
   // a page, and coordinates outside the cache read as zeros
   CUtensorMap map_k, map_v;
   uint32_t box_rows;
+  int device;                // the one that was current at wb_kv_open: calls launch there and nowhere else
 };
 
 namespace wbi {
@@ -50,13 +51,18 @@ inline KvBatch kv_batch(const wb_kv_batch* b) {
                  b->table_pitch ? b->table_pitch : b->table_stride, (int32_t)b->max_len};
 }
 
+inline bool on_kv_device(const wb_kv* kv) {
+  int dev = -1;
+  return cudaGetDevice(&dev) == cudaSuccess && dev == kv->device;
+}
+
 inline wb_status check_batch(const wb_kv* kv, const wb_kv_batch* b) {
   if (!kv || !b || b->n_seqs > WB_KV_MAX_SEQS || (b->table_pitch && b->table_pitch < b->table_stride)) return WB_ERR_INVALID_ARG;
   if (b->n_tokens > 0x7FFFFFFFu || b->max_len > 0x7FFFFFFFu || b->max_new > b->n_tokens) return WB_ERR_INVALID_ARG;
   if (b->n_seqs && (!b->new_start || !b->kv_len || (b->table_stride && !b->page_table))) return WB_ERR_INVALID_ARG;
   // positions are 32-bit: a row of the table covers fewer than 2^31 of them
   if ((uint64_t)b->table_stride * kv->d.page_size > 0x7FFFFFFFull) return WB_ERR_INVALID_ARG;
-  return WB_OK;
+  return on_kv_device(kv) ? WB_OK : WB_ERR_INVALID_ARG;
 }
 
 inline wb_status check_heads(const wb_heads* h, uint32_t n_tokens, bool allow_f32) {

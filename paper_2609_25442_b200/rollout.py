@@ -1,6 +1,6 @@
 """A rollout engine's step on torch tensors: the paged key/value cache (written, read back, attended over)
 and the verification of drafted tokens.  The work is done by libwb.so; this module checks tensors,
-allocates results and passes torch's current stream.
+allocates results and passes torch's current stream.  All tensors are on the current device.
 
     cache = KvCache.empty(n_pages, n_kv_heads, page_size, head_dim, dtype=torch.float8_e4m3fn)
     batch = KvBatch(page_table, new_start, kv_len, n_tokens=T, max_new=..., max_len=...)
@@ -21,6 +21,15 @@ _E4M3 = torch.float8_e4m3fn
 
 
 _stream = torch._C._cuda_getCurrentRawStream      # of a device index; torch.cuda.current_stream builds an object first
+
+
+_current_device = torch._C._cuda_getDevice
+
+
+def _on_device(index: int) -> None:
+    """Kernels go to the current device (a default stream has the same handle on all of them)."""
+    if _current_device() != index:
+        raise ValueError(f"tensors on cuda:{index}, but the current device is cuda:{_current_device()}")
 
 
 def _require(ok: bool, what: str) -> None:
@@ -84,6 +93,7 @@ class KvBatch:
     def _for(self, cache: "KvCache") -> wb.wb_kv_batch:
         if self.device != cache.device:
             raise ValueError(f"batch on {self.device}, cache on {cache.device}")
+        _on_device(cache._index)
         if self._max_len is None:                       # the table's capacity bounds every length
             self.args.max_len = self._table_pages * cache.page_size
         return self.args
@@ -97,6 +107,7 @@ class KvCache:
         _require(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device,
                  "k and v: the same shape [n_pages, n_kv_heads, page_size, head_dim], strides, type and device")
         _require(k.is_cuda, "the cache needs a CUDA device (sm_100a)")
+        _on_device(k.device.index)
         _require(k.dtype in (torch.bfloat16, _E4M3), f"cache of {k.dtype}: bfloat16 or float8_e4m3fn")
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = (int(x) for x in k.shape)
         _require(k.stride(3) == 1 and k.stride(2) == self.head_dim, "a page's slots must be contiguous rows")
@@ -182,7 +193,8 @@ class AttendWorkspace:
 
     def check(self) -> None:
         """Waits for the current stream; raises if a kernel that used this workspace gave up waiting inside."""
-        wb.wb_kv_attend_check(self.pointer, _stream(self.buffer.device.index))
+        _on_device(self.device.index)
+        wb.wb_kv_attend_check(self.pointer, _stream(self.device.index))
 
 
 def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tokens: torch.Tensor, draft_start: torch.Tensor,
@@ -196,6 +208,7 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
     n, vocab, total = draft_start.shape[0] - 1, target.shape[1], draft_tokens.shape[0]
     if not target.is_cuda or target.dim() != 2 or n < 0 or target.shape[0] != total + n or target.stride(1) != 1:
         raise ValueError("target: [n_drafts + n_seqs, vocab] with contiguous rows on a CUDA device")
+    _on_device(dev.index)
     if target.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError(f"probabilities of {target.dtype}: float32 or bfloat16")
     if draft is not None and (draft.shape != (total, vocab) or draft.dtype != target.dtype or draft.device != dev or draft.stride(1) != 1):

@@ -20,6 +20,7 @@ def gpu(t):
 def verified(monkeypatch):
     """The arguments of every wb_verify_drafts call."""
     calls = []
+    monkeypatch.setattr(rollout, "_current_device", lambda: 0, raising=False)
     monkeypatch.setattr(rollout, "_stream", lambda index: 0)
     monkeypatch.setattr(rollout.wb, "wb_verify_drafts", lambda args, stream=0: calls.append(args))
     return calls
@@ -106,7 +107,7 @@ class Recorder:
 def cache(monkeypatch):
     """A bf16 cache of 8 pages x 2 heads x 16 slots x 64 on cuda:0 without memory."""
     monkeypatch.setattr(rollout, "_stream", lambda index: 0)
-    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    monkeypatch.setattr(rollout, "_current_device", lambda: 0, raising=False)
     c = rollout.KvCache.__new__(rollout.KvCache)
     c.n_pages, c.n_kv_heads, c.page_size, c.head_dim = 8, 2, 16, 64
     c.device, c._index, c._scale, c._kv = torch.device("cuda", 0), 0, 0.125, Recorder()
@@ -146,3 +147,17 @@ def test_batches_and_workspaces_of_another_device_are_refused(cache):
     with pytest.raises(ValueError, match="workspace"):
         all_calls(cache, gpu_batch(), workspace(torch.device("cuda", 1)))[2]()
     assert not cache._kv.calls
+
+
+def test_calls_from_another_current_device_are_refused(cache, verified, monkeypatch):
+    """A default stream's handle is 0 on every device: a launch would go to the current one, with the other's pointers."""
+    batch, drafts, ws = gpu_batch(), drafts_of(), workspace()
+    ws.buffer = gpu(torch.zeros(8))
+    checked = []
+    monkeypatch.setattr(rollout.wb, "wb_kv_attend_check", lambda *a: checked.append(a))
+    pages = gpu(torch.zeros(8, 2, 16, 64, dtype=torch.bfloat16))
+    monkeypatch.setattr(rollout, "_current_device", lambda: 1, raising=False)
+    for f in all_calls(cache, batch) + [lambda: rollout.verify_drafts(**drafts, max_drafts=2), ws.check, lambda: rollout.KvCache(pages, pages)]:
+        with pytest.raises(ValueError, match="current device"):
+            f()
+    assert not cache._kv.calls and not verified and not checked
