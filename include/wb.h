@@ -666,11 +666,14 @@ wb_status wb_kv_read(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* 
 
 /* Attention of the new tokens over the cache (their own keys and values already written):
  *   out[t, h] = sum_j softmax_j(scale * q[t, h] . K[j, g]) V[j, g],   g = h / (n_heads / n_kv_heads),
- * over the positions j <= pos(t) of t's sequence, with window > 0 only those with j > pos(t) - window.
+ * over the positions j <= pos(t) of t's sequence, with window > 0 only those with j > pos(t) - window (a window of max_len or more
+ * limits nothing).
  * lse[t, h] (fp32, contiguous [n_tokens][n_heads], may be NULL) is the natural logarithm of the
  * softmax's denominator.  A row with nothing to attend over gives zeros and lse = -inf; what masked
  * slots and unused parts of pages hold does not matter (NaN included).  q and out are bf16;
- * n_heads is a multiple of n_kv_heads, n_heads / n_kv_heads at most 64, and scale is positive and finite.
+ * n_heads is a multiple of n_kv_heads, n_heads / n_kv_heads at most 64, and scale is positive and finite.  Refused where the
+ * work cannot be counted in 31 bits: max_len + n_tokens above 2^31 - 256, or
+ * (n_tokens * n_heads / n_kv_heads / 256 + n_seqs) * (max_len / 64 + 2) * n_kv_heads above 2^31.
  * workspace: wb_kv_attend_workspace_bytes device bytes, 256-byte aligned, zeroed once by the caller
  * before its first use; it carries no results from call to call, and calls that may overlap need one each. */
 wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* q, uint32_t n_heads,

@@ -123,7 +123,8 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < wb_kv_attend_workspace_bytes(kv, n_heads, batch->n_seqs))
     return WB_ERR_INVALID_ARG;
   if (!batch->n_tokens || !batch->n_seqs) return WB_OK;
-  // the kernels count tiles in 31 bits
+  // positions from -n_tokens to max_len, and what windows and tiles add to them, are counted in 31 bits, and so are tiles
+  if ((uint64_t)batch->max_len + batch->n_tokens > 0x7FFFFF00ull) return WB_ERR_INVALID_ARG;
   const uint64_t group = n_heads / kv->d.n_kv_heads, row_blocks = (uint64_t)batch->n_tokens * group / kQRows + batch->n_seqs;
   if (row_blocks * (batch->max_len / kKvTile + 2) * kv->d.n_kv_heads > 0x7FFFFFFFull) return WB_ERR_INVALID_ARG;
   AttendArgs a;
@@ -137,7 +138,7 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   a.scale_log2 = scale * 1.4426950408889634f;
   a.n_heads = n_heads;
   a.group = n_heads / kv->d.n_kv_heads;
-  a.window = window;
+  a.window = window < batch->max_len ? window : 0;      // (the kernels' first positions are differences with it)
   a.box_rows = kv->box_rows;
   a.error = (uint32_t*)workspace;
   a.cuts = (char*)workspace + kHeaderBytes;

@@ -6,7 +6,7 @@ import torch
 
 from oracle import rollout as orc
 from paper_2609_25442_b200 import rollout
-from test_gpu_rollout import DEV, E4M3, Case, run_verify
+from test_gpu_rollout import DEV, E4M3, Case, attend, run_verify
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,32 @@ def test_sliced_table_is_read_in_place(dtype):
     narrow = rollout.KvBatch(wide[:, 2:4], whole.new_start, lens_t, n_tokens=sum(lens))
     rk, _ = c.cache.read(narrow, dtype=torch.float32)
     assert torch.equal(rk[:32], same[0][:32]) and bool((rk[32:70] == 0).all()) and torch.equal(rk[70:102], same[0][70:102])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("heads", [4, 32])
+def test_windows_without_a_limit(dtype, heads):
+    """A window of the longest length or more limits nothing, up to the largest number there is, also in a sequence with more new
+    tokens than it holds."""
+    c = Case([3, 200, 1, 0], [6, 9, 6, 2], heads, 2, 64, 16, dtype, seed=31)
+    k, v = c.rows()
+    c.cache.write(c.whole, k, v)
+    q = c.queries()
+    want, wlse = attend(c, q)
+    c.check_attend(q, want, wlse)
+    for window in (200, 201, 1 << 20, (1 << 31) - 300, (1 << 31) - 7, (1 << 31) - 2, (1 << 31) - 1):
+        out, lse = attend(c, q, window)
+        assert torch.equal(out, want) and torch.equal(lse, wlse), window
+    for window in (198, 199):
+        out, lse = attend(c, q, window)
+        c.check_attend(q, out, lse, window)
+
+
+def test_lengths_that_positions_cannot_count_are_refused():
+    c = Case([20], [3], 2, 2, 64, 16, torch.bfloat16)
+    q = c.queries()
+    ws = rollout.AttendWorkspace(c.cache, 2, 1)
+    for most in ((1 << 31) - 1, (1 << 31) - 258):
+        b = rollout.KvBatch(c.batch.page_table, c.batch.new_start, c.batch.kv_len, n_tokens=3, max_new=3, max_len=most)
+        with pytest.raises(Exception, match="WB_ERR_INVALID_ARG"):
+            c.cache.attend(b, q, workspace=ws)
