@@ -312,8 +312,8 @@ __device__ __forceinline__ void queries_arrived() {
   fence_async();
 }
 
-// One cache row of a value tile: cleared if it lies past the end; else its values that are not finite are taken out, and the
-// flag is raised first, so that whoever finds them gone finds the flag.  True if anything was written.
+// One cache row of a value tile: cleared if it lies past the end; else its values that are not finite are taken out and the
+// flag is raised, which both tiles read after their last product.  True if anything was written.
 template <int D>
 __device__ __forceinline__ bool clear_values(char* tile, uint32_t row, bool past, volatile uint32_t* flag) {
   char* v = tile + row * 128;
@@ -333,7 +333,6 @@ __device__ __forceinline__ bool clear_values(char* tile, uint32_t row, bool past
   }
   if (!odd) return false;
   *flag = 1;
-  __threadfence_block();
   for (uint32_t c = 0; c < D / 2; ++c) {
     uint32_t* at = reinterpret_cast<uint32_t*>(v + (c >> 5) * (kKeys * 128)) + (c & 31);
     uint32_t y = *at;
@@ -485,8 +484,10 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           }
           const int32_t pos0 = (w.blk.kt0 + t - tile0) * (int32_t)kKeys;
           const bool cut = pos0 + (int32_t)kKeys - 1 > cut_hi || pos0 < cut_lo;
-          if (!Q && cut) {
-            // values past the end, and values that are not finite, must not meet weights of zero
+          if (!Q && cut && i == 0) {
+            // Values past the end, and values that are not finite, must not meet weights of zero.  Only the first tile's threads
+            // write, one to a row: each then orders its own writes before the products, which wait for this tile's
+            // weights first, and the other tile's products follow this one's.
             const uint32_t vq = 2 * jg + 1, slot = vq % C::kSlots;
             ok = wait_or_give_up(full + 8 * slot, (vq / C::kSlots) & 1, ok, a.error);
             if (clear_values<D>(smem + C::kOffSlots + slot * C::kSlotBytes, row, pos0 + (int32_t)row >= w.seq.len, misc + 8 + item % 8)) fence_async();

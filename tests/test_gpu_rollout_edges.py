@@ -90,3 +90,30 @@ def test_lengths_that_positions_cannot_count_are_refused():
         b = rollout.KvBatch(c.batch.page_table, c.batch.new_start, c.batch.kv_len, n_tokens=3, max_new=3, max_len=most)
         with pytest.raises(Exception, match="WB_ERR_INVALID_ARG"):
             c.cache.attend(b, q, workspace=ws)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("window", [0, 90])
+def test_values_that_are_not_finite_in_the_chunk_itself(dim, window):
+    """Infinities and NaN all over the new tokens' own values, which both row tiles of a block meet in tiles that are cut: a row
+    is not finite exactly where it sees one, and everything else is as if they were zeros."""
+    length, new = 700, 300
+    c = Case([length], [new], 8, 2, dim, 16, torch.bfloat16, seed=41 + dim)
+    k, v = c.rows()
+    bad = torch.zeros(length, 2, dim, dtype=torch.bool, device=DEV)
+    where = np.random.default_rng(5)
+    for pos in range(length - new, length, 7):
+        bad[pos, int(where.integers(2)), int(where.integers(dim))] = True
+    what = torch.tensor([float("inf"), float("-inf"), float("nan")], device=DEV).bfloat16()[torch.arange(length, device=DEV) % 3]
+    c.cache.write(c.whole, k, torch.where(bad, torch.zeros_like(v), v))
+    q = c.queries()
+    want, wlse = attend(c, q, window)
+    c.check_attend(q, want, wlse, window)
+    c.cache.write(c.whole, k, torch.where(bad, what[:, None, None], v))
+    pos, at = torch.arange(length, device=DEV), torch.arange(new, device=DEV)[:, None] + length - new
+    sees = (pos[None] <= at) & ((pos[None] > at - window) if window else True)
+    hit = torch.einsum("tl,lhd->thd", sees.float(), bad.float()).repeat_interleave(4, 1) > 0
+    for _ in range(5):
+        out, lse = attend(c, q, window)
+        assert torch.equal(out.isfinite(), ~hit) and torch.equal(lse, wlse)
+        assert torch.equal(out[~hit], want[~hit])
