@@ -753,6 +753,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
                             a.box_rows * 4, sbar);
                 } else if (Q) {
                   for (uint32_t e = 0; e < a.box_rows; ++e) reinterpret_cast<float*>(smem + C::kOffScale)[sc * kKeys + r0 + e] = 0.f;
+                  fence_async();      // before this lane's next load into the same place
                   bar_arrive(sbar);
                 }
               } else {
@@ -786,11 +787,11 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           // a weight of zero must not meet a scale that is none: one past the end may be anything, and one that is not
           // finite is taken out here and added to the rows that see it at the end
           float* at = reinterpret_cast<float*>(smem + C::kOffScale) + sc * kKeys + row;
-          if ((w.blk.kt0 + t - w.item0 - kItemCost) * (int32_t)kKeys + (int32_t)row >= w.seq.len) {
+          const bool past = (w.blk.kt0 + t - w.item0 - kItemCost) * (int32_t)kKeys + (int32_t)row >= w.seq.len;
+          if (past || !isfinite(*at)) {
+            if (!past) misc[8 + item % 8] = 1;
             *at = 0.f;
-          } else if (!isfinite(*at)) {
-            misc[8 + item % 8] = 1;
-            *at = 0.f;
+            fence_async();            // before the next load into the same place, which waits for the softmax's arrivals only
           }
           if (++t == min(end, w.item0 + w.blk.n) && t < end) {
             walk_on(w, a, cum, skip_rows);

@@ -6,7 +6,7 @@ import torch
 
 from oracle import rollout as orc
 from paper_2609_25442_b200 import rollout
-from test_gpu_rollout import DEV, E4M3, Case, attend, run_verify
+from test_gpu_rollout import DEV, E4M3, Case, attend, out_bound, run_verify
 
 pytestmark = pytest.mark.gpu
 
@@ -117,3 +117,27 @@ def test_values_that_are_not_finite_in_the_chunk_itself(dim, window):
         out, lse = attend(c, q, window)
         assert torch.equal(out.isfinite(), ~hit) and torch.equal(lse, wlse)
         assert torch.equal(out[~hit], want[~hit])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("dim,new,window", [(64, 100, 0), (128, 100, 0), (128, 2, 0), (64, 150, 400)])
+def test_attend_among_pages_that_do_not_exist(dtype, dim, new, window):
+    """Long sequences, a third of whose pages are missing: zeros take turns with loaded rows and scales in every slot."""
+    c = Case([2000, 900], [new, 1], 8, 2, dim, 16, dtype, seed=51)
+    k, v = c.rows()
+    c.cache.write(c.whole, k, v)
+    hole = np.random.default_rng(6).random(c.table.shape) < 0.33
+    c.table[hole] = np.where(np.arange(c.table.size).reshape(c.table.shape) % 2, -1, 1 << 29)[hole]
+    table = torch.tensor(c.table, device=DEV)
+    c.batch = rollout.KvBatch(table, c.batch.new_start, c.batch.kv_len, n_tokens=new + 1, max_new=new, max_len=2000)
+    whole = rollout.KvBatch(table, c.whole.new_start, c.whole.kv_len, n_tokens=2900)
+    kk, vv = (x.transpose(0, 1).cpu().numpy() for x in c.cache.read(whole, dtype=torch.float32))
+    assert 300 < (vv == 0).all((0, 2)).sum() < 1800
+    q = c.queries()
+    out, lse = attend(c, q, window)
+    t = 0
+    for (a, b), n in zip(((0, 2000), (2000, 2900)), (new, 1)):
+        want, wl, mag = orc.attend(q[t:t + n].float().cpu().numpy(), kk[:, a:b], vv[:, a:b], n, dim ** -0.5, window)
+        assert (np.abs(out[t:t + n].float().cpu().numpy() - want) <= out_bound(want, mag)).all()
+        assert np.allclose(lse[t:t + n].cpu().numpy(), wl, rtol=0, atol=1e-4)
+        t += n
