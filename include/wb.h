@@ -627,8 +627,10 @@ void wb_kv_free(wb_kv* kv);
  * slot t % page_size of page page_table[b][t / page_size].  After the step the cache holds kv_len[b]
  * tokens of it; the last new_start[b+1] - new_start[b] of them are the new ones, which are rows
  * [new_start[b], new_start[b+1]) of the step's tensors.  max_new and max_len are the host's upper
- * bounds on a sequence's new tokens and on kv_len (they size the launch; a loose max_len only costs
- * blocks that end at once, results beyond a max_new that is too small are not computed).  A position
+ * bounds on a sequence's new tokens and on kv_len.  wb_kv_attend goes by both: a loose max_len costs nothing, with one that is too
+ * small a longer sequence's rows are zeros with lse = -inf and wb_kv_attend_check tells; max_new chooses the kernels, by the rows
+ * of the longest chunk (a loose one costs time, up to twice a decoding step's), and results beyond one that is too
+ * small are not computed.  A position
  * that the table does not cover, or whose page is not in [0, n_pages), is not written, reads as zeros
  * and is attended over as zeros: table entries past a sequence's last page may hold anything.  The arrays are
  * read more than once: they must not change while a call that was given them runs. */
@@ -680,8 +682,9 @@ wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads
                        const wb_heads* out, float* lse, float scale, uint32_t window, void* workspace,
                        size_t workspace_bytes, void* cuda_stream);
 size_t wb_kv_attend_workspace_bytes(const wb_kv* kv, uint32_t n_heads, uint32_t n_seqs);
-/* Waits for the stream and reports whether a kernel that used the workspace gave up waiting inside (every wait is
- * bounded, so that a lost signal cannot hang the GPU): WB_ERR_CUDA, and its results are not to be used. */
+/* Waits for the stream and reports whether a call that used the workspace has results that are not to be used: WB_ERR_CUDA if a
+ * kernel gave up waiting inside (every wait is bounded, so that a lost signal cannot hang the GPU), WB_ERR_INVALID_ARG if a
+ * sequence was longer than max_len. */
 wb_status wb_kv_attend_check(const void* workspace, void* cuda_stream);
 
 /* Verification of drafted tokens.  Sequence b drafted K = draft_start[b+1] - draft_start[b] tokens

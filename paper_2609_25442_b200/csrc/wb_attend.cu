@@ -169,5 +169,5 @@ extern "C" wb_status wb_kv_attend_check(const void* workspace, void* stream) {
     (void)cudaGetLastError();
     return WB_ERR_CUDA;
   }
-  return error ? WB_ERR_CUDA : WB_OK;
+  return error & (kGaveUp | kMisplaced) ? WB_ERR_CUDA : error & kTooLong ? WB_ERR_INVALID_ARG : WB_OK;
 }

@@ -15,7 +15,7 @@ struct AttendArgs {
   float scale_log2;                             // softmax scale times log2(e)
   uint32_t n_heads, group, window;
   uint32_t box_rows;
-  uint32_t* error;                              // workspace: first word
+  uint32_t* error;                              // workspace: first word, bits of AttendError
   char* cuts;                                   // CutItem of every block
   float* partials;
 };
@@ -24,6 +24,12 @@ struct AttendArgs {
 struct CutItem {
   uint32_t parts;          // 0: none
   uint32_t s, h, rb;       // sequence, kv head, row block; for the row kernel: first row of the step's tensors, kv head, rows
+};
+
+enum AttendError : uint32_t {
+  kGaveUp = 1,             // a wait lasted too long
+  kMisplaced = 2,          // shared memory not where tiles need it
+  kTooLong = 4,            // a sequence was longer than max_len
 };
 
 constexpr float kLn2 = 0.69314718055994531f;
@@ -63,7 +69,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
 // error word tells.
 __device__ __forceinline__ bool wait_or_give_up(uint32_t bar, uint32_t parity, bool ok, uint32_t* error) {
   if (ok && !bar_wait(bar, parity)) {
-    atomicMax(error, 1u);
+    atomicOr(error, kGaveUp);
     return false;
   }
   return ok;
@@ -99,10 +105,16 @@ __device__ __forceinline__ uint32_t e4m3_to_bf16x2(uint32_t x) {
   return r;
 }
 
+// A sequence that is longer than the call was checked for has nothing to attend over: with its length cut its new tokens would
+// stand at other positions than they were written to, and its results would look right.
 __device__ __forceinline__ KvSeq attend_seq(const KvBatch& b, uint32_t s) {
   KvSeq q = kv_seq(b, s);
-  q.len = min(q.len, b.max_len);
+  if (q.len > b.max_len) q.len = 0;
   return q;
+}
+__device__ __forceinline__ void report_too_long(const AttendArgs& a, uint32_t s) {
+  const KvSeq q = kv_seq(a.b, s);
+  if (blockIdx.x == 0 && q.n_new > 0 && q.len > a.b.max_len) atomicOr(a.error, kTooLong);
 }
 
 // First position that any of the sequence's new tokens attends over.

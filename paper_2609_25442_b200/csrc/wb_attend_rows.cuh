@@ -144,6 +144,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         const int32_t lo = first_position(q, a.window) / (int32_t)kKvTile;
         nt = max(1, (q.len + (int32_t)kKvTile - 1) / (int32_t)kKvTile - lo);
       }
+      report_too_long(a, s);
       cum[s + 1] = nt * (int32_t)hk;     // this thread's own entries, made inclusive below
       sum += nt * (int32_t)hk;
     }

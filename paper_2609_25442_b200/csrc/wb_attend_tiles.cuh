@@ -359,7 +359,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
   volatile uint32_t* const misc = reinterpret_cast<volatile uint32_t*>(smem + C::kOffMisc);   // [0] tensor memory, [5, 6] share, [8..15] items' flags
   int32_t* const cum = reinterpret_cast<int32_t*>(smem + C::kOffCum);
   if (base & 1023u) {      // swizzled tiles need it; never the case without static shared memory
-    if (tid == 0) atomicMax(a.error, 2u);
+    if (tid == 0) atomicOr(a.error, kMisplaced);
     return;
   }
 
@@ -398,7 +398,10 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
     int32_t sum = 0;
     for (uint32_t rb = lane; rb < nb; rb += 32) sum += row_block(q, a.group, a.window, rb).n;
     sum = __reduce_add_sync(0xFFFFFFFFu, sum);
-    if (lane == 0) cum[s + 1] = sum * (int32_t)hk;
+    if (lane == 0) {
+      cum[s + 1] = sum * (int32_t)hk;
+      report_too_long(a, s);
+    }
   }
   if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(base + C::kOffMisc) : "memory");

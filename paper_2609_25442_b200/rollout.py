@@ -67,7 +67,9 @@ def _pitch(t: torch.Tensor, name: str) -> int:
 class KvBatch:
     """One step's sequences: `page_table` [n_seqs, pages] (a position's page), `new_start` [n_seqs + 1] (the rows of a
     sequence's new tokens), `kv_len` [n_seqs] (tokens in the cache after the step), all int32 on the device.
-    `max_new` and `max_len` bound a sequence's new tokens and its length; they size the launches.  The three tensors are used in
+    `max_new` and `max_len` bound a sequence's new tokens and its length.  Attention goes by them: its kernels are chosen by
+    `max_new` (give 1 for a batch that decodes: the default, `n_tokens`, is right but slower), and a sequence longer than
+    `max_len` (default: what the table covers) gets zeros and is reported by AttendWorkspace.check().  The three tensors are used in
     place (a table may be a slice of a wider one), so a batch can be kept while they are updated."""
 
     def __init__(self, page_table: torch.Tensor, new_start: torch.Tensor, kv_len: torch.Tensor, *, n_tokens: int,

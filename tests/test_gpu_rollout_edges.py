@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from oracle import rollout as orc
-from paper_2609_25442_b200 import rollout
+from paper_2609_25442_b200 import binding as wb, rollout
 from test_gpu_rollout import DEV, E4M3, Case, attend, out_bound, run_verify
 
 pytestmark = pytest.mark.gpu
@@ -141,3 +141,20 @@ def test_attend_among_pages_that_do_not_exist(dtype, dim, new, window):
         assert (np.abs(out[t:t + n].float().cpu().numpy() - want) <= out_bound(want, mag)).all()
         assert np.allclose(lse[t:t + n].cpu().numpy(), wl, rtol=0, atol=1e-4)
         t += n
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("new", [[3, 2, 1], [3, 90, 1]])
+def test_lengths_above_max_len_are_reported(dtype, new):
+    """A sequence longer than the host said has no results, rather than ones whose positions are off; the others have theirs."""
+    c = Case([150, 130, 40], new, 8, 2, 64, 16, dtype, seed=61)
+    k, v = c.rows()
+    c.cache.write(c.whole, k, v)
+    q = c.queries()
+    b = rollout.KvBatch(c.batch.page_table, c.batch.new_start, c.batch.kv_len, n_tokens=c.total, max_new=max(new), max_len=130)
+    ws = rollout.AttendWorkspace(c.cache, 8, 3)
+    out, lse = c.cache.attend(b, q, workspace=ws)
+    c.check_attend(q, out, lse, only=(1, 2))
+    assert bool((out[:3] == 0).all()) and bool(lse[:3].isneginf().all())
+    with pytest.raises(wb.WbError, match="WB_ERR_INVALID_ARG"):
+        ws.check()
