@@ -684,8 +684,9 @@ wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads
 size_t wb_kv_attend_workspace_bytes(const wb_kv* kv, uint32_t n_heads, uint32_t n_seqs);
 /* Waits for the stream and reports whether a call that used the workspace has results that are not to be used: WB_ERR_CUDA if a
  * kernel gave up waiting inside (every wait is bounded, so that a lost signal cannot hang the GPU), WB_ERR_INVALID_ARG if a
- * sequence was longer than max_len. */
-wb_status wb_kv_attend_check(const void* workspace, void* cuda_stream);
+ * sequence was longer than max_len.  Results count as confirmed when this returned WB_OK after them.  A report is given once: the
+ * workspace can be used again. */
+wb_status wb_kv_attend_check(void* workspace, void* cuda_stream);
 
 /* Verification of drafted tokens.  Sequence b drafted K = draft_start[b+1] - draft_start[b] tokens
  * x_0 .. x_{K-1} (K may be 0; at most max_drafts count), which are entries draft_start[b] + i of draft_tokens.

@@ -161,11 +161,12 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   return err == cudaSuccess ? WB_OK : WB_ERR_CUDA;
 }
 
-extern "C" wb_status wb_kv_attend_check(const void* workspace, void* stream) {
+extern "C" wb_status wb_kv_attend_check(void* workspace, void* stream) {
   if (!workspace || ((uintptr_t)workspace & 255u)) return WB_ERR_INVALID_ARG;
   uint32_t error = 0;
   const cudaStream_t st = (cudaStream_t)stream;
-  if (cudaMemcpyAsync(&error, workspace, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
+  if (cudaMemcpyAsync(&error, workspace, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess ||
+      (error && cudaMemsetAsync(workspace, 0, 4, st) != cudaSuccess)) {
     (void)cudaGetLastError();
     return WB_ERR_CUDA;
   }

@@ -163,7 +163,8 @@ class KvCache:
     def attend(self, batch: KvBatch, q: torch.Tensor, *, workspace: "AttendWorkspace", scale: Optional[float] = None,
                window: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
         """Attention of the new tokens' queries (bf16, [n_tokens, n_heads, head_dim]) over the cache, causal at the
-        sequences' ends; window > 0 limits a query to that many latest positions.  Returns (out, lse)."""
+        sequences' ends; window > 0 limits a query to that many latest positions.  Returns (out, lse), which are confirmed when
+        workspace.check() has passed after them; rows that no sequence holds are left as they are."""
         if q.dim() != 3:
             raise ValueError("q: [n_tokens, n_heads, head_dim]")
         if workspace.device != self.device:
@@ -185,7 +186,8 @@ class KvCache:
 
 
 class AttendWorkspace:
-    """Scratch memory of KvCache.attend for up to `n_seqs` sequences; calls that may overlap need one each."""
+    """Scratch memory of KvCache.attend for up to `n_seqs` sequences; calls that may overlap need one each.  What a call could not
+    do is noted in it (nothing is raised while kernels run): check() reads the note, for instance once a step."""
 
     def __init__(self, cache: KvCache, n_heads: int, n_seqs: int):
         self.bytes = cache._kv.attend_workspace_bytes(n_heads, n_seqs)
@@ -194,7 +196,8 @@ class AttendWorkspace:
         self.pointer, self.device = self.buffer.data_ptr(), cache.device
 
     def check(self) -> None:
-        """Waits for the current stream; raises if a kernel that used this workspace gave up waiting inside."""
+        """Waits for the current stream; raises if results of a call that used this workspace since the last check are not to be
+        used: a kernel gave up waiting inside, or a sequence was longer than the batch's max_len."""
         _on_device(self.device.index)
         wb.wb_kv_attend_check(self.pointer, _stream(self.device.index))
 

@@ -158,3 +158,19 @@ def test_lengths_above_max_len_are_reported(dtype, new):
     assert bool((out[:3] == 0).all()) and bool(lse[:3].isneginf().all())
     with pytest.raises(wb.WbError, match="WB_ERR_INVALID_ARG"):
         ws.check()
+
+
+def test_a_report_is_given_once():
+    """The check takes the report away: the workspace serves the next call, and says so."""
+    c = Case([50], [2], 4, 2, 64, 16, torch.bfloat16, seed=62)
+    k, v = c.rows()
+    c.cache.write(c.whole, k, v)
+    q = c.queries()
+    short = rollout.KvBatch(c.batch.page_table, c.batch.new_start, c.batch.kv_len, n_tokens=2, max_new=2, max_len=49)
+    ws = rollout.AttendWorkspace(c.cache, 4, 1)
+    c.cache.attend(short, q, workspace=ws)
+    with pytest.raises(wb.WbError):
+        ws.check()
+    out, lse = c.cache.attend(c.batch, q, workspace=ws)
+    ws.check()
+    c.check_attend(q, out, lse)
