@@ -26,18 +26,20 @@ __device__ __forceinline__ float prob(const uint16_t* p, uint64_t i) { return __
 __device__ __forceinline__ uint64_t key_max(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 
-// The best of a thread so far: its key (score bits above the complemented index; scores are positive, so their bits order as they
-// do, and a larger complement is a lower index), and the score a little lowered: a candidate whose weight does not exceed that
-// times its race variate cannot win, and is spared the division (all but about ln n of n candidates).
+// The best of a thread so far: its key (score bits above the complemented index; scores are not negative, so their bits order as
+// they do, and a larger complement is a lower index), and the score itself.  A candidate whose weight is below the rounded product
+// of that and its race variate is spared the division (all but about ln n of n are): the weight is then below the exact product
+// too, because it is a number that the product could have been rounded to, so its quotient is at most the score, and an equal one
+// of a later index does not win.  (A NaN product, of zero and infinity, spares nothing.)
 struct Best {
   uint64_t key = 0;                     // below every key: no weight is positive
   float bar = 0.f;
   __device__ __forceinline__ void offer(float w, float e, uint32_t v) {
-    if (!(w > 0.f) || !(w > bar * e)) return;
+    if (!(w > 0.f) || w < bar * e) return;
     const float score = __fdiv_rn(w, e);
     if (!(score >= 0.f)) return;        // a NaN or negative race variate takes no part
     key = key_max(key, (uint64_t)__float_as_uint(score) << 32 | (uint32_t)~v);
-    bar = fmaxf(bar, score * 0.999999f);
+    bar = fmaxf(bar, score);
   }
 };
 

@@ -174,3 +174,41 @@ def test_a_report_is_given_once():
     out, lse = c.cache.attend(c.batch, q, workspace=ws)
     ws.check()
     c.check_attend(q, out, lse)
+
+
+def race_cases():
+    """Target rows and race variates where quotients are zero, subnormal or infinite: [n, vocab] each."""
+    rng = np.random.default_rng(77)
+    vocab, tiny = 700, np.float32(2.0 ** -149)
+    rows = []
+    p, e = np.zeros(vocab, np.float32), np.ones(vocab, np.float32)
+    p[300], e[300] = 1.0, np.inf                               # the only token that can be drawn has an infinite variate
+    rows.append((p, e))
+    p, e = np.zeros(vocab, np.float32), np.full(vocab, np.inf, np.float32)
+    p[[9, 40, 41]] = [0.25, 0.5, 0.25]                         # all of them: the lowest index
+    rows.append((p, e))
+    p, e = p.copy(), e.copy()
+    e[[9, 41]] = [np.nan, 3e38]                                # a NaN takes no part, a finite quotient beats zero
+    rows.append((p, e))
+    for k in range(12):                                        # weights of a few units of the smallest subnormal
+        p = (rng.integers(0, 4, vocab) * tiny).astype(np.float32)
+        rows.append((p, rng.exponential(size=vocab).astype(np.float32) * np.float32(0.1 if k % 2 else 1.0)))
+    for k in range(6):                                         # quotients that are equal, infinite or underflow
+        with np.errstate(over="ignore"):                       # (some weights are infinite)
+            p = (rng.integers(0, 3, vocab) * np.float32([1e-38, 1.0, 3e38][k % 3])).astype(np.float32)
+        rows.append((p, np.float32(2.0) ** rng.integers(-3, 4, vocab) * np.float32([1e30, 1.0, 1e-30][k // 2])))
+    return np.stack([r[0] for r in rows]), np.stack([r[1] for r in rows]).astype(np.float32)
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+def test_verify_races_at_the_ends_of_the_range(pad):
+    p, race = race_cases()
+    n, vocab = p.shape
+    for copies in (1, 8):                                      # few sequences (clusters of 16), many (8 and less)
+        pp, ee = np.tile(p, (copies, 1)), np.tile(race, (copies, 1))
+        wide = torch.zeros(n * copies, vocab + pad, device=DEV)
+        wide[:, :vocab] = torch.tensor(pp, device=DEV)
+        a, out = run_verify(wide[:, :vocab], None, [], [0] * (n * copies + 1), [], torch.tensor(ee, device=DEV), 0)
+        for b in range(n * copies):
+            _, want = orc.verify(pp[b:b + 1], None, [], [], ee[b], 0)
+            assert a[b] == 0 and np.array_equal(out[b], want), (b % n, out[b], want)
