@@ -120,6 +120,7 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   if (wb_status s = check_heads(out, batch->n_tokens, false)) return s;
   if (!n_heads || n_heads % kv->d.n_kv_heads || n_heads / kv->d.n_kv_heads > 64) return WB_ERR_INVALID_ARG;
   if (!(scale > 0.f) || !std::isfinite(scale) || window > 0x7FFFFFFFu) return WB_ERR_INVALID_ARG;
+  if ((uintptr_t)lse & 3u) return WB_ERR_INVALID_ARG;
   if (!workspace || ((uintptr_t)workspace & 255u) || workspace_bytes < wb_kv_attend_workspace_bytes(kv, n_heads, batch->n_seqs))
     return WB_ERR_INVALID_ARG;
   if (!batch->n_tokens || !batch->n_seqs) return WB_OK;

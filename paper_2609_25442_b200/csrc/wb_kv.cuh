@@ -60,6 +60,7 @@ inline wb_status check_batch(const wb_kv* kv, const wb_kv_batch* b) {
   if (!kv || !b || b->n_seqs > WB_KV_MAX_SEQS || (b->table_pitch && b->table_pitch < b->table_stride)) return WB_ERR_INVALID_ARG;
   if (b->n_tokens > 0x7FFFFFFFu || b->max_len > 0x7FFFFFFFu || b->max_new > b->n_tokens) return WB_ERR_INVALID_ARG;
   if (b->n_seqs && (!b->new_start || !b->kv_len || (b->table_stride && !b->page_table))) return WB_ERR_INVALID_ARG;
+  if (((uintptr_t)b->page_table | (uintptr_t)b->new_start | (uintptr_t)b->kv_len) & 3u) return WB_ERR_INVALID_ARG;
   // positions are 32-bit: a row of the table covers fewer than 2^31 of them
   if ((uint64_t)b->table_stride * kv->d.page_size > 0x7FFFFFFFull) return WB_ERR_INVALID_ARG;
   return on_kv_device(kv) ? WB_OK : WB_ERR_INVALID_ARG;

@@ -212,3 +212,21 @@ def test_verify_races_at_the_ends_of_the_range(pad):
         for b in range(n * copies):
             _, want = orc.verify(pp[b:b + 1], None, [], [], ee[b], 0)
             assert a[b] == 0 and np.array_equal(out[b], want), (b % n, out[b], want)
+
+
+@pytest.mark.parametrize("name", ["page_table", "new_start", "kv_len", "lse"])
+def test_misaligned_arrays_are_refused(name):
+    c = Case([20], [3], 2, 2, 64, 16, torch.bfloat16)
+    rows, q = torch.zeros(3, 2, 64, dtype=torch.bfloat16, device=DEV), c.queries()
+    ws, lse = rollout.AttendWorkspace(c.cache, 2, 1), torch.zeros(3, 2, device=DEV)
+    heads = lambda t: wb.wb_heads(t.data_ptr(), wb.WB_BF16, 0, t.stride(0), t.stride(1))
+    b = wb.wb_kv_batch.from_buffer_copy(c.batch.args)
+    if name != "lse":
+        setattr(b, name, getattr(b, name) + 2)
+    kv, calls = c.cache._kv, []
+    if name != "lse":
+        calls = [lambda: kv.write(b, heads(rows), heads(rows)), lambda: kv.read(b, heads(rows), heads(rows))]
+    calls.append(lambda: kv.attend(b, heads(q), 2, heads(torch.empty_like(rows)), lse.data_ptr() + (2 if name == "lse" else 0), 1.0, 0, ws.pointer, ws.bytes))
+    for f in calls:
+        with pytest.raises(wb.WbError, match="WB_ERR_INVALID_ARG"):
+            f()
