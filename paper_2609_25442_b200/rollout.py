@@ -37,6 +37,14 @@ def _require(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
+def _count(x: int, name: str) -> int:
+    """A number as the C ABI's 31 bits hold it (ctypes would cut it to them)."""
+    x = int(x)
+    if x >> 31:
+        raise ValueError(f"{name}: {x} is negative or 2^31 and more")
+    return x
+
+
 def _ints(t: torch.Tensor, name: str, device: torch.device) -> torch.Tensor:
     if t.dtype != torch.int32 or t.device != device:
         raise ValueError(f"{name}: an int32 tensor on {device} is needed")
@@ -76,7 +84,9 @@ class KvBatch:
                  max_new: Optional[int] = None, max_len: Optional[int] = None):
         dev = kv_len.device
         self.n_seqs = int(kv_len.shape[0])
-        self.n_tokens = int(n_tokens)
+        self.n_tokens = _count(n_tokens, "n_tokens")
+        max_new = self.n_tokens if max_new is None else min(_count(max_new, "max_new"), self.n_tokens)
+        max_len = None if max_len is None else _count(max_len, "max_len")
         _require(page_table.dim() == 2 and page_table.shape[0] == self.n_seqs and (page_table.stride(1) == 1 or page_table.shape[1] <= 1),
                  "page_table: [n_seqs, pages] with contiguous rows")
         _require(new_start.shape == (self.n_seqs + 1,) and kv_len.dim() == 1 and new_start.is_contiguous() and kv_len.is_contiguous(),
@@ -87,9 +97,8 @@ class KvBatch:
         self.device = dev
         most = int(page_table.shape[1]) if max_len is None else None
         self._max_len, self._table_pages = max_len, most
-        self.args = wb.wb_kv_batch(self.n_seqs, self.n_tokens, min(self.n_tokens if max_new is None else int(max_new), self.n_tokens),
-                                   0 if max_len is None else int(max_len), int(page_table.shape[1]),
-                                   page_table.stride(0) if self.n_seqs > 1 else 0,
+        self.args = wb.wb_kv_batch(self.n_seqs, self.n_tokens, max_new, max_len or 0, int(page_table.shape[1]),
+                                   _count(page_table.stride(0), "page_table's pitch") if self.n_seqs > 1 else 0,
                                    self.page_table.data_ptr(), self.new_start.data_ptr(), self.kv_len.data_ptr())
 
     def _for(self, cache: "KvCache") -> wb.wb_kv_batch:
@@ -97,7 +106,7 @@ class KvBatch:
             raise ValueError(f"batch on {self.device}, cache on {cache.device}")
         _on_device(cache._index)
         if self._max_len is None:                       # the table's capacity bounds every length
-            self.args.max_len = self._table_pages * cache.page_size
+            self.args.max_len = _count(self._table_pages * cache.page_size, "the table's positions")
         return self.args
 
 
@@ -169,6 +178,8 @@ class KvCache:
             raise ValueError("q: [n_tokens, n_heads, head_dim]")
         if workspace.device != self.device:
             raise ValueError(f"workspace on {workspace.device}, cache on {self.device}")
+        if window >> 31:
+            raise ValueError(f"window: {window} is negative or 2^31 and more")
         n, h = batch.n_tokens, q.shape[1]
         a = _heads(q, "q", n, h, self.head_dim, self.device)
         if out is None:

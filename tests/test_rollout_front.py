@@ -161,3 +161,18 @@ def test_calls_from_another_current_device_are_refused(cache, verified, monkeypa
         with pytest.raises(ValueError, match="current device"):
             f()
     assert not cache._kv.calls and not verified and not checked
+
+
+@pytest.mark.parametrize("kw", [dict(max_len=-1), dict(max_len=1 << 31), dict(max_len=(1 << 32) + 5), dict(max_new=-1), dict(max_new=(1 << 32) + 1),
+                                dict(n_tokens=-1), dict(n_tokens=(1 << 32) + 2)])
+def test_numbers_of_a_batch_that_32_bits_do_not_hold_are_refused(kw):
+    """(The C struct would hold them modulo 2^32.)"""
+    with pytest.raises(ValueError, match=list(kw)[0]):
+        gpu_batch(**kw)
+
+
+@pytest.mark.parametrize("window", [-1, 1 << 31, 1 << 32, (1 << 32) + 5])
+def test_windows_that_32_bits_do_not_hold_are_refused(cache, window):
+    with pytest.raises(ValueError, match="window"):
+        all_calls(cache, gpu_batch(), window=window)[2]()
+    assert not cache._kv.calls
