@@ -83,13 +83,14 @@ class KvBatch:
     def __init__(self, page_table: torch.Tensor, new_start: torch.Tensor, kv_len: torch.Tensor, *, n_tokens: int,
                  max_new: Optional[int] = None, max_len: Optional[int] = None):
         dev = kv_len.device
+        _require(kv_len.dim() == 1, "kv_len: [n_seqs]")
         self.n_seqs = int(kv_len.shape[0])
         self.n_tokens = _count(n_tokens, "n_tokens")
         max_new = self.n_tokens if max_new is None else min(_count(max_new, "max_new"), self.n_tokens)
         max_len = None if max_len is None else _count(max_len, "max_len")
         _require(page_table.dim() == 2 and page_table.shape[0] == self.n_seqs and (page_table.stride(1) == 1 or page_table.shape[1] <= 1),
                  "page_table: [n_seqs, pages] with contiguous rows")
-        _require(new_start.shape == (self.n_seqs + 1,) and kv_len.dim() == 1 and new_start.is_contiguous() and kv_len.is_contiguous(),
+        _require(new_start.shape == (self.n_seqs + 1,) and new_start.is_contiguous() and kv_len.is_contiguous(),
                  "new_start: [n_seqs + 1], kv_len: [n_seqs], contiguous")
         _require(self.n_seqs <= 1 or page_table.shape[1] == 0 or page_table.stride(0) >= page_table.shape[1], "page_table: rows overlap")
         self.page_table = _ints(page_table, "page_table", dev)
@@ -221,8 +222,10 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
     uniform [n_drafts], draft_start [n_seqs + 1], race [n_seqs, vocab] (Exp(1) variates).  Returns (accepted [n_seqs],
     tokens [n_seqs, max_drafts + 1], -1 beyond the drawn token), int32.  Rows may be one row broadcast with expand."""
     dev = target.device
+    if target.dim() != 2 or draft_start.dim() != 1 or draft_tokens.dim() != 1:
+        raise ValueError("target: two dimensions, draft_start and draft_tokens: one")
     n, vocab, total = draft_start.shape[0] - 1, target.shape[1], draft_tokens.shape[0]
-    if not target.is_cuda or target.dim() != 2 or n < 0 or target.shape[0] != total + n or target.stride(1) != 1:
+    if not target.is_cuda or n < 0 or target.shape[0] != total + n or target.stride(1) != 1:
         raise ValueError("target: [n_drafts + n_seqs, vocab] with contiguous rows on a CUDA device")
     _on_device(dev.index)
     if target.dtype not in (torch.float32, torch.bfloat16):

@@ -176,3 +176,20 @@ def test_windows_that_32_bits_do_not_hold_are_refused(cache, window):
     with pytest.raises(ValueError, match="window"):
         all_calls(cache, gpu_batch(), window=window)[2]()
     assert not cache._kv.calls
+
+
+@pytest.mark.parametrize("kw", [dict(draft_tokens=torch.zeros(4, 2, dtype=torch.int32)), dict(draft_start=torch.zeros(3, 2, dtype=torch.int32)),
+                                dict(draft_start=torch.tensor(0, dtype=torch.int32)), dict(draft_tokens=torch.tensor(0, dtype=torch.int32)),
+                                dict(target=torch.rand(100)), dict(draft_start=torch.zeros(0, dtype=torch.int32))])
+def test_verify_refuses_shapes(verified, kw):
+    """(Of a table of tokens the kernel would read the first entries as if they were the column.)"""
+    with pytest.raises(ValueError):
+        rollout.verify_drafts(**drafts_of(**kw), max_drafts=2)
+    assert not verified
+
+
+def test_batch_refuses_shapes():
+    for kw in (dict(kv_len=gpu(torch.tensor(5, dtype=torch.int32))), dict(kv_len=gpu(torch.full((2, 1), 5, dtype=torch.int32))),
+               dict(new_start=gpu(torch.zeros(3, 1, dtype=torch.int32)))):
+        with pytest.raises(ValueError):
+            gpu_batch(**kw)
