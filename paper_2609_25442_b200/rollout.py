@@ -57,8 +57,12 @@ def _heads(t: torch.Tensor, name: str, n_tokens: int, heads: int, dim: int, devi
     if t.shape != (n_tokens, heads, dim) or t.device != device or dtype is None:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {(n_tokens, heads, dim)} on {device}")
     st, sh, se = t.stride()
-    if se != 1 or st < 0 or sh < 0:
+    if se != 1:
         raise ValueError(f"{name}: rows must be contiguous")
+    if n_tokens == 1:              # a stride that leads nowhere: the C ABI wants it aligned all the same
+        st = heads * dim
+    if heads == 1:
+        sh = dim
     return wb.wb_heads(t.data_ptr(), dtype, 0, st, sh)
 
 
@@ -116,7 +120,9 @@ class KvCache:
     scales [n_pages, n_kv_heads, page_size].  The tensors stay the caller's; the cache keeps references to them."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
-        _require(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device,
+        # the stride of a dimension of one leads nowhere
+        step = [tuple(st if n > 1 else 0 for n, st in zip(t.shape, t.stride())) for t in (k, v)]
+        _require(k.dim() == 4 and k.shape == v.shape and step[0] == step[1] and k.dtype == v.dtype and k.device == v.device,
                  "k and v: the same shape [n_pages, n_kv_heads, page_size, head_dim], strides, type and device")
         _require(k.is_cuda, "the cache needs a CUDA device (sm_100a)")
         _on_device(k.device.index)
@@ -134,7 +140,7 @@ class KvCache:
         # new_empty of these allocates results without looking a device and a type up again
         self._like = {t: torch.empty(0, dtype=t, device=k.device) for t in (torch.float32, torch.bfloat16)}
         self._kv = wb.Kv(wb.wb_kv_desc(_DTYPE[k.dtype], self.n_kv_heads, self.head_dim, self.page_size, self.n_pages,
-                                       k.stride(0), k.stride(1), k.data_ptr(), v.data_ptr(),
+                                       step[0][0], step[0][1], k.data_ptr(), v.data_ptr(),
                                        k_scale.data_ptr() if k_scale is not None else None,
                                        v_scale.data_ptr() if v_scale is not None else None))
 
@@ -225,16 +231,16 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
     if target.dim() != 2 or draft_start.dim() != 1 or draft_tokens.dim() != 1:
         raise ValueError("target: two dimensions, draft_start and draft_tokens: one")
     n, vocab, total = draft_start.shape[0] - 1, target.shape[1], draft_tokens.shape[0]
-    if not target.is_cuda or n < 0 or target.shape[0] != total + n or target.stride(1) != 1:
+    if not target.is_cuda or n < 0 or target.shape[0] != total + n or (target.stride(1) != 1 and vocab != 1):
         raise ValueError("target: [n_drafts + n_seqs, vocab] with contiguous rows on a CUDA device")
     _on_device(dev.index)
     if target.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError(f"probabilities of {target.dtype}: float32 or bfloat16")
-    if draft is not None and (draft.shape != (total, vocab) or draft.dtype != target.dtype or draft.device != dev or draft.stride(1) != 1):
+    if draft is not None and (draft.shape != (total, vocab) or draft.dtype != target.dtype or draft.device != dev or (draft.stride(1) != 1 and vocab != 1)):
         raise ValueError("draft: [n_drafts, vocab] of the target's type")
     if uniform.shape != (total,) or uniform.dtype != torch.float32 or uniform.device != dev or not uniform.is_contiguous():
         raise ValueError("uniform: fp32 [n_drafts]")
-    if race.shape != (n, vocab) or race.dtype != torch.float32 or race.device != dev or race.stride(1) != 1:
+    if race.shape != (n, vocab) or race.dtype != torch.float32 or race.device != dev or (race.stride(1) != 1 and vocab != 1):
         raise ValueError("race: fp32 [n_seqs, vocab]")
     if not draft_tokens.is_contiguous() or not draft_start.is_contiguous():
         raise ValueError("draft_tokens, draft_start: contiguous")

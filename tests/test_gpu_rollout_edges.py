@@ -230,3 +230,20 @@ def test_misaligned_arrays_are_refused(name):
     for f in calls:
         with pytest.raises(wb.WbError, match="WB_ERR_INVALID_ARG"):
             f()
+
+
+def test_cache_of_one_page_and_one_head():
+    """The strides of dimensions of one lead nowhere, and may be any."""
+    x = [torch.zeros(64 * 64, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    cache = rollout.KvCache(x[0].as_strided((1, 1, 64, 64), (7, 3, 64, 1)), x[1].as_strided((1, 1, 64, 64), (1, 5, 64, 1)))
+    i32 = dict(dtype=torch.int32, device=DEV)
+    b = rollout.KvBatch(torch.zeros(1, 1, **i32), torch.tensor([0, 50], **i32), torch.tensor([50], **i32), n_tokens=50)
+    k, v = (torch.randn(50, 1, 64, device=DEV).bfloat16() for _ in range(2))
+    cache.write(b, k, v)
+    assert torch.equal(x[0][:3200], k.flatten()) and torch.equal(x[1][:3200], v.flatten())
+    rk, rv = cache.read(b)
+    assert torch.equal(rk, k) and torch.equal(rv, v)
+    q = torch.randn(50, 4, 64, device=DEV).bfloat16()
+    out, _ = cache.attend(b, q, workspace=rollout.AttendWorkspace(cache, 4, 1))
+    want, _, mag = orc.attend(q.float().cpu().numpy(), *(y.float().transpose(0, 1).cpu().numpy() for y in (k, v)), 50, 0.125)
+    assert (np.abs(out.float().cpu().numpy() - want) <= out_bound(want, mag)).all()

@@ -193,3 +193,24 @@ def test_batch_refuses_shapes():
                dict(new_start=gpu(torch.zeros(3, 1, dtype=torch.int32)))):
         with pytest.raises(ValueError):
             gpu_batch(**kw)
+
+
+def test_the_pitch_of_a_dimension_of_one_does_not_matter(cache, verified):
+    """One token, or one head, cut out of rows of any width: there is no second one that its stride would lead to."""
+    k = gpu(torch.zeros(1, 2, 64, dtype=torch.bfloat16)).as_strided((1, 2, 64), (131, 64, 1))
+    batch = gpu_batch(n=1)
+    cache.write(batch, k, k)
+    cache.read(batch, out=(k, k))
+    q = gpu(torch.zeros(1, 4, 64, dtype=torch.bfloat16)).as_strided((1, 4, 64), (3, 64, 1))
+    cache.attend(batch, q, workspace=workspace(), out=q)
+    for _, args in cache._kv.calls:
+        for h in args:
+            if isinstance(h, rollout.wb.wb_heads):
+                assert h.token_stride % 8 == 0 and h.head_stride == 64
+    cache.n_kv_heads = 1
+    one = gpu(torch.zeros(3, 64, dtype=torch.bfloat16)).as_strided((3, 1, 64), (64, 5, 1))
+    cache.write(gpu_batch(n=3), one, one)
+    assert cache._kv.calls[-1][1][1].head_stride % 8 == 0 and cache._kv.calls[-1][1][1].token_stride == 64
+    # one token in the vocabulary
+    rollout.verify_drafts(**drafts_of(vocab=1, target=torch.rand(6).as_strided((6, 1), (1, 9))), max_drafts=2)
+    assert verified[-1].target_stride == 1
