@@ -1,6 +1,7 @@
 """A rollout engine's step on torch tensors: the paged key/value cache (written, read back, attended over)
 and the verification of drafted tokens.  The work is done by libwb.so; this module checks tensors,
 allocates results and passes torch's current stream.  All tensors are on the current device.
+There are no backward passes, and tensors that want gradients are refused.
 
     cache = KvCache.empty(n_pages, n_kv_heads, page_size, head_dim, dtype=torch.float8_e4m3fn)
     batch = KvBatch(page_table, new_start, kv_len, n_tokens=T, max_new=..., max_len=...)
@@ -51,11 +52,20 @@ def _ints(t: torch.Tensor, name: str, device: torch.device) -> torch.Tensor:
     return t
 
 
+_grad_enabled = torch.is_grad_enabled
+
+
+def _no_gradient(t: torch.Tensor, name: str) -> None:
+    if t.requires_grad and _grad_enabled():
+        raise ValueError(f"{name} wants a gradient, and there is no backward pass: use torch.no_grad() or detach()")
+
+
 def _heads(t: torch.Tensor, name: str, n_tokens: int, heads: int, dim: int, device: torch.device) -> wb.wb_heads:
     """A step's tensor [tokens, heads, dim] with contiguous rows, as the C ABI takes it."""
     dtype = _DTYPE.get(t.dtype)
     if t.shape != (n_tokens, heads, dim) or t.device != device or dtype is None:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {(n_tokens, heads, dim)} on {device}")
+    _no_gradient(t, name)
     st, sh, se = t.stride()
     if se != 1:
         raise ValueError(f"{name}: rows must be contiguous")
@@ -234,6 +244,10 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
     if not target.is_cuda or n < 0 or target.shape[0] != total + n or (target.stride(1) != 1 and vocab != 1):
         raise ValueError("target: [n_drafts + n_seqs, vocab] with contiguous rows on a CUDA device")
     _on_device(dev.index)
+    if _grad_enabled():
+        for t, name in ((target, "target"), (draft, "draft"), (race, "race"), (uniform, "uniform")):
+            if t is not None:
+                _no_gradient(t, name)
     if target.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError(f"probabilities of {target.dtype}: float32 or bfloat16")
     if draft is not None and (draft.shape != (total, vocab) or draft.dtype != target.dtype or draft.device != dev or (draft.stride(1) != 1 and vocab != 1)):

@@ -214,3 +214,22 @@ def test_the_pitch_of_a_dimension_of_one_does_not_matter(cache, verified):
     # one token in the vocabulary
     rollout.verify_drafts(**drafts_of(vocab=1, target=torch.rand(6).as_strided((6, 1), (1, 9))), max_drafts=2)
     assert verified[-1].target_stride == 1
+
+
+def test_tensors_that_want_gradients_are_refused(cache, verified):
+    """None of the operators has a backward pass: a result without a graph would drop the gradient without a word."""
+    batch = gpu_batch()
+    rows = lambda heads: gpu(torch.zeros(2, heads, 64, dtype=torch.bfloat16)).requires_grad_()
+    k, q = rows(2), rows(4)
+    calls = [lambda: cache.write(batch, k, k.detach()), lambda: cache.write(batch, k.detach(), k), lambda: cache.attend(batch, q, workspace=workspace()),
+             lambda: cache.attend(batch, q.detach(), workspace=workspace(), out=q), lambda: cache.read(batch, out=(k.detach(), k))]
+    drafts = drafts_of()
+    calls += [lambda n=n: rollout.verify_drafts(**{**drafts, n: drafts[n].clone().requires_grad_()}, max_drafts=2) for n in ("target", "draft", "race", "uniform")]
+    for f in calls:
+        with pytest.raises(ValueError, match="gradient"):
+            f()
+    assert not cache._kv.calls and not verified
+    with torch.no_grad():
+        for f in calls:
+            f()
+    assert len(cache._kv.calls) == 5 and len(verified) == 4
