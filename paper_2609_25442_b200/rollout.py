@@ -65,7 +65,8 @@ def _heads(t: torch.Tensor, name: str, n_tokens: int, heads: int, dim: int, devi
     dtype = _DTYPE.get(t.dtype)
     if t.shape != (n_tokens, heads, dim) or t.device != device or dtype is None:
         raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}, expected {(n_tokens, heads, dim)} on {device}")
-    _no_gradient(t, name)
+    if t.requires_grad:
+        _no_gradient(t, name)
     st, sh, se = t.stride()
     if se != 1:
         raise ValueError(f"{name}: rows must be contiguous")
@@ -76,14 +77,16 @@ def _heads(t: torch.Tensor, name: str, n_tokens: int, heads: int, dim: int, devi
     return wb.wb_heads(t.data_ptr(), dtype, 0, st, sh)
 
 
-def _pitch(t: torch.Tensor, name: str) -> int:
+def _pitch(t: torch.Tensor, n: int, name: str) -> int:
     """Elements from a row of a [rows, n] tensor to the next; 0 where all rows are one (a broadcast)."""
-    step, n = t.stride(0), t.shape[1]
+    step = t.stride(0)
+    if step >= n:
+        return step
     if t.shape[0] <= 1:
         return n                              # says nothing for a single row
-    if 0 < step < n:
+    if step:
         raise ValueError(f"{name}: rows overlap")
-    return step
+    return 0
 
 
 class KvBatch:
@@ -119,7 +122,8 @@ class KvBatch:
     def _for(self, cache: "KvCache") -> wb.wb_kv_batch:
         if self.device != cache.device:
             raise ValueError(f"batch on {self.device}, cache on {cache.device}")
-        _on_device(cache._index)
+        if _current_device() != cache._index:
+            _on_device(cache._index)
         if self._max_len is None:                       # the table's capacity bounds every length
             self.args.max_len = _count(self._table_pages * cache.page_size, "the table's positions")
         return self.args
@@ -264,8 +268,8 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
     tokens = draft_start.new_empty((n, max_drafts + 1))
     none = draft is None or total == 0
     wb.wb_verify_drafts(wb.wb_verify_args(n, vocab, max_drafts, _DTYPE[target.dtype], total, 0, target.data_ptr(),
-                                          None if none else draft.data_ptr(), _pitch(target, "target"),
-                                          0 if none else _pitch(draft, "draft"), _pitch(race, "race"),
+                                          None if none else draft.data_ptr(), _pitch(target, vocab, "target"),
+                                          0 if none else _pitch(draft, vocab, "draft"), _pitch(race, vocab, "race"),
                                           draft_tokens.data_ptr(), draft_start.data_ptr(), uniform.data_ptr(), race.data_ptr(),
                                           accepted.data_ptr(), tokens.data_ptr()), _stream(dev.index))
     return accepted, tokens
