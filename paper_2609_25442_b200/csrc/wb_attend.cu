@@ -24,13 +24,11 @@ constexpr uint32_t kMaxRowBlocks = 3 * kNumSMs;
 
 // A kernel's dynamic shared memory is raised once per device to the most that it may ask for; with `regs`, the kernel has to have been
 // compiled to that many registers and no static shared memory.  Returns an error only where it cannot run at all.
-template <typename K> cudaError_t prepare_kernel(K kernel, uint32_t most, int regs, std::atomic<uint64_t>& done) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
+template <typename K> cudaError_t prepare_kernel(K kernel, uint32_t most, int regs, int dev, std::atomic<uint64_t>& done) {
   const uint64_t bit = dev < 64 ? 1ull << dev : 0;
   if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
   cudaFuncAttributes f;
+  cudaError_t e;
   if ((e = cudaFuncGetAttributes(&f, kernel)) != cudaSuccess) return e;
   if (regs && (f.numRegs != regs || f.sharedSizeBytes != 0)) return cudaErrorInvalidConfiguration;
   most = std::min<uint32_t>(most, 232448 - (uint32_t)f.sharedSizeBytes);
@@ -54,7 +52,7 @@ cudaError_t launch_join(void (*kernel)(AttendArgs), dim3 grid, uint32_t threads,
 }
 
 template <int D, bool Q, int NT>
-cudaError_t launch_rows(const AttendArgs& a, cudaStream_t stream) {
+cudaError_t launch_rows(const AttendArgs& a, int dev, cudaStream_t stream) {
   using C = RowsCfg<D, Q, NT>;
   const size_t smem = C::smem_bytes(a.b.n_seqs);
   auto kernel = wb_attend_rows_kernel<D, Q, NT>;
@@ -62,7 +60,7 @@ cudaError_t launch_rows(const AttendArgs& a, cudaStream_t stream) {
   // prefix sums takes the place of a block)
   const uint32_t per_sm = std::min<uint32_t>(C::kBlocksPerSm, (uint32_t)(kSmemPerSm / (smem + 2048)));
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = prepare_kernel(kernel, 232448, 0, done);
+  cudaError_t e = prepare_kernel(kernel, 232448, 0, dev, done);
   if (e != cudaSuccess) return e;
   const uint32_t grid = kNumSMs * std::max(1u, per_sm);
   kernel<<<grid, C::kThreads, smem, stream>>>(a);
@@ -71,10 +69,10 @@ cudaError_t launch_rows(const AttendArgs& a, cudaStream_t stream) {
 }
 
 template <int D, bool Q>
-cudaError_t launch_rows_of(uint32_t rows, const AttendArgs& a, cudaStream_t stream) {
-  if (rows <= 8) return launch_rows<D, Q, 1>(a, stream);
-  if (rows <= 16) return launch_rows<D, Q, 2>(a, stream);
-  return launch_rows<D, Q, 4>(a, stream);
+cudaError_t launch_rows_of(uint32_t rows, const AttendArgs& a, int dev, cudaStream_t stream) {
+  if (rows <= 8) return launch_rows<D, Q, 1>(a, dev, stream);
+  if (rows <= 16) return launch_rows<D, Q, 2>(a, dev, stream);
+  return launch_rows<D, Q, 4>(a, dev, stream);
 }
 
 template <int D, bool Q>
@@ -83,7 +81,7 @@ cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_r
   auto kernel = wb_attend_tiles_kernel<D, Q>;
   // the softmax warps wait for registers that the others give back: the launch has to have them
   static std::atomic<uint64_t> done{0};
-  cudaError_t e = prepare_kernel(kernel, C::kSmemBytes, C::kLaunchRegs, done);
+  cudaError_t e = prepare_kernel(kernel, C::kSmemBytes, C::kLaunchRegs, kv->device, done);
   if (e != cudaSuccess) return e;
   for (uint32_t s0 = 0; s0 < all.b.n_seqs; s0 += C::kMaxSeqs) {
     AttendArgs a = all;
@@ -150,8 +148,8 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   cudaError_t err = cudaSuccess;
   if (rows <= kMaxRows || batch->n_seqs > 1) {
     const uint32_t r = (uint32_t)std::min<uint64_t>(rows, kMaxRows);
-    if (kv->d.head_dim == 128) err = e ? launch_rows_of<128, true>(r, a, st) : launch_rows_of<128, false>(r, a, st);
-    else err = e ? launch_rows_of<64, true>(r, a, st) : launch_rows_of<64, false>(r, a, st);
+    if (kv->d.head_dim == 128) err = e ? launch_rows_of<128, true>(r, a, kv->device, st) : launch_rows_of<128, false>(r, a, kv->device, st);
+    else err = e ? launch_rows_of<64, true>(r, a, kv->device, st) : launch_rows_of<64, false>(r, a, kv->device, st);
   }
   if (err == cudaSuccess && rows > kMaxRows) {
     const uint32_t skip = batch->n_seqs > 1 ? kMaxRows : 0;

@@ -112,7 +112,7 @@ class KvBatch:
         _require(self.n_seqs <= 1 or page_table.shape[1] == 0 or page_table.stride(0) >= page_table.shape[1], "page_table: rows overlap")
         self.page_table = _ints(page_table, "page_table", dev)
         self.new_start, self.kv_len = _ints(new_start, "new_start", dev), _ints(kv_len, "kv_len", dev)
-        self.device = dev
+        self.device, self._index = dev, dev.index if dev.type == "cuda" else None
         most = int(page_table.shape[1]) if max_len is None else None
         self._max_len, self._table_pages = max_len, most
         self.args = wb.wb_kv_batch(self.n_seqs, self.n_tokens, max_new, max_len or 0, int(page_table.shape[1]),
@@ -120,7 +120,7 @@ class KvBatch:
                                    self.page_table.data_ptr(), self.new_start.data_ptr(), self.kv_len.data_ptr())
 
     def _for(self, cache: "KvCache") -> wb.wb_kv_batch:
-        if self.device != cache.device:
+        if self._index != cache._index:
             raise ValueError(f"batch on {self.device}, cache on {cache.device}")
         if _current_device() != cache._index:
             _on_device(cache._index)
@@ -197,7 +197,7 @@ class KvCache:
         workspace.check() has passed after them; rows that no sequence holds are left as they are."""
         if q.dim() != 3:
             raise ValueError("q: [n_tokens, n_heads, head_dim]")
-        if workspace.device != self.device:
+        if workspace.device is not self.device and workspace.device != self.device:
             raise ValueError(f"workspace on {workspace.device}, cache on {self.device}")
         if window >> 31:
             raise ValueError(f"window: {window} is negative or 2^31 and more")
