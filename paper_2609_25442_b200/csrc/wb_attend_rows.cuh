@@ -27,14 +27,13 @@
 
 namespace wbi {
 
-constexpr uint32_t kSmemPerSm = 233472, kSmemPerBlock = 232448;
+constexpr uint32_t kSmemPerSm = 233472;
 
 template <int D, bool Q, int NT>
 struct RowsCfg {
   static constexpr uint32_t kElem = Q ? 1 : 2;
   static constexpr uint32_t kRowBytes = D * kElem;
   static constexpr uint32_t kSpan = kRowBytes < 128 ? kRowBytes : 128;       // bytes of a row in one box
-  static constexpr uint32_t kSpans = kRowBytes / kSpan;
   static constexpr uint32_t kPartBytes = 16 * kRowBytes;                     // a warp's keys of a tile, and as much of values
   static constexpr uint32_t kSlotBytes = 2 * kPartBytes;
   static constexpr uint32_t kScaleBytes = Q ? 128 : 0;                       // 16 scales of keys and of values

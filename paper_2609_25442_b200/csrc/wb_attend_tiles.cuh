@@ -167,12 +167,9 @@ __device__ __forceinline__ uint32_t row_blocks(const KvSeq& q, uint32_t group, u
 // not more than kSnap tiles away: joining a cut item costs more than so many tiles.  So an item [i0, i1) is cut at the multiples
 // of `per` that lie more than kSnap tiles inside.
 constexpr int32_t kSnap = 2;
-struct Cuts {
-  int32_t first, n;        // the block that holds the item's first tile, number of cuts
-};
-__device__ __forceinline__ Cuts cuts_of(int32_t i0, int32_t i1, int32_t per) {
+__device__ __forceinline__ int32_t cuts_of(int32_t i0, int32_t i1, int32_t per) {
   const int32_t lo = (i0 + kItemCost + kSnap + per) / per, hi = (i1 - kSnap - 1) / per;    // multiples in (i0 + kItemCost + kSnap, i1 - kSnap)
-  return Cuts{lo - 1, max(0, hi - lo + 1)};
+  return max(0, hi - lo + 1);
 }
 
 // Where a block is in the line of tiles; every warp walks it alike.
@@ -613,7 +610,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           ++is;
           tc_after();
           const bool odd = misc[8 + item % 8] != 0;
-          const Cuts cuts = cuts_of(w.item0, item1, per);
+          const int32_t cuts = cuts_of(w.item0, item1, per);
           char* dst = a.out + (uint64_t)x0.tok * a.o_token + x0.head * a.o_head;
           float* part = a.partials + (size_t)(2 * blockIdx.x + (w.item0 >= begin ? 1 : 0)) * C::kPartFloats + i * (D * 128 + 256) + row;
           const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
@@ -630,7 +627,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
 #pragma unroll
               for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(y[e]);
             }
-            if (cuts.n == 0) {
+            if (cuts == 0) {
               if (x0.in)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -645,13 +642,13 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               for (int e = 0; e < 32; ++e) part[(c + e) * 128] = __uint_as_float(o[e]);
             }
           }
-          if (cuts.n == 0) {
+          if (cuts == 0) {
             if (x0.in && a.lse)
               a.lse[(uint64_t)x0.tok * a.n_heads + x0.head] = l == 0.f ? -INFINITY : (ref * c2 + log2f(l)) * kLn2;
           } else {
             part[D * 128] = l == 0.f ? -INFINITY : ref * c2;
             part[D * 128 + 128] = l;
-            if (tid == 0 && w.item0 >= begin) *cut_item = CutItem{(uint32_t)cuts.n + 1, w.s, w.h, w.rb};
+            if (tid == 0 && w.item0 >= begin) *cut_item = CutItem{(uint32_t)cuts + 1, w.s, w.h, w.rb};
           }
         }
         w = w2;

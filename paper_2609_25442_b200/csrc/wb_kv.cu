@@ -29,19 +29,7 @@ Rows rows_of(const wb_heads* h) {
   return Rows{(char*)h->data, h->token_stride * e, h->head_stride * e};
 }
 
-// Eight elements of a row, the unit of a lane: 16 bytes of bf16, 32 of fp32, 8 codes.
-template <bool F32>
-__device__ __forceinline__ void load8(const char* p, float* x) {
-  if (F32) {
-    const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  } else {
-    const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
-  }
-}
+// Eight elements of a row, the unit of a lane: 16 bytes of bf16, 32 of fp32.
 template <bool F32>
 __device__ __forceinline__ void store8(char* p, const float* x) {
   if (F32) {
