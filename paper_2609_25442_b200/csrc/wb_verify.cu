@@ -168,40 +168,61 @@ __global__ void __launch_bounds__(kVerifyThreads, 1024 / kVerifyThreads) wb_veri
   }
 }
 
-template <typename T, uint32_t kVerifyThreads>
-wb_status launch_verify(const wb_verify_args& a, uint32_t size, cudaStream_t stream) {
-  auto kernel = wb_verify_kernel<T, kVerifyThreads>;
-  if (size > 8) {
-    static std::atomic<uint64_t> allowed{0};      // a bit per device
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
-    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-    if (!(allowed.load(std::memory_order_acquire) & bit)) {
-      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
-      allowed.fetch_or(bit, std::memory_order_release);
-    }
-  }
+cudaLaunchConfig_t config_of(uint32_t n_seqs, uint32_t threads, uint32_t size, cudaLaunchAttribute* at, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(a.n_seqs * size);
-  cfg.blockDim = dim3(kVerifyThreads);
+  cfg.gridDim = dim3(n_seqs * size);
+  cfg.blockDim = dim3(threads);
   cfg.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = size;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  at->id = cudaLaunchAttributeClusterDimension;
+  at->val.clusterDim.x = size;
+  at->val.clusterDim.y = at->val.clusterDim.z = 1;
   cfg.attrs = at;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kernel, a) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
+  return cfg;
+}
+
+// How many clusters of `size` blocks fit on the device at once: fewer than its places for blocks divided by size, because a
+// cluster lies within one group of SMs.  Asked for once.
+template <typename T, uint32_t kVerifyThreads>
+uint32_t resident_clusters(int dev, uint32_t size) {
+  static std::atomic<int32_t> known[64][17];      // plus one
+  const bool keep = (uint32_t)dev < 64;
+  if (const int32_t n = keep ? known[dev][size].load(std::memory_order_acquire) : 0) return (uint32_t)(n - 1);
+  auto kernel = wb_verify_kernel<T, kVerifyThreads>;
+  cudaLaunchAttribute at[1];
+  const cudaLaunchConfig_t cfg = config_of(1, kVerifyThreads, size, at, nullptr);
+  int n = 0;
+  if ((size > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
+      cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();
+    n = 0;
+  }
+  if (keep) known[dev][size].store(n + 1, std::memory_order_release);
+  return (uint32_t)n;
+}
+
+template <typename T, uint32_t kVerifyThreads>
+wb_status launch_verify(const wb_verify_args& a, uint32_t size, cudaStream_t stream) {
+  cudaLaunchAttribute at[1];
+  const cudaLaunchConfig_t cfg = config_of(a.n_seqs, kVerifyThreads, size, at, stream);
+  if (cudaLaunchKernelEx(&cfg, wb_verify_kernel<T, kVerifyThreads>, a) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
   return WB_OK;
 }
 
-// Up to 18 sequences get 16 blocks of 512 threads each (not a portable cluster size, but every B200's): 7.9 us for one sequence of
-// 151936, where 256 threads take 8.5.  More get as many blocks of 256 threads, at most 8, as fit at once, four on an SM: 192
-// sequences of 128256 take 45 us with 2 blocks each, 51 with 4, and 57 with 3, which leave holes in the groups of SMs.
+// A sequence gets as many blocks as let all sequences run at once: 16 of 512 threads (not a portable cluster size, but every
+// B200's), 8 of 512, then 8 to 1 of 256.  One size too large and a second wave of clusters waits for the first; both sides, bf16
+// rows of 128256: 14 | 15 sequences with 16 x 512 take 16.4 | 20.5 us, the latter with 8 x 512 16.4; 32 | 36 with 8 x 512 18.5 | 26.6, the latter
+// with 8 x 256 22.5; 68 | 72 with 8 25.5 | 34.8, with 7 26.6 | 26.6; 75 | 84 with 7 28.7 | 38.9, with 6 28.7 | 30.7; 90 | 98 with 6 30.7 | 44.0, with 5
+// 32.8 | 32.8; 110 | 118 with 5 33.1 | 49.2, with 4 35.8 | 36.9; 130 | 148 with 4 37.8 | 54.2, with 3 41.0 | 42.0; 180 | 192 with 3 45.1 | 65.5, with 2
+// 53.2 | 53.2.  (Each with the drafts' and the race's rows out of the caches.)
 template <typename T> wb_status launch_verify_of(const wb_verify_args& a, cudaStream_t stream) {
-  const uint32_t fit = kNumSMs * 4 / std::min<uint32_t>(a.n_seqs, kNumSMs * 4);
-  if (fit >= 32) return launch_verify<T, 512>(a, 16, stream);
-  return launch_verify<T, 256>(a, fit == 3 ? 2 : std::min(fit, 8u), stream);
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
+  for (uint32_t size : {16u, 8u})
+    if (a.n_seqs <= resident_clusters<T, 512>(dev, size)) return launch_verify<T, 512>(a, size, stream);
+  for (uint32_t size = 8; size > 1; --size)
+    if (a.n_seqs <= resident_clusters<T, 256>(dev, size)) return launch_verify<T, 256>(a, size, stream);
+  return launch_verify<T, 256>(a, 1, stream);
 }
 
 }  // namespace

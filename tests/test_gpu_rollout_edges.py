@@ -247,3 +247,21 @@ def test_cache_of_one_page_and_one_head():
     out, _ = cache.attend(b, q, workspace=rollout.AttendWorkspace(cache, 4, 1))
     want, _, mag = orc.attend(q.float().cpu().numpy(), *(y.float().transpose(0, 1).cpu().numpy() for y in (k, v)), 50, 0.125)
     assert (np.abs(out.float().cpu().numpy() - want) <= out_bound(want, mag)).all()
+
+
+@pytest.mark.parametrize("n", [1, 14, 15, 33, 34, 71, 72, 78, 79, 93, 94, 112, 113, 142, 143, 187, 188, 296, 297, 600])
+@pytest.mark.parametrize("vocab", [33, 4099])
+def test_verify_batches_of_every_cluster_size(n, vocab):
+    """Batches on both sides of the sizes at which a sequence gets fewer blocks (16 and 8 of 512 threads, then 8 to 1 of 256)."""
+    rng = np.random.default_rng(n)
+    counts = rng.integers(0, 3, n)
+    starts, total = np.concatenate([[0], np.cumsum(counts)]), int(counts.sum())
+    p = rng.dirichlet(np.full(vocab, 0.1), total + n).astype(np.float32)
+    q = rng.dirichlet(np.full(vocab, 0.1), total).astype(np.float32)
+    tokens, uniform = np.array([rng.choice(vocab, p=r.astype(np.float64) / r.sum(dtype=np.float64)) for r in q], int), rng.random(total).astype(np.float32)
+    race = rng.exponential(size=(n, vocab)).astype(np.float32)
+    a, out = run_verify(torch.tensor(p, device=DEV), torch.tensor(q, device=DEV), tokens, starts, uniform, torch.tensor(race, device=DEV), 2)
+    for b in range(n):
+        s, e = starts[b], starts[b + 1]
+        wa, wt = orc.verify(p[s + b:e + b + 1], q[s:e], tokens[s:e], uniform[s:e], race[b], 2)
+        assert a[b] == wa and np.array_equal(out[b], wt), b
