@@ -113,8 +113,9 @@ __device__ __forceinline__ KvSeq attend_seq(const KvBatch& b, uint32_t s) {
   return q;
 }
 __device__ __forceinline__ void report_too_long(const AttendArgs& a, uint32_t s) {
+  if (blockIdx.x != 0) return;
   const KvSeq q = kv_seq(a.b, s);
-  if (blockIdx.x == 0 && q.n_new > 0 && q.len > a.b.max_len) atomicOr(a.error, kTooLong);
+  if (q.n_new > 0 && q.len > a.b.max_len) atomicOr(a.error, kTooLong);
 }
 
 // First position that any of the sequence's new tokens attends over.

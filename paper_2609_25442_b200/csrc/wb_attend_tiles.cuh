@@ -43,7 +43,10 @@ struct TilesCfg {
   static constexpr uint32_t kSlots = Q ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 10);
   static constexpr uint32_t kRawBytes = Q ? kKeys * D : 0;         // a tile of codes
   static constexpr uint32_t kRaws = Q && D == 64 ? 8 : 4;
-  static constexpr uint32_t kScaleSlots = D == 64 ? 8 : 4;         // 128 scales each; keys and values in turn
+  // 128 scales each; keys and values in turn.  No fewer than the tiles of codes: a load of scales into a slot then comes after the
+  // widening threads have given back the codes of the slot's last user, which they do behind a proxy fence.
+  static constexpr uint32_t kScaleSlots = D == 64 ? 8 : 4;
+  static_assert(!Q || kScaleSlots >= kRaws, "");
   static constexpr uint32_t kRowSpan = D * (Q ? 1 : 2) < 128 ? D * (Q ? 1 : 2) : 128;   // bytes of a row in a box
   static constexpr uint32_t kRowSpans = D * (Q ? 1 : 2) / kRowSpan;
   // the quarter of a row's weights after which their product may start (3: all; measured best of 0, 1, 3)
@@ -790,8 +793,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           const bool past = (w.blk.kt0 + t - w.item0 - kItemCost) * (int32_t)kKeys + (int32_t)row >= w.seq.len;
           if (past || !isfinite(*at)) {
             if (!past) misc[8 + item % 8] = 1;
-            *at = 0.f;
-            fence_async();            // before the next load into the same place, which waits for the softmax's arrivals only
+            *at = 0.f;                // (ordered before the next load into the same place by the fence below: see kScaleSlots)
           }
           if (++t == min(end, w.item0 + w.blk.n) && t < end) {
             walk_on(w, a, cum, skip_rows);
