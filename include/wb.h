@@ -19,6 +19,10 @@
  * between packing and assembly is a device buffer ("bucket"), and a fused path
  * (wb_remap) goes from trainer tensors to rollout tensors directly.
  *
+ * It also has operators that the rollout engine runs on its weights between two transfers (the last
+ * section; they are not part of the paper's method): a paged key/value cache with the attention over it,
+ * and the verification of drafted tokens.
+ *
  * Conventions
  *   - Every function returns a wb_status and never throws or aborts.  On error the
  *     out-parameters are left untouched and nothing is launched.
@@ -630,7 +634,8 @@ void wb_kv_free(wb_kv* kv);
  * bounds on a sequence's new tokens and on kv_len.  wb_kv_attend goes by both: a loose max_len costs nothing, with one that is too
  * small a longer sequence's rows are zeros with lse = -inf and wb_kv_attend_check tells; max_new chooses the kernels, by the rows
  * of the longest chunk (a loose one costs time, up to twice a decoding step's), and results beyond one that is too
- * small are not computed.  A position
+ * small are not computed.  Rows of the step's tensors that no sequence holds are skipped by wb_kv_write, get zeros from
+ * wb_kv_read and are left as they are by wb_kv_attend; with n_seqs 0 nothing is done.  A position
  * that the table does not cover, or whose page is not in [0, n_pages), is not written, reads as zeros
  * and is attended over as zeros: table entries past a sequence's last page may hold anything.  The arrays are
  * read more than once: they must not change while a call that was given them runs. */

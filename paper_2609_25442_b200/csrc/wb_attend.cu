@@ -3,8 +3,10 @@
 // Two kernels share a batch by the sequences' rows (new tokens x query heads per kv head).  Up to 32 rows the cache's bytes are the
 // bound, and a kernel that streams them through the legacy matrix instructions is the faster; beyond, the products are, and they
 // need tensor memory, in a kernel that fills tiles of 128 rows whatever there are.  24 sequences of 300 to 5000 positions with 8 to 32
-// rows: 72 us (E4M3) and 75 us (bf16) with the border at 32, 103 and 91 with it at 16, 129 and 95 at 8.  Both are launched where a
-// batch may hold both kinds; each leaves the other's alone.
+// rows: 73 us (E4M3) and 75 us (bf16) with the border at 32, 103 and 91 with it at 16, 129 and 95 at 8.  Both are launched where a
+// batch may hold both kinds; each leaves the other's alone.  The row kernel comes with 8, 16 and 32 rows, chosen for the whole batch by
+// max_new: 64 sequences that decode one token with 4 rows each take 194 us with 8, 234 with 32, and 257 where max_new says that there
+// may be long chunks too; 96 over E4M3, 8 rows each, 85, 159 and 159 (caches cold).
 #include <algorithm>
 #include <atomic>
 #include <cmath>

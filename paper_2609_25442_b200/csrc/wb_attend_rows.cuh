@@ -13,11 +13,11 @@
 //     value near 2^8 (what falls below f16's range is under 2^-32 of that value), and weights times row scales f16
 //     relative to a power of two that follows their maximum like the softmax's own: each keeps 11 bits down to 2^-14 of the
 //     largest so far, and is off by at most 2^-25 of it below.  (Widening to bf16 took 10 instructions for
-//     four codes, and the kernel was bound by them: 115 us where this takes 66 for 96 sequences of 500 to 6000
-//     positions, 5.0 TB/s.)
+//     four codes, and the kernel was bound by them: 115 us where this takes 68 for 96 sequences of 500 to 6000
+//     positions, 4.8 TB/s.)
 //   - The running maximum and the f16 exponent move only when a weight would pass 2^8, checked without any exchange: one vote.
-//   - 64 sequences of 17 to 8192 positions, bf16: 178 us, 6.2 TB/s, 0.95 of the copy bandwidth.  With 32 query rows and E4M3 the
-//     matrix instructions of 64 products a tile and warp, and their latency with eight warps on an SM, are the bound: 71 us for 24
+//   - 64 sequences of 17 to 8192 positions, bf16: 179 to 183 us, 6.2 TB/s, 0.94 of the copy bandwidth.  With 32 query rows and E4M3 the
+//     matrix instructions of 64 products a tile and warp, and their latency with eight warps on an SM, are the bound: 73.5 us for 24
 //     sequences, 2.0 TB/s.
 //   - Work is cut evenly over the SMs whatever the lengths: all (sequence, kv head) items form one line of tiles, every block
 //     takes the same number of consecutive tiles, and a second kernel joins the items that cross blocks, in the order of the

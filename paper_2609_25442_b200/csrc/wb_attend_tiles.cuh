@@ -1,8 +1,8 @@
 // Attention for many rows: a block holds 256 rows (new token x query head of one kv head, as two tiles of 128) of a
 // sequence against 128 cache rows at a time.  Scores and the weighted sum of values are tcgen05 products with fp32
-// accumulators in tensor memory.  2048 tokens over 16384 positions, 32 heads of 128 over 8, bf16: 410 us on a cool GPU, 1255
-// TFLOP/s; 476 us, 1080 TFLOP/s, where the passes follow each other without a pause and the power limit sets the clock (a plain
-// bf16 matrix product: 1635 and 1405).
+// accumulators in tensor memory.  2048 tokens over 16384 positions, 32 heads of 128 over 8, bf16: 430 us, 1200
+// TFLOP/s, over 200 passes from a cool GPU; 479 us, 1075 TFLOP/s, where the passes go on and the power limit sets the
+// clock (a plain bf16 matrix product: 1635 and 1405).
 //
 //   - Tensor memory (512 columns): scores of tile 0 and 1 (128 each), outputs of tile 0 and 1 (D each).  A tile's weights
 //     replace its scores as bf16, and enter the second product from there.
@@ -17,8 +17,8 @@
 //   - One warp issues all products in the order  QK0 QK1 | PV0 QK0' PV1 QK1' | ..., one requests cache tiles into a
 //     ring of slots (keys, values, keys, ...) by tensor-map loads, a box per page piece and lane.
 //   - E4M3 caches: tiles arrive as codes, four more warps widen them to bf16 slots; the row scales multiply scores and
-//     weights in the softmax, where each is a value of its own.  This takes 680 us where bf16 takes 410 (tensor core 34 % busy,
-//     issue slots 43 %, ALU 31 %): the step's chain is a microsecond longer, by the scales' loads, products and barriers, and by the
+//     weights in the softmax, where each is a value of its own.  This takes 682 us where bf16 takes 430 (tensor core 36 % busy,
+//     issue slots 45 %, ALU 32 %): the step's chain is a microsecond longer, by the scales' loads, products and barriers, and by the
 //     widening warps' share of the schedulers; 616 us with nothing widened, 530 without scales as well.
 //   - Work is cut as in the kernel for few rows: one line of 128-row tiles over all (sequence, kv head, row block)
 //     items, an equal share for every SM; a second kernel joins the cut items.

@@ -77,8 +77,8 @@ __device__ __forceinline__ void place_tokens(const KvView& c, const KvBatch& b, 
 
 // step tensor -> cache.  A thread has 32 elements of a row, as four pieces of 8 (D / 32 pieces apart, so that the threads of a row
 // read and write whole sectors): with so few threads to a row its maximum takes two exchanges at most, and the two exact divisions
-// of its scale are shared by 32 elements (16 threads to a row, 8 elements each: 42 us for 13.4 thousand
-// tokens of 8 heads of 128 where this takes 17.7, 4.7 TB/s).
+// of its scale are shared by 32 elements (16 threads to a row, 8 elements each: 42 us for 13.4 thousand tokens of 8 heads of 128
+// where this takes 18.4 to 20.5, 4.5 to 4.1 TB/s; what it writes, 28 MB, stays in the second-level cache).
 template <int D, bool F32, bool Q>
 __global__ void __launch_bounds__(kRowThreads, F32 ? 4 : 6)
 wb_kv_write_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {
@@ -174,7 +174,7 @@ wb_kv_write_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {
 
 constexpr uint32_t kAhead = 4;      // rows whose loads a thread has in flight
 
-// cache -> step tensor.  56 thousand tokens of 8 heads of 128 from codes to bf16: 65 us, 5.3 TB/s.
+// cache -> step tensor.  56 thousand tokens of 8 heads of 128 from codes to bf16: 67.5 to 69 us, 5.1 TB/s.
 template <int D, bool F32, bool Q>
 __global__ void __launch_bounds__(kRowThreads)
 wb_kv_read_kernel(KvView c, KvBatch b, Rows k, Rows v, uint32_t per_block) {

@@ -131,7 +131,9 @@ class KvBatch:
 
 class KvCache:
     """Paged keys and values: `k`, `v` [n_pages, n_kv_heads, page_size, head_dim], bf16, or float8_e4m3fn with fp32
-    scales [n_pages, n_kv_heads, page_size].  The tensors stay the caller's; the cache keeps references to them."""
+    scales [n_pages, n_kv_heads, page_size].  The tensors stay the caller's; the cache keeps references to them.  Codes that
+    were not written by write() have to keep to its rule for NaN: attention takes a NaN code for a number unless its row's scale
+    is not finite either."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
         # the stride of a dimension of one leads nowhere
