@@ -724,6 +724,86 @@ typedef struct {
 } wb_verify_args;
 wb_status wb_verify_drafts(const wb_verify_args* args, void* cuda_stream);
 
+/* ---- Trees of drafted tokens ------------------------------------------------------------------------
+ * A sequence's new tokens as the rows of a tree: parent[t] is the row (counted within the sequence's new tokens) that row t
+ * continues, an earlier one; a row with any other parent, as row 0 always, continues the tokens before the new ones.
+ * Every row is written to the place after the row before it, as a chunk's tokens are, but stands at the position that its depth gives:
+ * wb_kv_tree_masks finds depths and ancestors, wb_kv_write_rotated turns queries and keys by such positions, wb_kv_attend_tree
+ * lets a row see the tokens before the tree and its ancestors, wb_verify_tree accepts a path, and wb_kv_keep moves the path's
+ * rows to the places that follow its root's, where the next step expects them. */
+
+/* mask[t][w] (device, n_tokens rows of `words`, 32 * words at least max_new) <- bit i of word w: row 32 w + i of t's sequence is t or an
+ * ancestor of t.  positions[t] (device, may be NULL) <- kv_len - new tokens + depth, a root's depth being 0.  Rows that no sequence
+ * holds are left as they are.  The batch's page table is not used. */
+wb_status wb_kv_tree_masks(const wb_kv_batch* batch, const int32_t* parent, uint32_t* mask, uint32_t words, int32_t* positions,
+                           void* cuda_stream);
+
+/* Angles of the position rotation.  The first rotary_dim elements of a row turn in pairs: element i with i + rotary_dim / 2, or if
+ * `interleaved` is 1, 2i with 2i + 1; the pair (a, b) of index i becomes (a cos - b sin, b cos + a sin), every product and sum rounded to
+ * fp32.  Row p of table holds position p's rotary_dim / 2 pairs (cos, sin).  positions[t] is token t's position; NULL: its place in the
+ * sequence, kv_len - new tokens + its index (max_len must not exceed n_positions then).  At a position that the table does not
+ * have, everything that turns becomes NaN. */
+typedef struct {
+  const float* table;       /* device, 16-byte aligned */
+  const int32_t* positions; /* device, n_tokens entries, or NULL */
+  uint32_t n_positions;
+  uint32_t rotary_dim;      /* head_dim, or a half or a quarter of it */
+  uint32_t interleaved;
+  uint32_t reserved;        /* must be 0 */
+} wb_rotation;
+
+/* wb_kv_write with the keys turned by their positions first, and q (n_heads heads, the type of k and v) turned into q_out (bf16); without
+ * queries n_heads is 0 and both are NULL.  q_out may be q itself (bf16, the same strides), and overlaps nothing else.  A token without
+ * a place in the cache still has its queries turned; rows that no sequence holds are left as they are. */
+wb_status wb_kv_write_rotated(const wb_kv* kv, const wb_kv_batch* batch, const wb_rotation* rotation, const wb_heads* q, uint32_t n_heads,
+                              const wb_heads* q_out, const wb_heads* k, const wb_heads* v, void* cuda_stream);
+
+/* wb_kv_attend for trees: row i of a sequence's new tokens sees all positions before them, and of the new rows 0 .. i those whose bit
+ * in its row of `mask` is set (itself only if its own is); later rows' bits are not looked at.  A window limits what it sees before
+ * the new tokens, by its position: the first new token's place + the number of set bits up to its own - 1.  A window is at least max_new (it
+ * cannot end inside a tree).  Everything else is wb_kv_attend's: types, empty rows, limits, workspace, wb_kv_attend_check. */
+wb_status wb_kv_attend_tree(const wb_kv* kv, const wb_kv_batch* batch, const uint32_t* mask, uint32_t words, const wb_heads* q,
+                            uint32_t n_heads, const wb_heads* out, float* lse, float scale, uint32_t window, void* workspace,
+                            size_t workspace_bytes, void* cuda_stream);
+
+/* Verification of drafted trees.  Sequence b's tree has rows new_start[b] .. new_start[b+1] - 1, row 0 the newest token; tokens[t] is a
+ * row's token (row 0's is not looked at), target row t the target's probabilities after it, draft row t the drafter's, from which the
+ * row's children were drawn independently of each other (draft = NULL: a drafter that is certain of each child).  From row 0 on, the
+ * children c_0, c_1, .. of the row that was accepted last are tried in the order of their rows:
+ *   c_j with token x is accepted if  uniform[c_j] * (S_j * q(x)) < R_j(x),   R_0 = p, S_0 = 1,
+ *   else R_{j+1} = max(R_j - S_j q, 0) and S_{j+1} = sum of R_{j+1}   (certain drafter: q(x) = 1, R_{j+1} = R_j but 0 at x,
+ *                                                                   S_{j+1} = max(S_j - R_j(x), 0)),
+ * in fp32, S rounded from a sum in 64 bits; a comparison with NaN is false, and max(NaN, 0) is 0.  When no child is accepted, or
+ * max_depth have been, one more token is drawn as argmax_v R(v) / race[b][v] (R of all rejected children; the lowest index of equal ones;
+ * if no R(v) is positive, R = p).  With independent Exp(1) variates in race and uniform in [0, 1) the emitted tokens are distributed as
+ * the target's own.  Children whose token is outside the vocabulary are none, and of one row's children the first 256 are looked at.
+ * accepted[b] = the number a of accepted rows; path[b][0 .. a-1] the rows (counted within the tree), emitted[b][0 .. a] their tokens and
+ * the drawn one, both -1 beyond.  A sequence without rows has 0 accepted and emits nothing.  Probabilities as in wb_verify_drafts. */
+typedef struct {
+  uint32_t n_seqs, n_tokens, vocab, max_depth;
+  uint32_t dtype;               /* of target and draft: WB_F32 or WB_BF16 */
+  uint32_t reserved;            /* must be 0 */
+  const void* target;           /* device, n_tokens rows */
+  const void* draft;            /* device, n_tokens rows, or NULL; rows without children are not read */
+  uint64_t target_stride, draft_stride, race_stride;
+  const int32_t* new_start;     /* device, n_seqs + 1 */
+  const int32_t* parent;        /* device, n_tokens */
+  const int32_t* tokens;        /* device, n_tokens */
+  const float* uniform;         /* device, n_tokens */
+  const float* race;            /* device, n_seqs rows */
+  int32_t* accepted;            /* device, n_seqs */
+  int32_t* path;                /* device, n_seqs x max_depth */
+  int32_t* emitted;             /* device, n_seqs x (max_depth + 1) */
+} wb_verify_tree_args;
+wb_status wb_verify_tree(const wb_verify_tree_args* args, void* cuda_stream);
+
+/* Moves the rows of an accepted path (as wb_verify_tree gives it: path[b][0 .. accepted[b] - 1] rising, `depth` entries a sequence) to
+ * the places after row 0's: keys, values and scales of row path[b][j] go to row 1 + j of the sequence's new tokens.  The batch is that
+ * of the tree: afterwards its first kv_len - new tokens + 1 + accepted tokens are the sequence's, and what the tree's other
+ * places hold is undefined.  A path ends where it does not rise or leaves the tree; a row without a page stays where it is. */
+wb_status wb_kv_keep(const wb_kv* kv, const wb_kv_batch* batch, const int32_t* path, const int32_t* accepted, uint32_t depth,
+                     void* cuda_stream);
+
 /* Number of kernels wb_remap / wb_pack / wb_unpack launch per call (always 1). */
 int wb_launches_per_call(void);
 

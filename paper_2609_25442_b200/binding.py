@@ -79,6 +79,19 @@ class wb_verify_args(C.Structure):
                 ("accepted", C.c_void_p), ("tokens", C.c_void_p)]
 
 
+class wb_rotation(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("positions", C.c_void_p), ("n_positions", C.c_uint32), ("rotary_dim", C.c_uint32),
+                ("interleaved", C.c_uint32), ("reserved", C.c_uint32)]
+
+
+class wb_verify_tree_args(C.Structure):
+    _fields_ = [("n_seqs", C.c_uint32), ("n_tokens", C.c_uint32), ("vocab", C.c_uint32), ("max_depth", C.c_uint32),
+                ("dtype", C.c_uint32), ("reserved", C.c_uint32), ("target", C.c_void_p), ("draft", C.c_void_p),
+                ("target_stride", C.c_uint64), ("draft_stride", C.c_uint64), ("race_stride", C.c_uint64),
+                ("new_start", C.c_void_p), ("parent", C.c_void_p), ("tokens", C.c_void_p), ("uniform", C.c_void_p), ("race", C.c_void_p),
+                ("accepted", C.c_void_p), ("path", C.c_void_p), ("emitted", C.c_void_p)]
+
+
 class wb_plan_opts(C.Structure):
     _fields_ = [("bucket_budget_bytes", C.c_uint64), ("tile_bytes", C.c_uint32),
                 ("grid_ctas", C.c_uint32), ("flags", C.c_uint32), ("host_group_kib", C.c_uint32)]
@@ -116,6 +129,7 @@ EXPORTS = [
     "wb_bucket_dequantize", "wb_transfer_rounds_fp8", "wb_pack_fp8", "wb_unpack_fp8", "wb_transfer_rounds_fp8_fused",
     "wb_diff2_nonzeros", "wb_diff2_nonzeros_batch", "wb_diff2_batch_scratch_bytes", "wb_diff2_recombine", "wb_diff2_chunk_pass", "wb_diff2_chunk_scratch_bytes", "wb_scan_slices", "wb_route_account", "wb_wait_probe", "wb_plan_check_replicas", "wb_launches_per_call", "wb_status_str", "wb_version",
     "wb_kv_open", "wb_kv_free", "wb_kv_write", "wb_kv_read", "wb_kv_attend", "wb_kv_attend_workspace_bytes", "wb_kv_attend_check", "wb_verify_drafts",
+    "wb_kv_tree_masks", "wb_kv_write_rotated", "wb_kv_attend_tree", "wb_verify_tree", "wb_kv_keep",
 ]
 
 _lib: Optional[C.CDLL] = None
@@ -192,6 +206,11 @@ def load() -> C.CDLL:
     lib.wb_kv_attend_workspace_bytes.restype = sz
     lib.wb_kv_attend_check.argtypes = [vp, vp]
     lib.wb_verify_drafts.argtypes = [vp, vp]
+    lib.wb_kv_tree_masks.argtypes = [vp, vp, vp, C.c_uint32, vp, vp]
+    lib.wb_kv_write_rotated.argtypes = [vp, vp, vp, vp, C.c_uint32, vp, vp, vp, vp]
+    lib.wb_kv_attend_tree.argtypes = [vp, vp, vp, C.c_uint32, vp, C.c_uint32, vp, vp, C.c_float, C.c_uint32, vp, sz, vp]
+    lib.wb_verify_tree.argtypes = [vp, vp]
+    lib.wb_kv_keep.argtypes = [vp, vp, vp, vp, C.c_uint32, vp]
     lib.wb_launches_per_call.restype = C.c_int
     lib.wb_status_str.argtypes = [C.c_int]
     lib.wb_status_str.restype = C.c_char_p
@@ -576,6 +595,19 @@ class Kv:
         _check(_lib.wb_kv_attend(self.handle, C.byref(batch), C.byref(q), n_heads, C.byref(out), lse_ptr, scale, window,
                                  workspace_ptr, workspace_bytes, stream), "wb_kv_attend")
 
+    def write_rotated(self, batch: wb_kv_batch, rotation: wb_rotation, q: Optional[wb_heads], n_heads: int, q_out: Optional[wb_heads],
+                      k: wb_heads, v: wb_heads, stream: int = 0) -> None:
+        _check(_lib.wb_kv_write_rotated(self.handle, C.byref(batch), C.byref(rotation), C.byref(q) if n_heads else None, n_heads,
+                                        C.byref(q_out) if n_heads else None, C.byref(k), C.byref(v), stream), "wb_kv_write_rotated")
+
+    def attend_tree(self, batch: wb_kv_batch, mask_ptr: int, words: int, q: wb_heads, n_heads: int, out: wb_heads, lse_ptr: int, scale: float,
+                    window: int, workspace_ptr: int, workspace_bytes: int, stream: int = 0) -> None:
+        _check(_lib.wb_kv_attend_tree(self.handle, C.byref(batch), mask_ptr, words, C.byref(q), n_heads, C.byref(out), lse_ptr, scale, window,
+                                      workspace_ptr, workspace_bytes, stream), "wb_kv_attend_tree")
+
+    def keep(self, batch: wb_kv_batch, path_ptr: int, accepted_ptr: int, depth: int, stream: int = 0) -> None:
+        _check(_lib.wb_kv_keep(self.handle, C.byref(batch), path_ptr, accepted_ptr, depth, stream), "wb_kv_keep")
+
 
 def wb_kv_attend_check(workspace_ptr: int, stream: int = 0) -> None:
     load()
@@ -585,3 +617,13 @@ def wb_kv_attend_check(workspace_ptr: int, stream: int = 0) -> None:
 def wb_verify_drafts(args: wb_verify_args, stream: int = 0) -> None:
     load()
     _check(_lib.wb_verify_drafts(C.byref(args), stream), "wb_verify_drafts")
+
+
+def wb_kv_tree_masks(batch: wb_kv_batch, parent_ptr: int, mask_ptr: int, words: int, positions_ptr: int, stream: int = 0) -> None:
+    load()
+    _check(_lib.wb_kv_tree_masks(C.byref(batch), parent_ptr, mask_ptr, words, positions_ptr, stream), "wb_kv_tree_masks")
+
+
+def wb_verify_tree(args: wb_verify_tree_args, stream: int = 0) -> None:
+    load()
+    _check(_lib.wb_verify_tree(C.byref(args), stream), "wb_verify_tree")

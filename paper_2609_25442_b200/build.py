@@ -9,7 +9,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwb.so")
 SOURCES = ["wb_layout.cpp", "wb_plan.cpp", "wb_exec.cu", "wb_extract.cu", "wb_scan.cpp", "wb_quant.cu",
-           "wb_kv.cu", "wb_attend.cu", "wb_verify.cu"]
+           "wb_kv.cu", "wb_attend.cu", "wb_verify.cu",
+           "wb_rotate.cu", "wb_tree.cu", "wb_verify_tree.cu"]
 
 
 def _nvcc() -> str:

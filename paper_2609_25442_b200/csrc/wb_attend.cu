@@ -7,6 +7,8 @@
 // batch may hold both kinds; each leaves the other's alone.  The row kernel comes with 8, 16 and 32 rows, chosen for the whole batch by
 // max_new: 64 sequences that decode one token with 4 rows each take 194 us with 8, 234 with 32, and 257 where max_new says that there
 // may be long chunks too; 96 over E4M3, 8 rows each, 85, 159 and 159 (caches cold).
+#include <cuda_bf16.h>
+
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -99,6 +101,54 @@ cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_r
 }
 
 
+// One warp per attended row, each position in turn.
+template <int D, bool Q>
+__global__ void __launch_bounds__(256) wb_attend_tree_simple(const __grid_constant__ AttendArgs a) {
+  constexpr int N = D / 32;
+  const uint64_t w = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const uint32_t lane = threadIdx.x & 31, head = (uint32_t)(w % a.n_heads), g = head / a.group;
+  const int32_t row = (int32_t)(w / a.n_heads);
+  if (row >= (int32_t)a.b.n_tokens) return;
+  const uint32_t s = kv_seq_of_row(a.b, row);
+  const KvSeq full = kv_seq(a.b, s);
+  const int32_t i = row - full.row0;
+  if (i < 0 || i >= full.n_new) return;
+  if (full.len > a.b.max_len && lane == 0) atomicOr(a.error, kTooLong);
+  const KvSeq q = attend_seq(a.b, s);
+  const uint32_t* mask = a.mask + (uint64_t)row * a.words;
+  const int32_t first = q.len - q.n_new;
+  int32_t sees = 0;
+  for (int32_t j = 0; j <= i; ++j) sees += (uint32_t)j / 32 < a.words ? mask[j / 32] >> (j & 31) & 1 : 0;
+  float x[N], o[N] = {}, m = -INFINITY, l = 0.f;
+  for (int e = 0; e < N; ++e) x[e] = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(a.q + (uint64_t)row * a.q_token + head * a.q_head)[lane * N + e]);
+  for (int32_t pos = a.window ? max(0, first + sees - (int32_t)a.window) : 0; pos <= first + i; ++pos) {
+    const int32_t j = pos - first;
+    if (j >= 0 && !((uint32_t)j / 32 < a.words && mask[j / 32] >> (j & 31) & 1)) continue;
+    const int32_t page = kv_page(a.b, a.c.n_pages, a.c.page_size, s, pos);
+    float k[N] = {}, v[N] = {};
+    if (page >= 0) {
+      const uint32_t slot = (uint32_t)pos % a.c.page_size;
+      const uint64_t at = (uint64_t)page * a.c.page_stride + g * a.c.head_stride + slot * D + lane * N;
+      const uint64_t sc = ((uint64_t)page * a.c.n_kv_heads + g) * a.c.page_size + slot;
+      for (int e = 0; e < N; ++e) {
+        k[e] = Q ? unpack_e4m3x2((uint8_t)a.c.k[at + e]).x * a.c.k_scale[sc] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(a.c.k)[at + e]);
+        v[e] = Q ? unpack_e4m3x2((uint8_t)a.c.v[at + e]).x * a.c.v_scale[sc] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(a.c.v)[at + e]);
+      }
+    }
+    float z = 0.f;
+    for (int e = 0; e < N; ++e) z += x[e] * k[e];
+    for (int d = 16; d; d >>= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, d);
+    if (z == -INFINITY) continue;
+    const float top = fmaxf(m, z), f = m == -INFINITY ? 0.f : exp2f((m - top) * a.scale_log2), p = exp2f((z - top) * a.scale_log2);
+    l = l * f + p;
+    for (int e = 0; e < N; ++e) o[e] = o[e] * f + p * v[e];
+    m = top;
+  }
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+  for (int e = 0; e < N; ++e) reinterpret_cast<__nv_bfloat16*>(a.out + (uint64_t)row * a.o_token + head * a.o_head)[lane * N + e] = __float2bfloat16(o[e] * inv);
+  if (a.lse && lane == 0) a.lse[(uint64_t)row * a.n_heads + head] = l == 0.f ? -INFINITY : (m * a.scale_log2 + log2f(l)) * kLn2;
+}
+
 constexpr uint32_t kCutBytes = (kMaxRowBlocks * sizeof(CutItem) + 255) / 256 * 256;
 template <int D> constexpr size_t partial_bytes() {
   return (size_t)2 * 4 * std::max({kMaxRowBlocks * RowsCfg<D, true, 2>::kPartFloats, 2 * kNumSMs * RowsCfg<D, true, 4>::kPartFloats,
@@ -112,9 +162,12 @@ extern "C" size_t wb_kv_attend_workspace_bytes(const wb_kv* kv, uint32_t n_heads
   return kHeaderBytes + kCutBytes + (kv->d.head_dim == 128 ? partial_bytes<128>() : partial_bytes<64>());
 }
 
-extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* q, uint32_t n_heads,
-                                  const wb_heads* out, float* lse, float scale, uint32_t window, void* workspace,
-                                  size_t workspace_bytes, void* stream) {
+namespace {
+
+// The checks and parameters that both forms share; `todo` is false if there is nothing to do.
+wb_status attend_args(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* q, uint32_t n_heads, const wb_heads* out, float* lse,
+                      float scale, uint32_t window, void* workspace, size_t workspace_bytes, AttendArgs& a, bool& todo) {
+  todo = false;
   if (wb_status s = check_batch(kv, batch)) return s;
   if (wb_status s = check_heads(q, batch->n_tokens, false)) return s;
   if (wb_status s = check_heads(out, batch->n_tokens, false)) return s;
@@ -128,7 +181,6 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   if ((uint64_t)batch->max_len + batch->n_tokens > 0x7FFFFF00ull) return WB_ERR_INVALID_ARG;
   const uint64_t group = n_heads / kv->d.n_kv_heads, row_blocks = (uint64_t)batch->n_tokens * group / kQRows + batch->n_seqs;
   if (row_blocks * (batch->max_len / kKvTile + 2) * kv->d.n_kv_heads > 0x7FFFFFFFull) return WB_ERR_INVALID_ARG;
-  AttendArgs a;
   a.c = kv_view(kv);
   a.b = kv_batch(batch);
   a.q = (const char*)q->data;
@@ -144,6 +196,21 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   a.error = (uint32_t*)workspace;
   a.cuts = (char*)workspace + kHeaderBytes;
   a.partials = (float*)((char*)workspace + kHeaderBytes + kCutBytes);
+  a.mask = nullptr;
+  a.words = 0;
+  todo = true;
+  return WB_OK;
+}
+
+}  // namespace
+
+extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* q, uint32_t n_heads,
+                                  const wb_heads* out, float* lse, float scale, uint32_t window, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  AttendArgs a;
+  bool todo;
+  if (wb_status s = attend_args(kv, batch, q, n_heads, out, lse, scale, window, workspace, workspace_bytes, a, todo)) return s;
+  if (!todo) return WB_OK;
   const bool e = kv->d.dtype == WB_E4M3;
   const cudaStream_t st = (cudaStream_t)stream;
   const uint64_t rows = (uint64_t)batch->max_new * a.group;
@@ -160,6 +227,27 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   }
   if (err != cudaSuccess) (void)cudaGetLastError();
   return err == cudaSuccess ? WB_OK : WB_ERR_CUDA;
+}
+
+extern "C" wb_status wb_kv_attend_tree(const wb_kv* kv, const wb_kv_batch* batch, const uint32_t* mask, uint32_t words, const wb_heads* q,
+                                       uint32_t n_heads, const wb_heads* out, float* lse, float scale, uint32_t window, void* workspace,
+                                       size_t workspace_bytes, void* stream) {
+  AttendArgs a;
+  bool todo;
+  if (wb_status s = attend_args(kv, batch, q, n_heads, out, lse, scale, window, workspace, workspace_bytes, a, todo)) return s;
+  if (((uintptr_t)mask & 3u) || (uint64_t)words * 32 < batch->max_new || words > 0x7FFFFFu) return WB_ERR_INVALID_ARG;
+  // a window that reaches back over a whole tree never ends inside one
+  if (window && window < batch->max_new) return WB_ERR_INVALID_ARG;
+  if (!todo) return WB_OK;
+  if (!mask || !words) return WB_ERR_INVALID_ARG;
+  a.mask = mask;
+  a.words = words;
+  const bool e = kv->d.dtype == WB_E4M3;
+  const cudaStream_t st = (cudaStream_t)stream;
+  const uint32_t grid = (uint32_t)(((uint64_t)batch->n_tokens * n_heads + 7) / 8);
+  if (kv->d.head_dim == 128) e ? wb_attend_tree_simple<128, true><<<grid, 256, 0, st>>>(a) : wb_attend_tree_simple<128, false><<<grid, 256, 0, st>>>(a);
+  else e ? wb_attend_tree_simple<64, true><<<grid, 256, 0, st>>>(a) : wb_attend_tree_simple<64, false><<<grid, 256, 0, st>>>(a);
+  return cudaPeekAtLastError() == cudaSuccess ? WB_OK : (cudaGetLastError(), WB_ERR_CUDA);
 }
 
 extern "C" wb_status wb_kv_attend_check(void* workspace, void* stream) {

@@ -15,6 +15,8 @@ struct AttendArgs {
   float scale_log2;                             // softmax scale times log2(e)
   uint32_t n_heads, group, window;
   uint32_t box_rows;
+  uint32_t words;                               // of a row of mask
+  const uint32_t* mask;                         // trees only: what a row sees of its sequence's new tokens
   uint32_t* error;                              // workspace: first word, bits of AttendError
   char* cuts;                                   // CutItem of every block
   float* partials;

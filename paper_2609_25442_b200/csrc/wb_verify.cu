@@ -10,50 +10,14 @@
 // key (score bits above the complemented index), so it does not depend on the order of the joining.
 #include <cooperative_groups.h>
 
-#include <algorithm>
-#include <atomic>
 #include <cmath>
 
-#include "wb_kv.cuh"
+#include "wb_verify.cuh"
 
 namespace cg = cooperative_groups;
 using namespace wbi;
 
 namespace {
-
-__device__ __forceinline__ float prob(const float* p, uint64_t i) { return __ldg(p + i); }
-__device__ __forceinline__ float prob(const uint16_t* p, uint64_t i) { return __uint_as_float((uint32_t)__ldg(p + i) << 16); }
-__device__ __forceinline__ uint64_t key_max(uint64_t a, uint64_t b) { return a > b ? a : b; }
-
-
-// The best of a thread so far: its key (score bits above the complemented index; scores are not negative, so their bits order as
-// they do, and a larger complement is a lower index), and the score itself.  A candidate whose weight is below the rounded product
-// of that and its race variate is spared the division (all but about ln n of n are): the weight is then below the exact product
-// too, because it is a number that the product could have been rounded to, so its quotient is at most the score, and an equal one
-// of a later index does not win.  (A NaN product, of zero and infinity, spares nothing.)
-struct Best {
-  uint64_t key = 0;                     // below every key: no weight is positive
-  float bar = 0.f;
-  __device__ __forceinline__ void offer(float w, float e, uint32_t v) {
-    if (!(w > 0.f) || w < bar * e) return;
-    const float score = __fdiv_rn(w, e);
-    if (!(score >= 0.f)) return;        // a NaN or negative race variate takes no part
-    key = key_max(key, (uint64_t)__float_as_uint(score) << 32 | (uint32_t)~v);
-    bar = fmaxf(bar, score);
-  }
-};
-
-// Eight probabilities from a 16-byte boundary.
-__device__ __forceinline__ void load8(const float* p, float* x) {
-  const float4 a = __ldcs(reinterpret_cast<const float4*>(p)), b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-__device__ __forceinline__ void load8(const uint16_t* p, float* x) {
-  const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p));
-  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
-}
 
 // w = p, or max(p - q, 0) where there is a q; index `skip` has none.  Rows that start on 16-byte boundaries are read eight
 // elements at a time; others element by element, six in flight (192 rows of 128255: 59 us,
@@ -168,39 +132,6 @@ __global__ void __launch_bounds__(kVerifyThreads, 1024 / kVerifyThreads) wb_veri
   }
 }
 
-cudaLaunchConfig_t config_of(uint32_t n_seqs, uint32_t threads, uint32_t size, cudaLaunchAttribute* at, cudaStream_t stream) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_seqs * size);
-  cfg.blockDim = dim3(threads);
-  cfg.stream = stream;
-  at->id = cudaLaunchAttributeClusterDimension;
-  at->val.clusterDim.x = size;
-  at->val.clusterDim.y = at->val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cfg;
-}
-
-// How many clusters of `size` blocks fit on the device at once: fewer than its places for blocks divided by size, because a
-// cluster lies within one group of SMs.  Asked for once.
-template <typename T, uint32_t kVerifyThreads>
-uint32_t resident_clusters(int dev, uint32_t size) {
-  static std::atomic<int32_t> known[64][17];      // plus one
-  const bool keep = (uint32_t)dev < 64;
-  if (const int32_t n = keep ? known[dev][size].load(std::memory_order_acquire) : 0) return (uint32_t)(n - 1);
-  auto kernel = wb_verify_kernel<T, kVerifyThreads>;
-  cudaLaunchAttribute at[1];
-  const cudaLaunchConfig_t cfg = config_of(1, kVerifyThreads, size, at, nullptr);
-  int n = 0;
-  if ((size > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
-      cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-    (void)cudaGetLastError();
-    n = 0;
-  }
-  if (keep) known[dev][size].store(n + 1, std::memory_order_release);
-  return (uint32_t)n;
-}
-
 template <typename T, uint32_t kVerifyThreads>
 wb_status launch_verify(const wb_verify_args& a, uint32_t size, cudaStream_t stream) {
   cudaLaunchAttribute at[1];
@@ -216,12 +147,13 @@ wb_status launch_verify(const wb_verify_args& a, uint32_t size, cudaStream_t str
 // 32.8 | 32.8; 110 | 118 with 5 33.1 | 49.2, with 4 35.8 | 36.9; 130 | 148 with 4 37.8 | 54.2, with 3 41.0 | 42.0; 180 | 192 with 3 45.1 | 65.5, with 2
 // 53.2 | 53.2.  (Each with the drafts' and the race's rows out of the caches.)
 template <typename T> wb_status launch_verify_of(const wb_verify_args& a, cudaStream_t stream) {
+  static ClusterCounts known[2];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
   for (uint32_t size : {16u, 8u})
-    if (a.n_seqs <= resident_clusters<T, 512>(dev, size)) return launch_verify<T, 512>(a, size, stream);
+    if (a.n_seqs <= resident_clusters(wb_verify_kernel<T, 512>, 512, dev, size, known[0])) return launch_verify<T, 512>(a, size, stream);
   for (uint32_t size = 8; size > 1; --size)
-    if (a.n_seqs <= resident_clusters<T, 256>(dev, size)) return launch_verify<T, 256>(a, size, stream);
+    if (a.n_seqs <= resident_clusters(wb_verify_kernel<T, 256>, 256, dev, size, known[1])) return launch_verify<T, 256>(a, size, stream);
   return launch_verify<T, 256>(a, 1, stream);
 }
 

@@ -1,5 +1,5 @@
 """A rollout engine's step on torch tensors: the paged key/value cache (written, read back, attended over)
-and the verification of drafted tokens.  The work is done by libwb.so; this module checks tensors,
+and the verification of drafted tokens, one after another or as trees.  The work is done by libwb.so; this module checks tensors,
 allocates results and passes torch's current stream.  All tensors are on the current device.
 There are no backward passes, and tensors that want gradients are refused.
 
@@ -8,6 +8,15 @@ There are no backward passes, and tensors that want gradients are refused.
     cache.write(batch, k, v)                      # k, v: [T, n_kv_heads, head_dim], e.g. slices of qkv
     out, lse = cache.attend(batch, q, workspace=AttendWorkspace(cache, n_heads, n_seqs))
     accepted, tokens = verify_drafts(target, draft, draft_tokens, draft_start, uniform, race, max_drafts=K)
+
+With trees of drafted tokens, and positions turned into queries and keys on their way:
+
+    rotation = Rotation.of(head_dim, n_positions)
+    tree = DraftTree(batch, parent)               # the batch's new tokens are the trees' rows
+    q = cache.write_rotated(batch, rotation, k, v, q=q, positions=tree.positions)
+    out, lse = cache.attend_tree(batch, q, tree, workspace=workspace)
+    accepted, path, emitted = verify_tree(tree, target, draft, tokens, uniform, race, max_depth=D)
+    cache.keep(batch, path, accepted)             # the sequences now have kv_len - rows + 1 + accepted tokens
 """
 from __future__ import annotations
 
@@ -197,6 +206,13 @@ class KvCache:
         """Attention of the new tokens' queries (bf16, [n_tokens, n_heads, head_dim]) over the cache, causal at the
         sequences' ends; window > 0 limits a query to that many latest positions.  Returns (out, lse), which are confirmed when
         workspace.check() has passed after them; rows that no sequence holds are left as they are."""
+        a, h, b, out, lse = self._attention(batch, q, workspace, window, out, lse)
+        self._kv.attend(batch._for(self), a, h, b, lse.data_ptr(), self._scale if scale is None else scale, window,
+                        workspace.pointer, workspace.bytes, _stream(self._index))
+        return out, lse
+
+    def _attention(self, batch: KvBatch, q: torch.Tensor, workspace: "AttendWorkspace", window: int, out: Optional[torch.Tensor],
+                   lse: Optional[torch.Tensor]):
         if q.dim() != 3:
             raise ValueError("q: [n_tokens, n_heads, head_dim]")
         if workspace.device is not self.device and workspace.device != self.device:
@@ -214,9 +230,113 @@ class KvCache:
             lse = self._like[torch.float32].new_empty((n, h))
         elif lse.shape != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != self.device:
             raise ValueError("lse: contiguous fp32 [n_tokens, n_heads]")
-        self._kv.attend(batch._for(self), a, h, b, lse.data_ptr(), self._scale if scale is None else scale, window,
-                        workspace.pointer, workspace.bytes, _stream(self._index))
+        return a, h, b, out, lse
+
+    def write_rotated(self, batch: KvBatch, rotation: "Rotation", k: torch.Tensor, v: torch.Tensor, *, q: Optional[torch.Tensor] = None,
+                      positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+        """write() with the keys turned by their positions first.  Queries (`q`, [n_tokens, n_heads, head_dim], the type of k and v)
+        are turned too and returned as bf16, in `q_out` if given, which may be q itself.  `positions` (int32 [n_tokens], e.g.
+        DraftTree.positions) are the tokens' places in their sequences if not given; the batch's max_len then has to be
+        within the rotation's table.  At a position outside the table, what turns becomes NaN."""
+        n, d, dev = batch.n_tokens, self.head_dim, self.device
+        a = _heads(k, "k", n, self.n_kv_heads, d, dev)
+        b = _heads(v, "v", n, self.n_kv_heads, d, dev)
+        _require(rotation.device == dev and rotation.rotary_dim in (d, d // 2, d // 4),
+                 f"rotation: a table on {dev} for {d}, {d // 2} or {d // 4} elements of a row")
+        args = batch._for(self)
+        if positions is not None:
+            _require(positions.shape == (n,) and positions.is_contiguous(), "positions: contiguous, [n_tokens]")
+            _ints(positions, "positions", dev)
+        else:
+            _require(args.max_len <= rotation.n_positions, f"the batch's max_len is {args.max_len}, the rotation's table has {rotation.n_positions} positions")
+        h, x, y = 0, None, None
+        if q is None:
+            _require(q_out is None, "q_out without q")
+        else:
+            _require(q.dim() == 3, "q: [n_tokens, n_heads, head_dim]")
+            h = q.shape[1]
+            x = _heads(q, "q", n, h, d, dev)
+            _require(q.dtype == k.dtype, f"q is {q.dtype}, k is {k.dtype}")
+            if q_out is None:
+                q_out = self._like[torch.bfloat16].new_empty((n, h, d))
+                y = wb.wb_heads(q_out.data_ptr(), wb.WB_BF16, 0, h * d, d)
+            else:
+                y = _heads(q_out, "q_out", n, h, d, dev)
+            if h == 0:
+                x = y = None
+        self._kv.write_rotated(args, rotation._args(positions), x, h, y, a, b, _stream(self._index))
+        return q_out
+
+    def attend_tree(self, batch: KvBatch, q: torch.Tensor, tree: "DraftTree", *, workspace: "AttendWorkspace", scale: Optional[float] = None,
+                    window: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
+        """attend() for the rows of trees: a row sees all tokens before its sequence's new ones (with window > 0, the latest of
+        them as its depth has it) and its ancestors.  A window is at least the batch's max_new."""
+        _require(tree.mask.shape[0] == batch.n_tokens and tree.device == self.device, "tree: of the batch's rows, on the cache's device")
+        a, h, b, out, lse = self._attention(batch, q, workspace, window, out, lse)
+        args = batch._for(self)
+        _require(32 * tree.words >= args.max_new and not 0 < window < args.max_new,
+                 f"trees of up to {args.max_new} rows: the tree's mask has {32 * tree.words} bits, and a window is 0 or at least that many")
+        self._kv.attend_tree(args, tree.mask.data_ptr(), tree.words, a, h, b, lse.data_ptr(), self._scale if scale is None else scale, window,
+                             workspace.pointer, workspace.bytes, _stream(self._index))
         return out, lse
+
+    def keep(self, batch: KvBatch, path: torch.Tensor, accepted: torch.Tensor) -> None:
+        """Moves the rows of accepted paths (`path` [n_seqs, depth], `accepted` [n_seqs], as verify_tree returns them) to the places
+        after their trees' roots.  The batch is the trees'; afterwards a sequence's first kv_len - rows + 1 + accepted tokens are its
+        own, and what the tree's other places hold is undefined."""
+        _require(path.dim() == 2 and path.shape[0] == batch.n_seqs and path.is_contiguous() and accepted.shape == (batch.n_seqs,) and accepted.is_contiguous(),
+                 "path: [n_seqs, depth], accepted: [n_seqs], contiguous")
+        _ints(path, "path", self.device)
+        _ints(accepted, "accepted", self.device)
+        self._kv.keep(batch._for(self), path.data_ptr(), accepted.data_ptr(), path.shape[1], _stream(self._index))
+
+
+class Rotation:
+    """Angles of the position rotation: `cos`, `sin` [n_positions, rotary_dim / 2], kept as one fp32 table.  The first rotary_dim elements
+    of a row turn (all of its head_dim, a half or a quarter): element i with i + rotary_dim / 2, or, if `interleaved`, 2i with 2i + 1."""
+
+    def __init__(self, cos: torch.Tensor, sin: torch.Tensor, *, interleaved: bool = False):
+        _require(cos.dim() == 2 and cos.shape == sin.shape and cos.device == sin.device and cos.is_cuda and cos.shape[1] > 0,
+                 "cos and sin: [n_positions, rotary_dim / 2] on a CUDA device")
+        for t, name in ((cos, "cos"), (sin, "sin")):
+            _no_gradient(t, name)
+        self.n_positions, self.rotary_dim, self.interleaved = _count(cos.shape[0], "positions"), 2 * int(cos.shape[1]), bool(interleaved)
+        self.table = torch.stack((cos, sin), -1).to(torch.float32).contiguous()
+        self.device = cos.device
+
+    @classmethod
+    def of(cls, rotary_dim: int, n_positions: int, *, base: float = 10000.0, interleaved: bool = False, device="cuda") -> "Rotation":
+        """Angle p * base^(-2 i / rotary_dim) of pair i at position p, its cosine and sine taken in 64 bits."""
+        half = rotary_dim // 2
+        _require(half > 0 and rotary_dim % 2 == 0, f"rotary_dim: {rotary_dim} is not a positive even number")
+        freq = float(base) ** (-torch.arange(half, dtype=torch.float64, device=device) / half)
+        angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * freq
+        return cls(angle.cos(), angle.sin(), interleaved=interleaved)
+
+    def _args(self, positions: Optional[torch.Tensor]) -> wb.wb_rotation:
+        return wb.wb_rotation(self.table.data_ptr(), None if positions is None else positions.data_ptr(), self.n_positions, self.rotary_dim,
+                              int(self.interleaved), 0)
+
+
+class DraftTree:
+    """The trees that a batch's new tokens are: `parent` (int32 [n_tokens]) is the row that a row continues, counted within
+    its sequence's new tokens, and an earlier one; any other value makes it a root, as row 0 always is.  `mask` [n_tokens, words] (int32)
+    holds a row's ancestors and itself as bits, `positions` [n_tokens] the place before the new tokens plus one plus the depth.  Rows that
+    no sequence holds are undefined in both.  build() finds them again after the batch's or the parents' tensors were changed."""
+
+    def __init__(self, batch: KvBatch, parent: torch.Tensor):
+        _require(parent.shape == (batch.n_tokens,) and parent.is_contiguous(), "parent: contiguous, [n_tokens]")
+        _require(batch._index is not None, "the batch needs a CUDA device (sm_100a)")
+        self.batch, self.parent, self.device = batch, _ints(parent, "parent", batch.device), batch.device
+        self.words = max(1, (int(batch.args.max_new) + 31) // 32)
+        self.mask = parent.new_empty((batch.n_tokens, self.words))
+        self.positions = parent.new_empty(batch.n_tokens)
+        self.build()
+
+    def build(self) -> None:
+        _on_device(self.batch._index)
+        wb.wb_kv_tree_masks(self.batch.args, self.parent.data_ptr(), self.mask.data_ptr(), self.words, self.positions.data_ptr(),
+                            _stream(self.batch._index))
 
 
 class AttendWorkspace:
@@ -275,3 +395,42 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
                                           draft_tokens.data_ptr(), draft_start.data_ptr(), uniform.data_ptr(), race.data_ptr(),
                                           accepted.data_ptr(), tokens.data_ptr()), _stream(dev.index))
     return accepted, tokens
+
+
+def verify_tree(tree: DraftTree, target: torch.Tensor, draft: Optional[torch.Tensor], tokens: torch.Tensor, uniform: torch.Tensor,
+                race: torch.Tensor, *, max_depth: int):
+    """Accept a path of each drafted tree against the target's probabilities and draw the token after it.
+
+    target and draft [n_tokens, vocab]: the distributions after each row (draft None: a drafter that is certain of each child;
+    else a row's children were drawn independently from its draft row), tokens and uniform [n_tokens], race [n_seqs, vocab]
+    (Exp(1) variates).  Returns (accepted [n_seqs], path [n_seqs, max_depth], emitted [n_seqs, max_depth + 1]), int32: how many rows were
+    accepted, which (counted within the tree), and their tokens with the drawn one; -1 beyond.  Rows may be one row broadcast."""
+    dev, n, total = tree.device, tree.batch.n_seqs, tree.batch.n_tokens
+    if target.dim() != 2 or target.shape[0] != total or target.device != dev or (target.stride(1) != 1 and target.shape[1] != 1):
+        raise ValueError(f"target: [n_tokens, vocab] with contiguous rows on {dev}")
+    vocab = target.shape[1]
+    _on_device(dev.index)
+    if _grad_enabled():
+        for t, name in ((target, "target"), (draft, "draft"), (race, "race"), (uniform, "uniform")):
+            if t is not None:
+                _no_gradient(t, name)
+    if target.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"probabilities of {target.dtype}: float32 or bfloat16")
+    if draft is not None and (draft.shape != (total, vocab) or draft.dtype != target.dtype or draft.device != dev or (draft.stride(1) != 1 and vocab != 1)):
+        raise ValueError("draft: [n_tokens, vocab] of the target's type")
+    if uniform.shape != (total,) or uniform.dtype != torch.float32 or uniform.device != dev or not uniform.is_contiguous():
+        raise ValueError("uniform: fp32 [n_tokens]")
+    if race.shape != (n, vocab) or race.dtype != torch.float32 or race.device != dev or (race.stride(1) != 1 and vocab != 1):
+        raise ValueError("race: fp32 [n_seqs, vocab]")
+    if tokens.shape != (total,) or not tokens.is_contiguous():
+        raise ValueError("tokens: contiguous, [n_tokens]")
+    _ints(tokens, "tokens", dev)
+    max_depth = _count(max_depth, "max_depth")
+    accepted, path, emitted = tokens.new_empty(n), tokens.new_empty((n, max_depth)), tokens.new_empty((n, max_depth + 1))
+    none = draft is None or total == 0
+    wb.wb_verify_tree(wb.wb_verify_tree_args(n, total, vocab, max_depth, _DTYPE[target.dtype], 0, target.data_ptr(),
+                                             None if none else draft.data_ptr(), _pitch(target, vocab, "target"),
+                                             0 if none else _pitch(draft, vocab, "draft"), _pitch(race, vocab, "race"),
+                                             tree.batch.new_start.data_ptr(), tree.parent.data_ptr(), tokens.data_ptr(), uniform.data_ptr(),
+                                             race.data_ptr(), accepted.data_ptr(), path.data_ptr(), emitted.data_ptr()), _stream(dev.index))
+    return accepted, path, emitted
