@@ -7,8 +7,6 @@
 // batch may hold both kinds; each leaves the other's alone.  The row kernel comes with 8, 16 and 32 rows, chosen for the whole batch by
 // max_new: 64 sequences that decode one token with 4 rows each take 194 us with 8, 234 with 32, and 257 where max_new says that there
 // may be long chunks too; 96 over E4M3, 8 rows each, 85, 159 and 159 (caches cold).
-#include <cuda_bf16.h>
-
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -55,11 +53,11 @@ cudaError_t launch_join(void (*kernel)(AttendArgs), dim3 grid, uint32_t threads,
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <int D, bool Q, int NT>
+template <int D, bool Q, int NT, bool TREE>
 cudaError_t launch_rows(const AttendArgs& a, int dev, cudaStream_t stream) {
   using C = RowsCfg<D, Q, NT>;
   const size_t smem = C::smem_bytes(a.b.n_seqs);
-  auto kernel = wb_attend_rows_kernel<D, Q, NT>;
+  auto kernel = wb_attend_rows_kernel<D, Q, NT, TREE>;
   // every block gets the same share of the tiles, so the grid is what fits at once (with thousands of sequences the table of
   // prefix sums takes the place of a block)
   const uint32_t per_sm = std::min<uint32_t>(C::kBlocksPerSm, (uint32_t)(kSmemPerSm / (smem + 2048)));
@@ -72,17 +70,17 @@ cudaError_t launch_rows(const AttendArgs& a, int dev, cudaStream_t stream) {
   return launch_join(wb_attend_join_rows_kernel<D, NT>, dim3(grid, 2 * NT), 256, a, stream);
 }
 
-template <int D, bool Q>
+template <int D, bool Q, bool TREE>
 cudaError_t launch_rows_of(uint32_t rows, const AttendArgs& a, int dev, cudaStream_t stream) {
-  if (rows <= 8) return launch_rows<D, Q, 1>(a, dev, stream);
-  if (rows <= 16) return launch_rows<D, Q, 2>(a, dev, stream);
-  return launch_rows<D, Q, 4>(a, dev, stream);
+  if (rows <= 8) return launch_rows<D, Q, 1, TREE>(a, dev, stream);
+  if (rows <= 16) return launch_rows<D, Q, 2, TREE>(a, dev, stream);
+  return launch_rows<D, Q, 4, TREE>(a, dev, stream);
 }
 
-template <int D, bool Q>
+template <int D, bool Q, bool TREE>
 cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_rows, cudaStream_t stream) {
   using C = TilesCfg<D, Q>;
-  auto kernel = wb_attend_tiles_kernel<D, Q>;
+  auto kernel = wb_attend_tiles_kernel<D, Q, TREE>;
   // the softmax warps wait for registers that the others give back: the launch has to have them
   static std::atomic<uint64_t> done{0};
   cudaError_t e = prepare_kernel(kernel, C::kSmemBytes, C::kLaunchRegs, kv->device, done);
@@ -100,54 +98,6 @@ cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_r
   return cudaSuccess;
 }
 
-
-// One warp per attended row, each position in turn.
-template <int D, bool Q>
-__global__ void __launch_bounds__(256) wb_attend_tree_simple(const __grid_constant__ AttendArgs a) {
-  constexpr int N = D / 32;
-  const uint64_t w = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const uint32_t lane = threadIdx.x & 31, head = (uint32_t)(w % a.n_heads), g = head / a.group;
-  const int32_t row = (int32_t)(w / a.n_heads);
-  if (row >= (int32_t)a.b.n_tokens) return;
-  const uint32_t s = kv_seq_of_row(a.b, row);
-  const KvSeq full = kv_seq(a.b, s);
-  const int32_t i = row - full.row0;
-  if (i < 0 || i >= full.n_new) return;
-  if (full.len > a.b.max_len && lane == 0) atomicOr(a.error, kTooLong);
-  const KvSeq q = attend_seq(a.b, s);
-  const uint32_t* mask = a.mask + (uint64_t)row * a.words;
-  const int32_t first = q.len - q.n_new;
-  int32_t sees = 0;
-  for (int32_t j = 0; j <= i; ++j) sees += (uint32_t)j / 32 < a.words ? mask[j / 32] >> (j & 31) & 1 : 0;
-  float x[N], o[N] = {}, m = -INFINITY, l = 0.f;
-  for (int e = 0; e < N; ++e) x[e] = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(a.q + (uint64_t)row * a.q_token + head * a.q_head)[lane * N + e]);
-  for (int32_t pos = a.window ? max(0, first + sees - (int32_t)a.window) : 0; pos <= first + i; ++pos) {
-    const int32_t j = pos - first;
-    if (j >= 0 && !((uint32_t)j / 32 < a.words && mask[j / 32] >> (j & 31) & 1)) continue;
-    const int32_t page = kv_page(a.b, a.c.n_pages, a.c.page_size, s, pos);
-    float k[N] = {}, v[N] = {};
-    if (page >= 0) {
-      const uint32_t slot = (uint32_t)pos % a.c.page_size;
-      const uint64_t at = (uint64_t)page * a.c.page_stride + g * a.c.head_stride + slot * D + lane * N;
-      const uint64_t sc = ((uint64_t)page * a.c.n_kv_heads + g) * a.c.page_size + slot;
-      for (int e = 0; e < N; ++e) {
-        k[e] = Q ? unpack_e4m3x2((uint8_t)a.c.k[at + e]).x * a.c.k_scale[sc] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(a.c.k)[at + e]);
-        v[e] = Q ? unpack_e4m3x2((uint8_t)a.c.v[at + e]).x * a.c.v_scale[sc] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(a.c.v)[at + e]);
-      }
-    }
-    float z = 0.f;
-    for (int e = 0; e < N; ++e) z += x[e] * k[e];
-    for (int d = 16; d; d >>= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, d);
-    if (z == -INFINITY) continue;
-    const float top = fmaxf(m, z), f = m == -INFINITY ? 0.f : exp2f((m - top) * a.scale_log2), p = exp2f((z - top) * a.scale_log2);
-    l = l * f + p;
-    for (int e = 0; e < N; ++e) o[e] = o[e] * f + p * v[e];
-    m = top;
-  }
-  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
-  for (int e = 0; e < N; ++e) reinterpret_cast<__nv_bfloat16*>(a.out + (uint64_t)row * a.o_token + head * a.o_head)[lane * N + e] = __float2bfloat16(o[e] * inv);
-  if (a.lse && lane == 0) a.lse[(uint64_t)row * a.n_heads + head] = l == 0.f ? -INFINITY : (m * a.scale_log2 + log2f(l)) * kLn2;
-}
 
 constexpr uint32_t kCutBytes = (kMaxRowBlocks * sizeof(CutItem) + 255) / 256 * 256;
 template <int D> constexpr size_t partial_bytes() {
@@ -202,6 +152,24 @@ wb_status attend_args(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads*
   return WB_OK;
 }
 
+template <bool TREE> wb_status launch_attend(const AttendArgs& a, const wb_kv* kv, const wb_kv_batch* batch, cudaStream_t st) {
+  const bool e = kv->d.dtype == WB_E4M3;
+  const uint64_t rows = (uint64_t)batch->max_new * a.group;
+  cudaError_t err = cudaSuccess;
+  if (rows <= kMaxRows || batch->n_seqs > 1) {
+    const uint32_t r = (uint32_t)std::min<uint64_t>(rows, kMaxRows);
+    if (kv->d.head_dim == 128) err = e ? launch_rows_of<128, true, TREE>(r, a, kv->device, st) : launch_rows_of<128, false, TREE>(r, a, kv->device, st);
+    else err = e ? launch_rows_of<64, true, TREE>(r, a, kv->device, st) : launch_rows_of<64, false, TREE>(r, a, kv->device, st);
+  }
+  if (err == cudaSuccess && rows > kMaxRows) {
+    const uint32_t skip = batch->n_seqs > 1 ? kMaxRows : 0;
+    if (kv->d.head_dim == 128) err = e ? launch_tiles<128, true, TREE>(a, kv, skip, st) : launch_tiles<128, false, TREE>(a, kv, skip, st);
+    else err = e ? launch_tiles<64, true, TREE>(a, kv, skip, st) : launch_tiles<64, false, TREE>(a, kv, skip, st);
+  }
+  if (err != cudaSuccess) (void)cudaGetLastError();
+  return err == cudaSuccess ? WB_OK : WB_ERR_CUDA;
+}
+
 }  // namespace
 
 extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads* q, uint32_t n_heads,
@@ -211,22 +179,7 @@ extern "C" wb_status wb_kv_attend(const wb_kv* kv, const wb_kv_batch* batch, con
   bool todo;
   if (wb_status s = attend_args(kv, batch, q, n_heads, out, lse, scale, window, workspace, workspace_bytes, a, todo)) return s;
   if (!todo) return WB_OK;
-  const bool e = kv->d.dtype == WB_E4M3;
-  const cudaStream_t st = (cudaStream_t)stream;
-  const uint64_t rows = (uint64_t)batch->max_new * a.group;
-  cudaError_t err = cudaSuccess;
-  if (rows <= kMaxRows || batch->n_seqs > 1) {
-    const uint32_t r = (uint32_t)std::min<uint64_t>(rows, kMaxRows);
-    if (kv->d.head_dim == 128) err = e ? launch_rows_of<128, true>(r, a, kv->device, st) : launch_rows_of<128, false>(r, a, kv->device, st);
-    else err = e ? launch_rows_of<64, true>(r, a, kv->device, st) : launch_rows_of<64, false>(r, a, kv->device, st);
-  }
-  if (err == cudaSuccess && rows > kMaxRows) {
-    const uint32_t skip = batch->n_seqs > 1 ? kMaxRows : 0;
-    if (kv->d.head_dim == 128) err = e ? launch_tiles<128, true>(a, kv, skip, st) : launch_tiles<128, false>(a, kv, skip, st);
-    else err = e ? launch_tiles<64, true>(a, kv, skip, st) : launch_tiles<64, false>(a, kv, skip, st);
-  }
-  if (err != cudaSuccess) (void)cudaGetLastError();
-  return err == cudaSuccess ? WB_OK : WB_ERR_CUDA;
+  return launch_attend<false>(a, kv, batch, (cudaStream_t)stream);
 }
 
 extern "C" wb_status wb_kv_attend_tree(const wb_kv* kv, const wb_kv_batch* batch, const uint32_t* mask, uint32_t words, const wb_heads* q,
@@ -242,12 +195,7 @@ extern "C" wb_status wb_kv_attend_tree(const wb_kv* kv, const wb_kv_batch* batch
   if (!mask || !words) return WB_ERR_INVALID_ARG;
   a.mask = mask;
   a.words = words;
-  const bool e = kv->d.dtype == WB_E4M3;
-  const cudaStream_t st = (cudaStream_t)stream;
-  const uint32_t grid = (uint32_t)(((uint64_t)batch->n_tokens * n_heads + 7) / 8);
-  if (kv->d.head_dim == 128) e ? wb_attend_tree_simple<128, true><<<grid, 256, 0, st>>>(a) : wb_attend_tree_simple<128, false><<<grid, 256, 0, st>>>(a);
-  else e ? wb_attend_tree_simple<64, true><<<grid, 256, 0, st>>>(a) : wb_attend_tree_simple<64, false><<<grid, 256, 0, st>>>(a);
-  return cudaPeekAtLastError() == cudaSuccess ? WB_OK : (cudaGetLastError(), WB_ERR_CUDA);
+  return launch_attend<true>(a, kv, batch, (cudaStream_t)stream);
 }
 
 extern "C" wb_status wb_kv_attend_check(void* workspace, void* stream) {

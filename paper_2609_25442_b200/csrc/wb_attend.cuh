@@ -120,9 +120,23 @@ __device__ __forceinline__ void report_too_long(const AttendArgs& a, uint32_t s)
   if (q.n_new > 0 && q.len > a.b.max_len) atomicOr(a.error, kTooLong);
 }
 
-// First position that any of the sequence's new tokens attends over.
-__device__ __forceinline__ int32_t first_position(const KvSeq& q, uint32_t window) {
-  return window ? max(0, q.len - q.n_new - (int32_t)window + 1) : 0;
+// First position that any of the sequence's new tokens attends over.  (A tree's row that sees none of the tree, itself included, stands
+// before it.)
+template <bool TREE> __device__ __forceinline__ int32_t first_position(const KvSeq& q, uint32_t window) {
+  return window ? max(0, q.len - q.n_new - (int32_t)window + (TREE ? 0 : 1)) : 0;
+}
+
+// Word w of the row of mask of row t of the step's tensors; before the tree everything is seen, beyond the mask nothing.
+__device__ __forceinline__ uint32_t tree_word(const AttendArgs& a, uint32_t t, int32_t w) {
+  return w < 0 ? 0xFFFFFFFFu : (uint32_t)w < a.words ? __ldg(a.mask + (uint64_t)t * a.words + w) : 0u;
+}
+// The lowest position that row i of a tree, row t of the step's tensors, sees: its own is the first new token's place plus the rows
+// that it sees, less one.
+__device__ __forceinline__ int32_t tree_low(const AttendArgs& a, const KvSeq& q, uint32_t t, int32_t i) {
+  if (!a.window) return 0;
+  int32_t sees = 0;
+  for (int32_t w = 0; w <= i >> 5; ++w) sees += __popc(tree_word(a, t, w) & (w == i >> 5 ? 0xFFFFFFFFu >> (31 - (i & 31)) : 0xFFFFFFFFu));
+  return q.len - q.n_new + sees - (int32_t)a.window;
 }
 
 }  // namespace wbi

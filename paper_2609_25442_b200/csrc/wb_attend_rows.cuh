@@ -115,7 +115,7 @@ struct TilePlace {
   uint32_t slot;
 };
 
-template <int D, bool Q, int NT>
+template <int D, bool Q, int NT, bool TREE>
 __global__ void __launch_bounds__(128, RowsCfg<D, Q, NT>::kBlocksPerSm)
 wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   using C = RowsCfg<D, Q, NT>;
@@ -140,7 +140,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       const KvSeq q = attend_seq(a.b, s);
       int32_t nt = 0;
       if (q.n_new > 0 && (uint32_t)q.n_new * a.group <= C::kRows) {
-        const int32_t lo = first_position(q, a.window) / (int32_t)kKvTile;
+        const int32_t lo = first_position<TREE>(q, a.window) / (int32_t)kKvTile;
         nt = max(1, (q.len + (int32_t)kKvTile - 1) / (int32_t)kKvTile - lo);
       }
       report_too_long(a, s);
@@ -192,7 +192,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       const uint32_t s = find(t);
       const KvSeq q = attend_seq(a.b, s);
       const int32_t nt = (cum[s + 1] - cum[s]) / (int32_t)hk, local = t - cum[s], h = local / nt;
-      const uint32_t pos = (uint32_t)(first_position(q, a.window) / (int32_t)kKvTile + local - h * nt) * kKvTile + warp * 16;
+      const uint32_t pos = (uint32_t)(first_position<TREE>(q, a.window) / (int32_t)kKvTile + local - h * nt) * kKvTile + warp * 16;
       const uint32_t entry = pos / a.c.page_size;
       x.slot = pos - entry * a.c.page_size;
       if (pos < (uint32_t)q.len && entry < a.b.table_stride) {
@@ -242,7 +242,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     while (cum[x.s + 1] <= t) ++x.s;
     const KvSeq q = attend_seq(a.b, x.s);
     const int32_t nt = (cum[x.s + 1] - cum[x.s]) / (int32_t)hk;
-    x.tile0 = first_position(q, a.window) / (int32_t)kKvTile;
+    x.tile0 = first_position<TREE>(q, a.window) / (int32_t)kKvTile;
     x.h = (t - cum[x.s]) / nt;
     x.i0 = cum[x.s] + x.h * nt;
     x.i1 = x.i0 + nt;
@@ -252,6 +252,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     x.n_new = q.n_new;
   };
   uint32_t qf[kGroups][D / 16][2];
+  uint32_t tree[NT][2];            // trees: what rows 2t, 2t + 1 of every group of 8 see of the sequence's new tokens, at most 32
   const uint32_t group_inv = (65536 + a.group - 1) / a.group;      // r / group = r * group_inv >> 16 for r < 64
   auto fetch_queries = [&](const Item& x) {
 #pragma unroll
@@ -274,6 +275,15 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         qf[n][ks][0] = w.x;
         qf[n][ks][1] = w.y;
       }
+    }
+    if (TREE) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t r = n * 8 + 2 * t4 + e;
+          tree[n][e] = r < x.n_rows ? tree_word(a, (uint32_t)x.row0 + (r * group_inv >> 16), 0) : 0xFFFFFFFFu;
+        }
     }
   };
 
@@ -350,6 +360,13 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     };
     // how far row r sees; a row that is none sees everything
     auto sees_to = [&](uint32_t r) { return r < n_rows ? first_hi + (int32_t)(r * group_inv >> 16) : 0x7FFFFFFF; };
+    // whether row 2t + e of group n does not see a position that it reaches: it lies before its window, or is not in its mask
+    auto hidden = [&](int n, int e, int32_t up, int32_t pos) {
+      if (!TREE) return a.window && up != 0x7FFFFFFF && pos <= up - (int32_t)a.window;
+      if (pos >= first_hi) return !(tree[n][e] >> ((pos - first_hi) & 31) & 1);
+      // (its own position is first_hi plus the rows that it sees, less one)
+      return a.window && up != 0x7FFFFFFF && pos < first_hi + __popc(tree[n][e] & 0xFFFFFFFFu >> (31 - ((up - first_hi) & 31))) - (int32_t)a.window;
+    };
 
     float acc[NT][D / 16][4];
     // the score that the weights are relative to, the score above which it moves, sums; 2^-(f16 exponent), the weight
@@ -416,16 +433,15 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         for (int n = 0; n < NT; ++n) { sc[n][0] *= k0; sc[n][1] *= k0; sc[n][2] *= k1; sc[n][3] *= k1; }
       }
       // rows that some query row does not see, or that lie past the end of the cache
-      const bool partial = pos0 + 15 > first_hi || pos0 < last_lo;
+      const bool partial = (TREE ? pos0 + 15 >= first_hi : pos0 + 15 > first_hi) || pos0 < last_lo;
       if (partial) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const int32_t up = sees_to(n * 8 + 2 * t4 + e), low = a.window && up != 0x7FFFFFFF ? up - (int32_t)a.window + 1 : 0;
-            const int32_t pos = pos0 + (int32_t)r8;
-            if (pos > up || pos < low) sc[n][e] = -INFINITY;
-            if (pos + 8 > up || pos + 8 < low) sc[n][2 + e] = -INFINITY;
+            const int32_t up = sees_to(n * 8 + 2 * t4 + e), pos = pos0 + (int32_t)r8;
+            if (pos > up || hidden(n, e, up, pos)) sc[n][e] = -INFINITY;
+            if (pos + 8 > up || hidden(n, e, up, pos + 8)) sc[n][2 + e] = -INFINITY;
           }
       }
       // a new reference where a weight would pass 2^8
@@ -567,7 +583,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
 #pragma unroll
                   for (int e = 0; e < 2; ++e) {
                     const int32_t up = sees_to(n * 8 + 2 * t4 + e);
-                    if (pos < cur.len && pos <= up && !(a.window && up != 0x7FFFFFFF && pos <= up - (int32_t)a.window)) acc[n][i][2 * half + e] += p[e] * __uint_as_float(v << 16);
+                    if (pos < cur.len && pos <= up && !hidden(n, e, up, pos)) acc[n][i][2 * half + e] += p[e] * __uint_as_float(v << 16);
                   }
                 }
             }

@@ -151,11 +151,11 @@ __device__ __forceinline__ ulonglong2 load_scales(uint32_t addr) {
 struct RowBlock {
   int32_t kt0, n;          // first tile of 128 cache rows; its length in the line: kItemCost and its tiles (at least one)
 };
-__device__ __forceinline__ RowBlock row_block(const KvSeq& q, uint32_t group, uint32_t window, uint32_t rb) {
+template <bool TREE> __device__ __forceinline__ RowBlock row_block(const KvSeq& q, uint32_t group, uint32_t window, uint32_t rb) {
   const uint32_t rows = (uint32_t)q.n_new * group, r0 = rb * kQRows, r1 = min(r0 + kQRows, rows);
   const int32_t base = q.len - q.n_new;
   const int32_t hi = base + (int32_t)((r1 - 1) / group);
-  const int32_t lo = window ? max(0, base + (int32_t)(r0 / group) - (int32_t)window + 1) : 0;
+  const int32_t lo = window ? max(0, TREE ? base - (int32_t)window : base + (int32_t)(r0 / group) - (int32_t)window + 1) : 0;
   RowBlock b;
   b.kt0 = lo / (int32_t)kKeys;
   b.n = kItemCost + max(1, (hi + (int32_t)kKeys) / (int32_t)kKeys - b.kt0);
@@ -193,7 +193,7 @@ __device__ __forceinline__ int32_t warp_inclusive(int32_t x) {
 }
 
 // The item that holds tile t; by a whole warp.
-__device__ __forceinline__ Walk walk_to(const AttendArgs& a, const int32_t* cum, uint32_t skip_rows, int32_t t) {
+template <bool TREE> __device__ __forceinline__ Walk walk_to(const AttendArgs& a, const int32_t* cum, uint32_t skip_rows, int32_t t) {
   Walk w;
   uint32_t lo = 0, hi = a.b.n_seqs;
   while (hi - lo > 1) {
@@ -211,7 +211,7 @@ __device__ __forceinline__ Walk walk_to(const AttendArgs& a, const int32_t* cum,
   const uint32_t lane = threadIdx.x & 31;
   for (uint32_t rb0 = 0;; rb0 += 32) {
     const uint32_t rb = rb0 + lane;
-    const int32_t n = rb < w.n_rb ? row_block(w.seq, a.group, a.window, rb).n : 0;
+    const int32_t n = rb < w.n_rb ? row_block<TREE>(w.seq, a.group, a.window, rb).n : 0;
     const int32_t inc = warp_inclusive(n);
     const uint32_t over = __ballot_sync(0xFFFFFFFFu, inc > rem);
     if (over || rb0 + 32 >= w.n_rb) {
@@ -222,11 +222,11 @@ __device__ __forceinline__ Walk walk_to(const AttendArgs& a, const int32_t* cum,
     }
     rem -= __shfl_sync(0xFFFFFFFFu, inc, 31);
   }
-  w.blk = row_block(w.seq, a.group, a.window, w.rb);
+  w.blk = row_block<TREE>(w.seq, a.group, a.window, w.rb);
   w.item0 = t - rem;
   return w;
 }
-__device__ __forceinline__ void walk_on(Walk& w, const AttendArgs& a, const int32_t* cum, uint32_t skip_rows) {
+template <bool TREE> __device__ __forceinline__ void walk_on(Walk& w, const AttendArgs& a, const int32_t* cum, uint32_t skip_rows) {
   w.item0 += w.blk.n;
   if (++w.rb == w.n_rb) {
     w.rb = 0;
@@ -237,14 +237,14 @@ __device__ __forceinline__ void walk_on(Walk& w, const AttendArgs& a, const int3
       w.n_rb = row_blocks(w.seq, a.group, skip_rows);
     }
   }
-  w.blk = row_block(w.seq, a.group, a.window, w.rb);
+  w.blk = row_block<TREE>(w.seq, a.group, a.window, w.rb);
 }
 
 // The beginning of block x's share.
-__device__ __forceinline__ int32_t share_begin(const AttendArgs& a, const int32_t* cum, uint32_t skip_rows, int32_t x, int32_t per, int32_t total) {
+template <bool TREE> __device__ __forceinline__ int32_t share_begin(const AttendArgs& a, const int32_t* cum, uint32_t skip_rows, int32_t x, int32_t per, int32_t total) {
   const int32_t t = x * per;
   if (t <= 0 || t >= total) return t <= 0 ? 0 : total;
-  const Walk w = walk_to(a, cum, skip_rows, t);
+  const Walk w = walk_to<TREE>(a, cum, skip_rows, t);
   if (t - w.item0 <= kItemCost + kSnap) return w.item0;
   if (w.item0 + w.blk.n - t <= kSnap) return w.item0 + w.blk.n;
   return t;
@@ -252,10 +252,12 @@ __device__ __forceinline__ int32_t share_begin(const AttendArgs& a, const int32_
 
 // Values that are not finite were taken out of a tile that not every row sees (of any tile, where a scale was not finite): a row that
 // does see one has it added here (its weight is positive, whatever it is).  Rare, so straight from the cache.
-template <bool Q>
-__device__ __noinline__ void add_odd_values(const AttendArgs& a, const Walk& w, int32_t kt_begin, int32_t kt_end, int32_t lo, int32_t hi, uint32_t d0,
-                                            float* o) {
+template <bool Q, bool TREE>
+__device__ __noinline__ void add_odd_values(const AttendArgs& a, const Walk& w, int32_t kt_begin, int32_t kt_end, int32_t lo, int32_t hi, uint32_t tok,
+                                            uint32_t d0, float* o) {
+  const int32_t first = w.seq.len - w.seq.n_new;
   for (int32_t pos = max(lo, kt_begin * (int32_t)kKeys); pos <= min(hi, kt_end * (int32_t)kKeys - 1); ++pos) {
+    if (TREE && !(tree_word(a, tok, (pos - first) >> 5) >> ((pos - first) & 31) & 1)) continue;
     const int32_t page = kv_page(a.b, a.c.n_pages, a.c.page_size, w.s, pos);
     if (page < 0) continue;
     const uint32_t slot = (uint32_t)pos % a.c.page_size;
@@ -278,7 +280,7 @@ struct RowOf {
   uint32_t tok, head;      // row and head of the step's tensors
   int32_t hi, lo;          // positions that it sees
 };
-__device__ __forceinline__ RowOf row_of(const AttendArgs& a, const Walk& w, uint32_t r0) {
+template <bool TREE> __device__ __forceinline__ RowOf row_of(const AttendArgs& a, const Walk& w, uint32_t r0) {
   RowOf x;
   const uint32_t n_rows = (uint32_t)w.seq.n_new * a.group, r = w.rb * kQRows + r0;
   x.in = r < n_rows;
@@ -286,7 +288,9 @@ __device__ __forceinline__ RowOf row_of(const AttendArgs& a, const Walk& w, uint
   x.head = w.h * a.group + (x.in ? r - x.tok * a.group : 0);
   x.hi = w.seq.len - w.seq.n_new + (int32_t)x.tok;
   x.lo = a.window ? x.hi - (int32_t)a.window + 1 : 0;
+  const int32_t i = (int32_t)x.tok;
   x.tok += (uint32_t)w.seq.row0;
+  if (TREE) x.lo = tree_low(a, w.seq, x.tok, i);
   return x;
 }
 
@@ -344,7 +348,7 @@ __device__ __forceinline__ bool clear_values(char* tile, uint32_t row, bool past
 }
 
 
-template <int D, bool Q>
+template <int D, bool Q, bool TREE>
 __global__ void __launch_bounds__(TilesCfg<D, Q>::kThreads, 1)
 wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                        uint32_t skip_rows) {
@@ -396,7 +400,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
     const KvSeq q = attend_seq(a.b, s);
     const uint32_t nb = row_blocks(q, a.group, skip_rows);
     int32_t sum = 0;
-    for (uint32_t rb = lane; rb < nb; rb += 32) sum += row_block(q, a.group, a.window, rb).n;
+    for (uint32_t rb = lane; rb < nb; rb += 32) sum += row_block<TREE>(q, a.group, a.window, rb).n;
     sum = __reduce_add_sync(0xFFFFFFFFu, sum);
     if (lane == 0) {
       cum[s + 1] = sum * (int32_t)hk;
@@ -424,7 +428,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
   const int32_t total = cum[n_seqs];
   const int32_t per = (total + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
   if (warp < 2) {
-    const int32_t t = share_begin(a, cum, skip_rows, (int32_t)(blockIdx.x + warp), per, total);
+    const int32_t t = share_begin<TREE>(a, cum, skip_rows, (int32_t)(blockIdx.x + warp), per, total);
     if (lane == 0) misc[5 + warp] = (uint32_t)t;
   }
   __syncthreads();
@@ -443,8 +447,8 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       uint32_t jg = 0, item = 0;                    // steps and items of the block so far
       uint32_t js = 0, is = 0;                      // those that this tile took part in
       bool ok = true;
-      Walk w = walk_to(a, cum, skip_rows, begin);
-      RowOf x0 = row_of(a, w, i * 128 + row);
+      Walk w = walk_to<TREE>(a, cum, skip_rows, begin);
+      RowOf x0 = row_of<TREE>(a, w, i * 128 + row);
       const uint32_t q_tile = base + i * C::kSlotBytes, warp_row = (warp & 3) * 32;
       copy_queries<D>(a, q_tile, warp_row, x0);
       queries_arrived();
@@ -456,18 +460,20 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         const uint32_t n_rows = (uint32_t)w.seq.n_new * a.group;
         const int32_t base_pos = w.seq.len - w.seq.n_new;
         // tiles that not every row of the block sees whole
-        const int32_t cut_hi = base_pos + (int32_t)(w.rb * kQRows / a.group);
+        const int32_t cut_hi = TREE ? base_pos - 1 : base_pos + (int32_t)(w.rb * kQRows / a.group);
         const int32_t cut_lo = a.window ? base_pos + (int32_t)((min(n_rows, (w.rb + 1) * kQRows) - 1) / a.group) - (int32_t)a.window + 1 : 0;
         // rows of a warp are in the order of their tokens: its first row sees the least far, its last row's window begins last
-        const int32_t warp_hi = __shfl_sync(0xFFFFFFFFu, x0.hi, 0), warp_lo = a.window ? __shfl_sync(0xFFFFFFFFu, x0.lo, 31) : 0;
+        // (in a tree, any row may not see any of the new rows)
+        const int32_t warp_hi = TREE ? base_pos - 1 : __shfl_sync(0xFFFFFFFFu, x0.hi, 0);
+        const int32_t warp_lo = !a.window ? 0 : TREE ? __reduce_max_sync(0xFFFFFFFFu, x0.lo) : __shfl_sync(0xFFFFFFFFu, x0.lo, 31);
         const bool takes_part = i == 0 || n_rows > w.rb * kQRows + 128;
         if (tid == 0) misc[8 + (item + 5) % 8] = 0;     // that of three items ago: the other tile is at most one behind, nobody five ahead
         Walk w2 = w;                                // the next item, once this one's last scores are there
         RowOf x2 = x0;
         // the scores of this item are done with: the next one's queries take their place while its last weights are computed
         auto prepare_next = [&]() {
-          walk_on(w2, a, cum, skip_rows);
-          x2 = row_of(a, w2, i * 128 + row);
+          walk_on<TREE>(w2, a, cum, skip_rows);
+          x2 = row_of<TREE>(a, w2, i * 128 + row);
           copy_queries<D>(a, q_tile, warp_row, x2);
         };
         // the score that the weights are relative to (differences are formed before they are scaled: scores of any finite size
@@ -521,7 +527,11 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             for (int c = 0; c < 128; c += 32) {
               if (pos0 + c + 31 <= warp_hi && pos0 + c >= warp_lo) continue;
               const int32_t up = min(max(h1 - c, 0), 32), low = min(max(l1 - c, 0), 32);
-              const uint32_t bits = (uint32_t)((1ull << up) - 1) & ~(uint32_t)((1ull << low) - 1);
+              uint32_t bits = (uint32_t)((1ull << up) - 1) & ~(uint32_t)((1ull << low) - 1);
+              if (TREE) {
+                const int32_t j = pos0 + c - base_pos;      // the first column's row of the tree
+                bits &= __funnelshift_r(tree_word(a, x0.tok, j >> 5), tree_word(a, x0.tok, (j >> 5) + 1), j & 31);
+              }
 #pragma unroll
               for (int e = 0; e < 32; ++e) x[c + e] = bits & 1u << e ? x[c + e] : -INFINITY;
             }
@@ -626,7 +636,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               float y[32];
 #pragma unroll
               for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(o[e]);
-              add_odd_values<Q>(a, w, w.blk.kt0 + from - tile0, w.blk.kt0 + stop - tile0, x0.lo, x0.hi, c, y);
+              add_odd_values<Q, TREE>(a, w, w.blk.kt0 + from - tile0, w.blk.kt0 + stop - tile0, x0.lo, x0.hi, x0.tok, c, y);
 #pragma unroll
               for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(y[e]);
             }
@@ -695,7 +705,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             tc_mma_ts(tm + 256 + i * 128, tm + i * 128 + ks * 8, vd + (ks * 2048 >> 4), kPv, ks > 0 ? 1u : add, leader);
           }
         };
-        Walk w = walk_to(a, cum, skip_rows, begin);
+        Walk w = walk_to<TREE>(a, cum, skip_rows, begin);
         for (int32_t t = uniform(begin); t < t_end; ++item) {
           const int32_t stop = uniform(min(end, w.item0 + w.blk.n));
           t = uniform(max(t, w.item0 + kItemCost));
@@ -719,7 +729,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             tc_commit(empty + 8 * ((2 * jg + 1) % C::kSlots), leader);
             if (more) tc_commit(empty + 8 * ((2 * jg + 2) % C::kSlots), leader);
           }
-          if (t < t_end) walk_on(w, a, cum, skip_rows);
+          if (t < t_end) walk_on<TREE>(w, a, cum, skip_rows);
         }
         // the last commit arrives before the block ends (waited for even after a wait that gave up)
         (void)wait_or_give_up(empty + 8 * ((2 * jg - 1) % C::kSlots), ((2 * jg - 1) / C::kSlots) & 1, true, a.error);
@@ -729,7 +739,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         const uint32_t pieces = kKeys / a.box_rows;
         uint32_t jg = 0;
         bool ok = true;
-        Walk w = walk_to(a, cum, skip_rows, begin);
+        Walk w = walk_to<TREE>(a, cum, skip_rows, begin);
         for (int32_t t = begin; t < end;) {
           const int32_t stop = min(end, w.item0 + w.blk.n), tile0 = w.item0 + kItemCost;
           for (t = max(t, tile0); t < stop; ++t, ++jg) {
@@ -765,7 +775,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               }
             }
           }
-          if (t < end) walk_on(w, a, cum, skip_rows);
+          if (t < end) walk_on<TREE>(w, a, cum, skip_rows);
         }
         // every load lands before the block ends, also where the others gave up waiting and left some unread
         const uint32_t n = 2 * jg, ring = Q ? C::kRaws : C::kSlots;
@@ -779,7 +789,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kOtherRegs));
       const uint32_t row = tid & 127;
       bool ok = true;
-      Walk w = walk_to(a, cum, skip_rows, begin);
+      Walk w = walk_to<TREE>(a, cum, skip_rows, begin);
       int32_t t = begin;
       uint32_t item = 0;
       for (uint32_t q = 0; t < end; ++q) {
@@ -796,7 +806,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             *at = 0.f;                // (ordered before the next load into the same place by the fence below: see kScaleSlots)
           }
           if (++t == min(end, w.item0 + w.blk.n) && t < end) {
-            walk_on(w, a, cum, skip_rows);
+            walk_on<TREE>(w, a, cum, skip_rows);
             ++item;
           }
         }
@@ -845,7 +855,7 @@ __global__ void __launch_bounds__(256) wb_attend_join_kernel(const __grid_consta
   w.h = it.h;
   w.rb = it.rb;
   const uint32_t r = blockIdx.y * 32 + lane;
-  const RowOf row = row_of(a, w, r);
+  const RowOf row = row_of<false>(a, w, r);      // (of which only its place in the step's tensors matters here)
   if (!__any_sync(0xFFFFFFFFu, row.in)) return;
   const float* parts = a.partials + (r >> 7) * (D * 128 + 256) + (r & 127);
   auto part_of = [&](uint32_t p) { return parts + (size_t)(2 * (x + p) + (p == 0 ? 1 : 0)) * kPart; };
