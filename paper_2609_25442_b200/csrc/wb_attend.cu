@@ -77,10 +77,10 @@ cudaError_t launch_rows_of(uint32_t rows, const AttendArgs& a, int dev, cudaStre
   return launch_rows<D, Q, 4, TREE>(a, dev, stream);
 }
 
-template <int D, bool Q, bool TREE>
+template <int D, bool Q, Rows256 MODE>
 cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_rows, cudaStream_t stream) {
   using C = TilesCfg<D, Q>;
-  auto kernel = wb_attend_tiles_kernel<D, Q, TREE>;
+  auto kernel = wb_attend_tiles_kernel<D, Q, MODE>;
   // the softmax warps wait for registers that the others give back: the launch has to have them
   static std::atomic<uint64_t> done{0};
   cudaError_t e = prepare_kernel(kernel, C::kSmemBytes, C::kLaunchRegs, kv->device, done);
@@ -93,7 +93,7 @@ cudaError_t launch_tiles(const AttendArgs& all, const wb_kv* kv, uint32_t skip_r
     a.b.kv_len += s0;
     kernel<<<kNumSMs, C::kThreads, C::kSmemBytes, stream>>>(a, kv->map_k, kv->map_v, skip_rows);
     if ((e = cudaPeekAtLastError()) != cudaSuccess) return e;
-    if ((e = launch_join(wb_attend_join_kernel<D>, dim3(kNumSMs, kQRows / 32), 256, a, stream)) != cudaSuccess) return e;
+    if ((e = launch_join(wb_attend_join_kernel<D>, dim3(kNumSMs, (MODE == Rows256::kTreeShared ? kQRows / 2 : kQRows) / 32), 256, a, stream)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
@@ -152,19 +152,27 @@ wb_status attend_args(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads*
   return WB_OK;
 }
 
+template <Rows256 MODE> cudaError_t launch_tiles_of(const AttendArgs& a, const wb_kv* kv, uint32_t skip_rows, cudaStream_t stream) {
+  const bool q = kv->d.dtype == WB_E4M3;
+  if (kv->d.head_dim == 128) return q ? launch_tiles<128, true, MODE>(a, kv, skip_rows, stream) : launch_tiles<128, false, MODE>(a, kv, skip_rows, stream);
+  return q ? launch_tiles<64, true, MODE>(a, kv, skip_rows, stream) : launch_tiles<64, false, MODE>(a, kv, skip_rows, stream);
+}
+
 template <bool TREE> wb_status launch_attend(const AttendArgs& a, const wb_kv* kv, const wb_kv_batch* batch, cudaStream_t st) {
   const bool e = kv->d.dtype == WB_E4M3;
   const uint64_t rows = (uint64_t)batch->max_new * a.group;
   cudaError_t err = cudaSuccess;
-  if (rows <= kMaxRows || batch->n_seqs > 1) {
+  // (a batch of trees is of a kind: sequences with few rows go with the others instead of costing two launches of their own)
+  const bool mixed = !TREE && batch->n_seqs > 1;
+  if (rows <= kMaxRows || mixed) {
     const uint32_t r = (uint32_t)std::min<uint64_t>(rows, kMaxRows);
     if (kv->d.head_dim == 128) err = e ? launch_rows_of<128, true, TREE>(r, a, kv->device, st) : launch_rows_of<128, false, TREE>(r, a, kv->device, st);
     else err = e ? launch_rows_of<64, true, TREE>(r, a, kv->device, st) : launch_rows_of<64, false, TREE>(r, a, kv->device, st);
   }
   if (err == cudaSuccess && rows > kMaxRows) {
-    const uint32_t skip = batch->n_seqs > 1 ? kMaxRows : 0;
-    if (kv->d.head_dim == 128) err = e ? launch_tiles<128, true, TREE>(a, kv, skip, st) : launch_tiles<128, false, TREE>(a, kv, skip, st);
-    else err = e ? launch_tiles<64, true, TREE>(a, kv, skip, st) : launch_tiles<64, false, TREE>(a, kv, skip, st);
+    const uint32_t skip = mixed ? kMaxRows : 0;
+    constexpr Rows256 kMode = TREE ? Rows256::kTree : Rows256::kChunk;
+    err = TREE && rows <= kQRows / 2 ? launch_tiles_of<Rows256::kTreeShared>(a, kv, skip, st) : launch_tiles_of<kMode>(a, kv, skip, st);
   }
   if (err != cudaSuccess) (void)cudaGetLastError();
   return err == cudaSuccess ? WB_OK : WB_ERR_CUDA;

@@ -107,6 +107,13 @@ __device__ __forceinline__ void tm_store16(uint32_t addr, const uint32_t* r) {
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
                "r"(r[14]), "r"(r[15]), "r"(addr) : "memory");
 }
+// two columns
+__device__ __forceinline__ void tm_store2(uint32_t addr, float x, float y) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x2.b32 [%0], {%1, %2};" ::"r"(addr), "f"(x), "f"(y) : "memory");
+}
+__device__ __forceinline__ void tm_load2(uint32_t addr, float& x, float& y) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x2.b32 {%0, %1}, [%2];" : "=f"(x), "=f"(y) : "r"(addr));
+}
 __device__ __forceinline__ void tm_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -147,6 +154,19 @@ __device__ __forceinline__ ulonglong2 load_scales(uint32_t addr) {
   return f;
 }
 
+// What the rows are: a chunk's, a tree's, or trees' of at most one tile of rows each.  Of those, both groups of softmax warps hold the
+// same rows, and the cache tiles are shared out between them: each takes every other one, at the end they add up what they have.
+enum class Rows256 { kChunk, kTree, kTreeShared };
+
+// The order in which an item's n cache tiles are loaded and used: keys and values in turn, or, where the two groups of softmax warps
+// take them alternately, keys two ahead of values: K0 K1 V0 K2 V1 ... V(n-1).  A tile's load, counted from the item's first, and back.
+__device__ __forceinline__ uint32_t key_load(bool shared, uint32_t j) { return shared ? (j ? 2 * j - 1 : 0) : 2 * j; }
+__device__ __forceinline__ uint32_t value_load(bool shared, uint32_t j, uint32_t n) { return shared ? min(2 * j + 2, 2 * n - 1) : 2 * j + 1; }
+__device__ __forceinline__ bool load_is_value(bool shared, uint32_t r, uint32_t n) { return shared ? r == 2 * n - 1 || (r != 0 && (r & 1) == 0) : r & 1; }
+__device__ __forceinline__ uint32_t load_tile(bool shared, uint32_t r, uint32_t n) {
+  return !shared ? r >> 1 : r == 2 * n - 1 ? n - 1 : load_is_value(true, r, n) ? (r - 2) >> 1 : (r + 1) >> 1;
+}
+
 // ---- geometry -----------------------------------------------------------------------------------
 struct RowBlock {
   int32_t kt0, n;          // first tile of 128 cache rows; its length in the line: kItemCost and its tiles (at least one)
@@ -166,6 +186,17 @@ __device__ __forceinline__ uint32_t row_blocks(const KvSeq& q, uint32_t group, u
   return rows > skip_rows ? (uint32_t)((rows + kQRows - 1) / kQRows) : 0;
 }
 
+// Where a block is in the line of tiles; every warp walks it alike.
+struct Walk {
+  uint32_t s, h, rb, n_rb;
+  KvSeq seq;
+  RowBlock blk;
+  int32_t item0;           // the item's first tile in the line
+};
+
+// Whether an item's rows are one tile.
+__device__ __forceinline__ bool one_tile(const Walk& w, uint32_t group) { return (uint32_t)w.seq.n_new * group <= w.rb * kQRows + 128; }
+
 // A block's share of the line begins at the multiple of `per` that is its number, moved to the next end of an item where that is
 // not more than kSnap tiles away: joining a cut item costs more than so many tiles.  So an item [i0, i1) is cut at the multiples
 // of `per` that lie more than kSnap tiles inside.
@@ -174,14 +205,6 @@ __device__ __forceinline__ int32_t cuts_of(int32_t i0, int32_t i1, int32_t per) 
   const int32_t lo = (i0 + kItemCost + kSnap + per) / per, hi = (i1 - kSnap - 1) / per;    // multiples in (i0 + kItemCost + kSnap, i1 - kSnap)
   return max(0, hi - lo + 1);
 }
-
-// Where a block is in the line of tiles; every warp walks it alike.
-struct Walk {
-  uint32_t s, h, rb, n_rb;
-  KvSeq seq;
-  RowBlock blk;
-  int32_t item0;           // the item's first tile in the line
-};
 
 __device__ __forceinline__ int32_t warp_inclusive(int32_t x) {
 #pragma unroll
@@ -348,11 +371,12 @@ __device__ __forceinline__ bool clear_values(char* tile, uint32_t row, bool past
 }
 
 
-template <int D, bool Q, bool TREE>
+template <int D, bool Q, Rows256 MODE>
 __global__ void __launch_bounds__(TilesCfg<D, Q>::kThreads, 1)
 wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                        uint32_t skip_rows) {
   using C = TilesCfg<D, Q>;
+  constexpr bool TREE = MODE != Rows256::kChunk, SHARED = MODE == Rows256::kTreeShared;
   extern __shared__ __align__(1024) char smem[];
   const uint32_t base = smem_addr(smem);
   const uint32_t tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
@@ -445,10 +469,10 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       const uint32_t tm_s = tm_lane + i * 128, tm_o = tm_lane + 256 + i * 128;
       const float c2 = a.scale_log2;
       uint32_t jg = 0, item = 0;                    // steps and items of the block so far
-      uint32_t js = 0, is = 0;                      // those that this tile took part in
+      uint32_t js = 0, is = 0, io = 0;              // those that this tile took part in; items that the other one did
       bool ok = true;
       Walk w = walk_to<TREE>(a, cum, skip_rows, begin);
-      RowOf x0 = row_of<TREE>(a, w, i * 128 + row);
+      RowOf x0 = row_of<TREE>(a, w, (SHARED ? 0 : i * 128) + row);
       const uint32_t q_tile = base + i * C::kSlotBytes, warp_row = (warp & 3) * 32;
       copy_queries<D>(a, q_tile, warp_row, x0);
       queries_arrived();
@@ -466,39 +490,42 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         // (in a tree, any row may not see any of the new rows)
         const int32_t warp_hi = TREE ? base_pos - 1 : __shfl_sync(0xFFFFFFFFu, x0.hi, 0);
         const int32_t warp_lo = !a.window ? 0 : TREE ? __reduce_max_sync(0xFFFFFFFFu, x0.lo) : __shfl_sync(0xFFFFFFFFu, x0.lo, 31);
-        const bool takes_part = i == 0 || n_rows > w.rb * kQRows + 128;
+        const bool takes_part = SHARED || i == 0 || !one_tile(w, a.group);
+        const uint32_t n_tiles = (uint32_t)(stop - t), q0 = 2 * jg;
+        jg += n_tiles;
         if (tid == 0) misc[8 + (item + 5) % 8] = 0;     // that of three items ago: the other tile is at most one behind, nobody five ahead
         Walk w2 = w;                                // the next item, once this one's last scores are there
         RowOf x2 = x0;
         // the scores of this item are done with: the next one's queries take their place while its last weights are computed
         auto prepare_next = [&]() {
           walk_on<TREE>(w2, a, cum, skip_rows);
-          x2 = row_of<TREE>(a, w2, i * 128 + row);
+          x2 = row_of<TREE>(a, w2, (SHARED ? 0 : i * 128) + row);
           copy_queries<D>(a, q_tile, warp_row, x2);
         };
         // the score that the weights are relative to (differences are formed before they are scaled: scores of any finite size
         // give weights of 2^8 and less), and that above which it moves
         float ref = 0.f, limit = -INFINITY;
         uint64_t sum2[2] = {0, 0};
-        for (bool first = true; t < stop; ++t, ++jg, first = false) {
-          const uint32_t sk = (2 * jg) % C::kScaleSlots, sv = sk + 1;
+        bool first = true;
+        for (uint32_t j = SHARED ? i : 0; j < n_tiles; j += SHARED ? 2 : 1, first = false) {
+          const uint32_t qk = q0 + key_load(SHARED, j), qv = q0 + value_load(SHARED, j, n_tiles), sk = qk % C::kScaleSlots, sv = qv % C::kScaleSlots;
           if (!takes_part) {                        // keeps the pace of the scales' ring
             if (Q) {
-              ok = wait_or_give_up(scale_ready + 8 * sk, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
-              ok = wait_or_give_up(scale_ready + 8 * sv, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
+              ok = wait_or_give_up(scale_ready + 8 * sk, (qk / C::kScaleSlots) & 1, ok, a.error);
+              ok = wait_or_give_up(scale_ready + 8 * sv, (qv / C::kScaleSlots) & 1, ok, a.error);
               bar_arrive(scale_empty + 8 * sk);
               bar_arrive(scale_empty + 8 * sv);
             }
             continue;
           }
-          const int32_t pos0 = (w.blk.kt0 + t - tile0) * (int32_t)kKeys;
+          const int32_t pos0 = (w.blk.kt0 + from + (int32_t)j - tile0) * (int32_t)kKeys;
           const bool cut = pos0 + (int32_t)kKeys - 1 > cut_hi || pos0 < cut_lo;
-          if (!Q && cut && i == 0) {
+          if (!Q && cut && (i == 0 || SHARED)) {
             // Values past the end, and values that are not finite, must not meet weights of zero.  Only the first tile's threads
-            // write, one to a row: each then orders its own writes before the products, which wait for this tile's
-            // weights first, and the other tile's products follow this one's.
-            const uint32_t vq = 2 * jg + 1, slot = vq % C::kSlots;
-            ok = wait_or_give_up(full + 8 * slot, (vq / C::kSlots) & 1, ok, a.error);
+            // (those that alone use the cache tile, where tiles are shared out) write, one to a row: each then orders its own writes before
+            // the products, which wait for this tile's weights first, and the other tile's products follow this one's.
+            const uint32_t slot = qv % C::kSlots;
+            ok = wait_or_give_up(full + 8 * slot, (qv / C::kSlots) & 1, ok, a.error);
             if (clear_values<D>(smem + C::kOffSlots + slot * C::kSlotBytes, row, pos0 + (int32_t)row >= w.seq.len, misc + 8 + item % 8)) fence_async();
           }
           float x[128];
@@ -507,10 +534,10 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           tc_after();
 #pragma unroll
           for (int c = 0; c < 128; c += 32) tm_load32(tm_s + c, reinterpret_cast<uint32_t*>(x) + c);
-          if (t + 1 == stop && stop < end) prepare_next();
+          if (j + (SHARED ? 2 : 1) >= n_tiles && stop < end) prepare_next();
           tm_wait_load();
           if (Q) {
-            ok = wait_or_give_up(scale_ready + 8 * sk, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
+            ok = wait_or_give_up(scale_ready + 8 * sk, (qk / C::kScaleSlots) & 1, ok, a.error);
             const uint32_t scales = base + C::kOffScale + sk * (kKeys * 4);
 #pragma unroll
             for (int c = 0; c < 128; c += 4) {
@@ -568,7 +595,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               }
             }
           }
-          if (Q) ok = wait_or_give_up(scale_ready + 8 * sv, (2 * jg / C::kScaleSlots) & 1, ok, a.error);
+          if (Q) ok = wait_or_give_up(scale_ready + 8 * sv, (qv / C::kScaleSlots) & 1, ok, a.error);
           const uint64_t c22 = pack2(c2, c2), ref2 = pack2(-ref, -ref);
           const uint32_t vscales = base + C::kOffScale + sv * (kKeys * 4);
 #pragma unroll
@@ -602,35 +629,74 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             bar_arrive(p_full + 8 * i);
           }
           if (Q) {
-            bar_arrive(scale_empty + 8 * sk);
-            bar_arrive(scale_empty + 8 * sv);
+            bar_arrive_n(scale_empty + 8 * sk, SHARED ? 2 : 1);      // for the other group's threads too, which do not read them
+            bar_arrive_n(scale_empty + 8 * sv, SHARED ? 2 : 1);
           }
         }
+        t = stop;
+        float m2 = -INFINITY, l2 = 0.f;               // the other group's maximum and sum, where tiles are shared out
+        float l, l1;
+        unpack2(add2(sum2[0], sum2[1]), l, l1);
+        l += l1;
+        const float m = l == 0.f ? -INFINITY : ref * c2;
+        if (SHARED) {      // they change hands in columns of the scores that weights do not reach; a row has the same lane in both groups
+          tm_store2(tm_s + 64, m, l);
+          tm_wait_store();
+          tc_before();
+        }
         if (t < end) {
-          if (!takes_part) prepare_next();
+          if (!takes_part || (SHARED && i >= n_tiles)) prepare_next();
           queries_arrived();
+        }
+        if (t < end || SHARED) {
           // Neither tile's warps get an item ahead of the other's: a tile that takes no part in an item has nothing to wait for, and
           // its arrivals for the items after would stand in for the other's.
           asm volatile("bar.sync 1, 256;" ::: "memory");
-          bar_arrive(q_full);
+          if (SHARED) {
+            tc_after();
+            tm_load2(tm_lane + (1 - i) * 128 + 64, m2, l2);
+            tm_wait_load();
+            tc_before();
+          }
+          if (t < end) bar_arrive(q_full);
         }
         // ---- outputs ---------------------------------------------------------------------------------
+        // A thread writes its row; where tiles were shared out, both threads of a row add up what their groups have, each in half of
+        // the columns (a group that had no tile has nothing, not even zeros: what is read is not used).
         if (takes_part) {
-          float l, l1;
-          unpack2(add2(sum2[0], sum2[1]), l, l1);
-          l += l1;
-          ok = wait_or_give_up(o_full + 8 * i, is & 1, ok, a.error);
-          ++is;
+          const uint32_t here = i < n_tiles || !SHARED, there = SHARED && 1 - i < n_tiles;
+          if (here) {
+            ok = wait_or_give_up(o_full + 8 * i, is & 1, ok, a.error);
+            ++is;
+          }
+          if (there) ok = wait_or_give_up(o_full + 8 * (1 - i), io & 1, ok, a.error);
+          if (there) ++io;
           tc_after();
           const bool odd = misc[8 + item % 8] != 0;
           const int32_t cuts = cuts_of(w.item0, item1, per);
           char* dst = a.out + (uint64_t)x0.tok * a.o_token + x0.head * a.o_head;
-          float* part = a.partials + (size_t)(2 * blockIdx.x + (w.item0 >= begin ? 1 : 0)) * C::kPartFloats + i * (D * 128 + 256) + row;
+          float* part = a.partials + (size_t)(2 * blockIdx.x + (w.item0 >= begin ? 1 : 0)) * C::kPartFloats + (SHARED ? 0 : i * (D * 128 + 256)) + row;
+          float top = m, f = 1.f, f2 = 0.f;
+          if (SHARED) {
+            top = fmaxf(m, m2);
+            f = m == -INFINITY ? 0.f : fast_exp2(m - top);
+            f2 = m2 == -INFINITY ? 0.f : fast_exp2(m2 - top);
+            l = i ? __fmaf_rn(l, f, __fmul_rn(l2, f2)) : __fmaf_rn(l2, f2, __fmul_rn(l, f));      // (the same in both)
+          }
           const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+          const int c_begin = SHARED ? (int)i * (D / 2) : 0, c_end = SHARED ? c_begin + D / 2 : D;
 #pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
+          for (int c = c_begin; c < c_end; c += 32) {
             uint32_t o[32];
             tm_load32(tm_o + c, o);
+            if (SHARED) {
+              uint32_t y[32];
+              tm_load32(tm_lane + 256 + (1 - i) * 128 + c, y);
+              tm_wait_load();
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                o[e] = __float_as_uint((here ? __uint_as_float(o[e]) * f : 0.f) + (there ? __uint_as_float(y[e]) * f2 : 0.f));
+            }
             tm_wait_load();
             if (odd && x0.in) {
               float y[32];
@@ -656,13 +722,19 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             }
           }
           if (cuts == 0) {
-            if (x0.in && a.lse)
-              a.lse[(uint64_t)x0.tok * a.n_heads + x0.head] = l == 0.f ? -INFINITY : (ref * c2 + log2f(l)) * kLn2;
+            if (x0.in && a.lse && (i == 0 || !SHARED))
+              a.lse[(uint64_t)x0.tok * a.n_heads + x0.head] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
           } else {
-            part[D * 128] = l == 0.f ? -INFINITY : ref * c2;
-            part[D * 128 + 128] = l;
+            if (i == 0 || !SHARED) {
+              part[D * 128] = l == 0.f ? -INFINITY : top;
+              part[D * 128 + 128] = l;
+            }
             if (tid == 0 && w.item0 >= begin) *cut_item = CutItem{(uint32_t)cuts + 1, w.s, w.h, w.rb};
           }
+        }
+        if (SHARED) {      // neither group's next products take the place of what the other still reads
+          tc_before();
+          asm volatile("bar.sync 1, 256;" ::: "memory");
         }
         w = w2;
         x0 = x2;
@@ -675,7 +747,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         constexpr uint32_t kQk = kF32Bf16 | (kKeys / 8) << 17, kPv = kF32Bf16 | 1u << 16 | (uint32_t)(D / 8) << 17;
         const uint32_t leader = lane == 0, tm = uniform(tmem);
         const int32_t t_end = uniform(end);
-        uint32_t jg = 0, item = 0, js = 0;          // steps, items, steps of the second tile
+        uint32_t jg = 0, item = 0, j0 = 0, js = 0;  // steps, items, steps of the first and the second tile
         bool ok = true;
         auto wait_all = [&](uint32_t bar, uint32_t parity) {
           ok = wait_or_give_up(bar, parity, ok, a.error);
@@ -711,6 +783,28 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           t = uniform(max(t, w.item0 + kItemCost));
           const uint32_t two = uniform((uint32_t)((uint32_t)w.seq.n_new * a.group > w.rb * kQRows + 128));
           wait_all(q_full, item & 1);
+          if (SHARED) {      // cache tiles are shared out between the two groups of softmax warps, each with a copy of the queries
+            const uint32_t n = uniform((uint32_t)(stop - t)), q0 = 2 * jg;
+            for (uint32_t g = 0; g < min(n, 2u); ++g) {
+              scores(g, slot_wait(q0 + g));
+              tc_commit(empty + 8 * ((q0 + g) % C::kSlots), leader);
+            }
+            for (uint32_t j = 0; j < n; ++j) {
+              const uint32_t g = j & 1, qv = q0 + value_load(true, j, n), qk = q0 + key_load(true, j + 2);
+              values(g, slot_wait(qv), j >= 2, g ? js : j0);
+              if (g) ++js; else ++j0;
+              if (j + 2 >= n) tc_commit(o_full + 8 * g, leader);
+              tc_commit(empty + 8 * (qv % C::kSlots), leader);
+              if (j + 2 < n) {
+                scores(g, slot_wait(qk));
+                tc_commit(empty + 8 * (qk % C::kSlots), leader);
+              }
+            }
+            jg += n;
+            t = stop;
+            if (t < t_end) walk_on<TREE>(w, a, cum, skip_rows);
+            continue;
+          }
           uint32_t k_addr = slot_wait(2 * jg);
           scores(0, k_addr);
           if (two) scores(1, k_addr);
@@ -719,7 +813,8 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             const uint32_t v_addr = slot_wait(2 * jg + 1);
             const bool more = t + 1 < stop;
             if (more) k_addr = slot_wait(2 * jg + 2);
-            values(0, v_addr, add, jg);
+            values(0, v_addr, add, j0);
+            ++j0;
             if (more) scores(0, k_addr); else tc_commit(o_full, leader);
             if (two) {
               values(1, v_addr, add, js);
@@ -742,39 +837,46 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         Walk w = walk_to<TREE>(a, cum, skip_rows, begin);
         for (int32_t t = begin; t < end;) {
           const int32_t stop = min(end, w.item0 + w.blk.n), tile0 = w.item0 + kItemCost;
-          for (t = max(t, tile0); t < stop; ++t, ++jg) {
-            const int32_t pos = (w.blk.kt0 + t - tile0) * (int32_t)kKeys + (int32_t)(lane * a.box_rows);
+          t = max(t, tile0);
+          const uint32_t n = (uint32_t)(stop - t);
             int32_t page = -1;
-            if (lane < pieces && pos < w.seq.len) page = kv_page(a.b, a.c.n_pages, a.c.page_size, w.s, pos);
-            const uint32_t in_page = (uint32_t)pos % a.c.page_size, r0 = lane * a.box_rows;
+          uint32_t in_page = 0;
+          const uint32_t r0 = lane * a.box_rows;
+          for (uint32_t r = 0; r < 2 * n; ++r) {
+            const bool kv = load_is_value(SHARED, r, n);
+            if (!kv || SHARED) {      // (a tile's values follow its keys otherwise)
+              const int32_t pos = (w.blk.kt0 + t + (int32_t)load_tile(SHARED, r, n) - tile0) * (int32_t)kKeys + (int32_t)r0;
+              page = -1;
+              if (lane < pieces && pos < w.seq.len) page = kv_page(a.b, a.c.n_pages, a.c.page_size, w.s, pos);
+              in_page = (uint32_t)pos % a.c.page_size;
+            }
             const int32_t where = page < 0 ? (int32_t)a.c.n_pages : page;      // outside the cache: zeros
+            const uint32_t q = 2 * jg + r, ring = Q ? C::kRaws : C::kSlots, slot = q % ring, sc = q % C::kScaleSlots;
+            const uint32_t bar = (Q ? raw_full : full) + 8 * slot, sbar = scale_full + 8 * sc;
+            if (q >= ring) ok = wait_or_give_up((Q ? raw_empty : empty) + 8 * slot, (q / ring + 1) & 1, ok, a.error);
+            if (Q && q >= C::kScaleSlots) ok = wait_or_give_up(scale_empty + 8 * sc, (q / C::kScaleSlots + 1) & 1, ok, a.error);
+            const uint32_t dst = base + (Q ? C::kOffRaw + slot * C::kRawBytes : C::kOffSlots + slot * C::kSlotBytes);
+            if (lane < pieces) {
+              bar_arrive_tx(bar, a.box_rows * D * (Q ? 1 : 2));
 #pragma unroll
-            for (uint32_t kv = 0; kv < 2; ++kv) {
-              const uint32_t q = 2 * jg + kv, ring = Q ? C::kRaws : C::kSlots, slot = q % ring, sc = q % C::kScaleSlots;
-              const uint32_t bar = (Q ? raw_full : full) + 8 * slot, sbar = scale_full + 8 * sc;
-              if (q >= ring) ok = wait_or_give_up((Q ? raw_empty : empty) + 8 * slot, (q / ring + 1) & 1, ok, a.error);
-              if (Q && q >= C::kScaleSlots) ok = wait_or_give_up(scale_empty + 8 * sc, (q / C::kScaleSlots + 1) & 1, ok, a.error);
-              const uint32_t dst = base + (Q ? C::kOffRaw + slot * C::kRawBytes : C::kOffSlots + slot * C::kSlotBytes);
-              if (lane < pieces) {
-                bar_arrive_tx(bar, a.box_rows * D * (Q ? 1 : 2));
-#pragma unroll
-                for (uint32_t e = 0; e < C::kRowSpans; ++e)
-                  load_box(dst + e * (kKeys * C::kRowSpan) + r0 * C::kRowSpan, kv ? &map_v : &map_k, (int32_t)(e * 64), (int32_t)in_page, (int32_t)w.h, where, bar);
-                if (Q && page >= 0) {
-                  bar_arrive_tx(sbar, a.box_rows * 4);
-                  load_bulk(base + C::kOffScale + (sc * kKeys + r0) * 4, (kv ? a.c.v_scale : a.c.k_scale) + ((uint64_t)page * hk + w.h) * a.c.page_size + in_page,
-                            a.box_rows * 4, sbar);
-                } else if (Q) {
-                  for (uint32_t e = 0; e < a.box_rows; ++e) reinterpret_cast<float*>(smem + C::kOffScale)[sc * kKeys + r0 + e] = 0.f;
-                  fence_async();      // before this lane's next load into the same place
-                  bar_arrive(sbar);
-                }
-              } else {
-                bar_arrive(bar);
-                if (Q) bar_arrive(sbar);
+              for (uint32_t e = 0; e < C::kRowSpans; ++e)
+                load_box(dst + e * (kKeys * C::kRowSpan) + r0 * C::kRowSpan, kv ? &map_v : &map_k, (int32_t)(e * 64), (int32_t)in_page, (int32_t)w.h, where, bar);
+              if (Q && page >= 0) {
+                bar_arrive_tx(sbar, a.box_rows * 4);
+                load_bulk(base + C::kOffScale + (sc * kKeys + r0) * 4, (kv ? a.c.v_scale : a.c.k_scale) + ((uint64_t)page * hk + w.h) * a.c.page_size + in_page,
+                          a.box_rows * 4, sbar);
+              } else if (Q) {
+                for (uint32_t e = 0; e < a.box_rows; ++e) reinterpret_cast<float*>(smem + C::kOffScale)[sc * kKeys + r0 + e] = 0.f;
+                fence_async();      // before this lane's next load into the same place
+                bar_arrive(sbar);
               }
+            } else {
+              bar_arrive(bar);
+              if (Q) bar_arrive(sbar);
             }
           }
+          jg += n;
+          t = stop;
           if (t < end) walk_on<TREE>(w, a, cum, skip_rows);
         }
         // every load lands before the block ends, also where the others gave up waiting and left some unread
@@ -791,21 +893,26 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       bool ok = true;
       Walk w = walk_to<TREE>(a, cum, skip_rows, begin);
       int32_t t = begin;
-      uint32_t item = 0;
-      for (uint32_t q = 0; t < end; ++q) {
-        if ((q & 1) == 0) t = max(t, w.item0 + kItemCost);
+      uint32_t item = 0, q = 0, r = 0;                // loads of the block so far, and of the item
+      for (; t < end; ++q) {
+        if (r == 0) t = max(t, w.item0 + kItemCost);
+        const uint32_t n = (uint32_t)(min(end, w.item0 + w.blk.n) - t);
         const uint32_t raw = q % C::kRaws, slot = q % C::kSlots, sc = q % C::kScaleSlots;
         ok = wait_or_give_up(scale_full + 8 * sc, (q / C::kScaleSlots) & 1, ok, a.error);
-        if (q & 1) {
+        if (load_is_value(SHARED, r, n)) {
           // a weight of zero must not meet a scale that is none: one past the end may be anything, and one that is not
           // finite is taken out here and added to the rows that see it at the end
           float* at = reinterpret_cast<float*>(smem + C::kOffScale) + sc * kKeys + row;
-          const bool past = (w.blk.kt0 + t - w.item0 - kItemCost) * (int32_t)kKeys + (int32_t)row >= w.seq.len;
+          const bool past = (w.blk.kt0 + t + (int32_t)load_tile(SHARED, r, n) - w.item0 - kItemCost) * (int32_t)kKeys + (int32_t)row >= w.seq.len;
           if (past || !isfinite(*at)) {
             if (!past) misc[8 + item % 8] = 1;
             *at = 0.f;                // (ordered before the next load into the same place by the fence below: see kScaleSlots)
           }
-          if (++t == min(end, w.item0 + w.blk.n) && t < end) {
+        }
+        if (++r == 2 * n) {
+          r = 0;
+          t += (int32_t)n;
+          if (t < end) {
             walk_on<TREE>(w, a, cum, skip_rows);
             ++item;
           }
