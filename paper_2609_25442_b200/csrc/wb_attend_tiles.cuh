@@ -98,6 +98,11 @@ __device__ __forceinline__ void tm_load32(uint32_t addr, uint32_t* r) {
   asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
                "%24,%25,%26,%27,%28,%29,%30,%31}, [%32];" : WB_W32(r) : "r"(addr));
 }
+__device__ __forceinline__ void tm_load16(uint32_t addr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                 "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(addr));
+}
 __device__ __forceinline__ void tm_store32(uint32_t addr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,"
                "%24,%25,%26,%27,%28,%29,%30,%31};" ::WB_R32(r), "r"(addr) : "memory");
@@ -275,7 +280,7 @@ template <bool TREE> __device__ __forceinline__ int32_t share_begin(const Attend
 
 // Values that are not finite were taken out of a tile that not every row sees (of any tile, where a scale was not finite): a row that
 // does see one has it added here (its weight is positive, whatever it is).  Rare, so straight from the cache.
-template <bool Q, bool TREE>
+template <bool Q, bool TREE, int W>
 __device__ __noinline__ void add_odd_values(const AttendArgs& a, const Walk& w, int32_t kt_begin, int32_t kt_end, int32_t lo, int32_t hi, uint32_t tok,
                                             uint32_t d0, float* o) {
   const int32_t first = w.seq.len - w.seq.n_new;
@@ -288,10 +293,10 @@ __device__ __noinline__ void add_odd_values(const AttendArgs& a, const Walk& w, 
     if (Q) {
       const float s = a.c.v_scale[((uint64_t)page * a.c.n_kv_heads + w.h) * a.c.page_size + slot];
       if (isfinite(s)) continue;
-      for (int d = 0; d < 32; ++d) o[d] += unpack_e4m3x2((uint8_t)a.c.v[at + d]).x * s;
+      for (int d = 0; d < W; ++d) o[d] += unpack_e4m3x2((uint8_t)a.c.v[at + d]).x * s;
     } else {
       const uint16_t* v = reinterpret_cast<const uint16_t*>(a.c.v) + at;
-      for (int d = 0; d < 32; ++d)
+      for (int d = 0; d < W; ++d)
         if ((v[d] & 0x7F80u) == 0x7F80u) o[d] += __uint_as_float((uint32_t)v[d] << 16);
     }
   }
@@ -319,13 +324,14 @@ template <bool TREE> __device__ __forceinline__ RowOf row_of(const AttendArgs& a
 
 // The queries of a warp's 32 rows into shared memory, swizzled as the products read them; lane i knows row i.  Eight lanes copy 128
 // bytes of a row together (a thread copying its own row would touch a line per thread and load).
-template <int D>
-__device__ __forceinline__ void copy_queries(const AttendArgs& a, uint32_t tile, uint32_t row0, const RowOf& x) {
+// (N of the eight groups of four rows, from row `skip` of the 32 on.)
+template <int D, uint32_t N = 8>
+__device__ __forceinline__ void copy_queries(const AttendArgs& a, uint32_t tile, uint32_t row0, const RowOf& x, uint32_t skip = 0) {
   const uint32_t lane = threadIdx.x & 31, c = lane & 7;
   const uint64_t mine = (uint64_t)(a.q + (uint64_t)x.tok * a.q_token + x.head * a.q_head);
 #pragma unroll
-  for (uint32_t i = 0; i < 8; ++i) {
-    const uint32_t from = i * 4 + (lane >> 3), row = row0 + from;
+  for (uint32_t i = 0; i < N; ++i) {
+    const uint32_t from = skip + i * 4 + (lane >> 3), row = row0 + from;
     const uint64_t src = __shfl_sync(0xFFFFFFFFu, mine, from);
     const uint32_t bytes = __shfl_sync(0xFFFFFFFFu, (uint32_t)x.in, from) ? 16 : 0;      // a row that is none: zeros
 #pragma unroll
@@ -333,6 +339,14 @@ __device__ __forceinline__ void copy_queries(const AttendArgs& a, uint32_t tile,
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tile + sp * (kKeys * 128) + row * 128 + ((c ^ (row & 7)) << 4)),
                    "l"(src + sp * 128 + c * 16), "r"(bytes) : "memory");
   }
+}
+// What a tree's row will need: its words of the mask, and its queries where they are not copied yet.
+template <int D>
+__device__ __forceinline__ void row_ahead(const AttendArgs& a, const RowOf& x, bool queries) {
+  if (!x.in) return;
+  for (uint32_t w = 0; w < a.words; w += 32) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.mask + (uint64_t)x.tok * a.words + w) : "memory");
+  if (queries)
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(a.q + (uint64_t)x.tok * a.q_token + x.head * a.q_head), "n"(D * 2) : "memory");
 }
 __device__ __forceinline__ void queries_arrived() {
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -420,7 +434,17 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     for (int i = 8; i < 16; ++i) misc[i] = 0;
   }
-  for (uint32_t s = warp; s < n_seqs; s += C::kThreads / 32) {
+  if (TREE) {      // few row blocks each: a thread per sequence
+    for (uint32_t s = tid; s < n_seqs; s += C::kThreads) {
+      const KvSeq q = attend_seq(a.b, s);
+      const uint32_t nb = row_blocks(q, a.group, skip_rows);
+      int32_t sum = 0;
+      for (uint32_t rb = 0; rb < nb; ++rb) sum += row_block<TREE>(q, a.group, a.window, rb).n;
+      cum[s + 1] = sum * (int32_t)hk;
+      report_too_long(a, s);
+    }
+  }
+  for (uint32_t s = warp; !TREE && s < n_seqs; s += C::kThreads / 32) {
     const KvSeq q = attend_seq(a.b, s);
     const uint32_t nb = row_blocks(q, a.group, skip_rows);
     int32_t sum = 0;
@@ -430,6 +454,10 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       cum[s + 1] = sum * (int32_t)hk;
       report_too_long(a, s);
     }
+  }
+  if (TREE && tid == 288) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
   }
   if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(base + C::kOffMisc) : "memory");
@@ -474,7 +502,10 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       Walk w = walk_to<TREE>(a, cum, skip_rows, begin);
       RowOf x0 = row_of<TREE>(a, w, (SHARED ? 0 : i * 128) + row);
       const uint32_t q_tile = base + i * C::kSlotBytes, warp_row = (warp & 3) * 32;
-      copy_queries<D>(a, q_tile, warp_row, x0);
+      // (shared tiles: both groups' rows are the same, a warp copies 16 of its 32, and the two places hold this item's and the next one's)
+      if (SHARED) copy_queries<D, 4>(a, base, warp_row, x0, i * 16);
+      else copy_queries<D>(a, q_tile, warp_row, x0);
+      if (TREE) row_ahead<D>(a, x0, false);
       queries_arrived();
       bar_arrive(q_full);
       for (int32_t t = begin; t < end; ++item) {
@@ -499,9 +530,20 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         // the scores of this item are done with: the next one's queries take their place while its last weights are computed
         auto prepare_next = [&]() {
           walk_on<TREE>(w2, a, cum, skip_rows);
-          x2 = row_of<TREE>(a, w2, (SHARED ? 0 : i * 128) + row);
+          x2 = row_of<TREE>(a, w2, i * 128 + row);
           copy_queries<D>(a, q_tile, warp_row, x2);
         };
+        // (queries that were first asked for at an item's end took 5 us to come, behind the cache tiles in flight)
+        if (SHARED && stop < end) {
+          walk_on<TREE>(w2, a, cum, skip_rows);
+          x2 = row_of<TREE>(a, w2, row);
+          row_ahead<D>(a, x2, false);
+          copy_queries<D, 4>(a, base + ((item + 1) & 1) * C::kSlotBytes, warp_row, x2, i * 16);
+        } else if (TREE && stop < end) {
+          Walk w1 = w;
+          walk_on<TREE>(w1, a, cum, skip_rows);
+          row_ahead<D>(a, row_of<TREE>(a, w1, i * 128 + row), true);
+        }
         // the score that the weights are relative to (differences are formed before they are scaled: scores of any finite size
         // give weights of 2^8 and less), and that above which it moves
         float ref = 0.f, limit = -INFINITY;
@@ -534,7 +576,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           tc_after();
 #pragma unroll
           for (int c = 0; c < 128; c += 32) tm_load32(tm_s + c, reinterpret_cast<uint32_t*>(x) + c);
-          if (j + (SHARED ? 2 : 1) >= n_tiles && stop < end) prepare_next();
+          if (!SHARED && j + 1 == n_tiles && stop < end) prepare_next();
           tm_wait_load();
           if (Q) {
             ok = wait_or_give_up(scale_ready + 8 * sk, (qk / C::kScaleSlots) & 1, ok, a.error);
@@ -645,7 +687,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           tc_before();
         }
         if (t < end) {
-          if (!takes_part || (SHARED && i >= n_tiles)) prepare_next();
+          if (!takes_part) prepare_next();
           queries_arrived();
         }
         if (t < end || SHARED) {
@@ -685,31 +727,32 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           }
           const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
           const int c_begin = SHARED ? (int)i * (D / 2) : 0, c_end = SHARED ? c_begin + D / 2 : D;
+          constexpr int W = TREE ? 16 : 32;      // columns at a time (a tree's items are short: the code itself has to come from memory)
 #pragma unroll 1
-          for (int c = c_begin; c < c_end; c += 32) {
-            uint32_t o[32];
-            tm_load32(tm_o + c, o);
+          for (int c = c_begin; c < c_end; c += W) {
+            uint32_t o[W];
+            if (TREE) tm_load16(tm_o + c, o); else tm_load32(tm_o + c, o);
             if (SHARED) {
-              uint32_t y[32];
-              tm_load32(tm_lane + 256 + (1 - i) * 128 + c, y);
+              uint32_t y[W];
+              tm_load16(tm_lane + 256 + (1 - i) * 128 + c, y);
               tm_wait_load();
 #pragma unroll
-              for (int e = 0; e < 32; ++e)
+              for (int e = 0; e < W; ++e)
                 o[e] = __float_as_uint((here ? __uint_as_float(o[e]) * f : 0.f) + (there ? __uint_as_float(y[e]) * f2 : 0.f));
             }
             tm_wait_load();
             if (odd && x0.in) {
-              float y[32];
+              float y[W];
 #pragma unroll
-              for (int e = 0; e < 32; ++e) y[e] = __uint_as_float(o[e]);
-              add_odd_values<Q, TREE>(a, w, w.blk.kt0 + from - tile0, w.blk.kt0 + stop - tile0, x0.lo, x0.hi, x0.tok, c, y);
+              for (int e = 0; e < W; ++e) y[e] = __uint_as_float(o[e]);
+              add_odd_values<Q, TREE, W>(a, w, w.blk.kt0 + from - tile0, w.blk.kt0 + stop - tile0, x0.lo, x0.hi, x0.tok, c, y);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(y[e]);
+              for (int e = 0; e < W; ++e) o[e] = __float_as_uint(y[e]);
             }
             if (cuts == 0) {
               if (x0.in)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < W / 8; ++e) {
                   uint32_t y[4];
 #pragma unroll
                   for (int k = 0; k < 4; ++k)
@@ -718,7 +761,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
                 }
             } else {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) part[(c + e) * 128] = __uint_as_float(o[e]);
+              for (int e = 0; e < W; ++e) part[(c + e) * 128] = __uint_as_float(o[e]);
             }
           }
           if (cuts == 0) {
@@ -760,7 +803,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           return base + C::kOffSlots + slot * C::kSlotBytes;
         };
         auto scores = [&](uint32_t i, uint32_t k_addr) {
-          const uint64_t qd = smem_desc(base + i * C::kSlotBytes, 16), kd = smem_desc(k_addr, 16);
+          const uint64_t qd = smem_desc(base + (SHARED ? item & 1 : i) * C::kSlotBytes, 16), kd = smem_desc(k_addr, 16);
 #pragma unroll
           for (uint32_t ks = 0; ks < D / 16; ++ks) {
             const uint32_t off = ((ks >> 2) * C::kSpanBytes + (ks & 3) * 32) >> 4;
@@ -783,7 +826,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           t = uniform(max(t, w.item0 + kItemCost));
           const uint32_t two = uniform((uint32_t)((uint32_t)w.seq.n_new * a.group > w.rb * kQRows + 128));
           wait_all(q_full, item & 1);
-          if (SHARED) {      // cache tiles are shared out between the two groups of softmax warps, each with a copy of the queries
+          if (SHARED) {      // cache tiles are shared out between the two groups of softmax warps
             const uint32_t n = uniform((uint32_t)(stop - t)), q0 = 2 * jg;
             for (uint32_t g = 0; g < min(n, 2u); ++g) {
               scores(g, slot_wait(q0 + g));
