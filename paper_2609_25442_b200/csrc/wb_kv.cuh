@@ -120,36 +120,35 @@ constexpr uint32_t kTokensPerBlock = 32;   // of the kernels that move rows, at 
 // Where the block's tokens live: page and slot of each, page -1 for one that has no place.  One warp: it finds the first token's
 // sequence by a 32-way search (a load per factor of 32, where a search per token would be five), and the others' by counting
 // the starts that follow.  `position`: their positions too, INT32_MIN of one that no sequence holds.
-__device__ __forceinline__ void place_tokens(const KvView& c, const KvBatch& b, uint32_t t0, uint32_t n, int2* place,
-                                             int32_t* position = nullptr) {
-  if (threadIdx.x < 32) {
-    const uint32_t lane = threadIdx.x;
-    const int32_t first = (int32_t)t0, row = (int32_t)(t0 + lane);
-    uint32_t lo = 0, hi = b.n_seqs;                     // new_start[lo] <= first < new_start[hi]
-    while (hi - lo > 1) {
-      const uint32_t step = (hi - lo + 31) / 32, at = lo + lane * step;
-      const bool before = at < hi && (lane == 0 || __ldg(b.new_start + at) <= first);
-      const uint32_t k = 31 - __clz(__ballot_sync(0xFFFFFFFFu, before));
-      lo += k * step;
-      hi = min(hi, lo + step);
-    }
-    // sequences after the first that start within the block's tokens
-    uint32_t s = lo;
-    if (n > 1 && b.n_seqs > 1) {
-      const uint32_t next = lo + 1 + lane;
-      const int32_t start = next < b.n_seqs ? __ldg(b.new_start + next) : 0x7FFFFFFF;
-#pragma unroll
-      for (int j = 0; j < 32; ++j) s += __shfl_sync(0xFFFFFFFFu, start, j) <= row;
-      if (s == lo + 32) s = kv_seq_of_row(b, row);      // more than 32 of them (most without tokens)
-    }
-    if (lane < n) {
-      const KvSeq q = kv_seq(b, s);
-      const int32_t at = row - q.row0, pos = q.len - q.n_new + at;
-      const int32_t page = at >= 0 && at < q.n_new ? kv_page(b, c.n_pages, c.page_size, s, pos) : -1;
-      place[lane] = make_int2(page, page < 0 ? 0 : pos % (int32_t)c.page_size);
-      if (position) position[lane] = at >= 0 && at < q.n_new ? pos : INT32_MIN;
-    }
+__device__ __forceinline__ void place_by_warp(const KvView& c, const KvBatch& b, uint32_t t0, uint32_t n, int2* place, int32_t* position, uint32_t lane) {
+  const int32_t first = (int32_t)t0, row = (int32_t)(t0 + lane);
+  uint32_t lo = 0, hi = b.n_seqs;                     // new_start[lo] <= first < new_start[hi]
+  while (hi - lo > 1) {
+    const uint32_t step = (hi - lo + 31) / 32, at = lo + lane * step;
+    const bool before = at < hi && (lane == 0 || __ldg(b.new_start + at) <= first);
+    const uint32_t k = 31 - __clz(__ballot_sync(0xFFFFFFFFu, before));
+    lo += k * step;
+    hi = min(hi, lo + step);
   }
+  // sequences after the first that start within the block's tokens
+  uint32_t s = lo;
+  if (n > 1 && b.n_seqs > 1) {
+    const uint32_t next = lo + 1 + lane;
+    const int32_t start = next < b.n_seqs ? __ldg(b.new_start + next) : 0x7FFFFFFF;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) s += __shfl_sync(0xFFFFFFFFu, start, j) <= row;
+    if (s == lo + 32) s = kv_seq_of_row(b, row);      // more than 32 of them (most without tokens)
+  }
+  if (lane < n) {
+    const KvSeq q = kv_seq(b, s);
+    const int32_t at = row - q.row0, pos = q.len - q.n_new + at;
+    const int32_t page = at >= 0 && at < q.n_new ? kv_page(b, c.n_pages, c.page_size, s, pos) : -1;
+    place[lane] = make_int2(page, page < 0 ? 0 : pos % (int32_t)c.page_size);
+    if (position) position[lane] = at >= 0 && at < q.n_new ? pos : INT32_MIN;
+  }
+}
+__device__ __forceinline__ void place_tokens(const KvView& c, const KvBatch& b, uint32_t t0, uint32_t n, int2* place) {
+  if (threadIdx.x < 32) place_by_warp(c, b, t0, n, place, nullptr, threadIdx.x);
   __syncthreads();
 }
 

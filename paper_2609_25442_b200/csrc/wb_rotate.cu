@@ -8,6 +8,7 @@
 // their 16 angles at most stay in registers while it goes through the rows of one token: the table is read once per token and
 // slot instead of once per row.
 #include <algorithm>
+#include <atomic>
 
 #include "wb_kv.cuh"
 
@@ -28,23 +29,72 @@ struct RotateArgs {
   uint32_t slots;            // rows of a token that are worked on at once: a power of two, at most kThreads / (D / 32)
 };
 
+// Rows in flight per thread: 64 KiB a block, three blocks an SM, or of fp32 rows 96 KiB and two.
+template <bool F32> constexpr uint32_t kDepth = F32 ? 3 : 4;
+template <bool F32> constexpr uint32_t kRingBytes = kDepth<F32> * (F32 ? 8 : 4) * kThreads * 16;
+
 // PART: the turning elements are the first D / PART of a row.
 template <int D, int PART, bool PAIRS, bool F32, bool Q>
-__global__ void __launch_bounds__(kThreads, F32 ? 2 : 3)
+__global__ void __launch_bounds__(kThreads, 2)
 wb_kv_write_rotated_kernel(const __grid_constant__ RotateArgs a) {
   constexpr uint32_t LANES = D / 32, ROWS = kThreads / LANES, N = F32 ? 2 : 1, HALF = D / PART / 2;
+  constexpr uint32_t DEPTH = kDepth<F32>;
   constexpr int kAngles = PART == 1 ? 16 : 8;      // of a thread: of pieces 0, 1 (2, 3), or of piece 0 or two
-  __shared__ int2 place[kTokensPerBlock];
-  __shared__ int32_t position[kTokensPerBlock];
-  const uint32_t t0 = blockIdx.x * a.per_block, n = min(a.per_block, a.b.n_tokens - t0);
+  __shared__ int2 places[2][kTokensPerBlock];
+  __shared__ int32_t positions[2][kTokensPerBlock];
+  const uint32_t t0 = blockIdx.x * a.per_block, n = min(a.per_block, a.b.n_tokens - t0), warp = threadIdx.x / 32;
   const uint32_t lane = threadIdx.x % LANES, row_slot = threadIdx.x / LANES, slot = row_slot % a.slots;
   const uint32_t hk = a.c.n_kv_heads, hq = a.n_heads, rows = hq + 2 * hk, at_once = ROWS / a.slots;
-  place_tokens(a.c, a.b, t0, n, place, position);
+  // A thread's pieces of the rows that come next, asked for DEPTH rows ahead; only the thread itself reads them.
+  extern __shared__ uint4 ring[];                  // [DEPTH][4 N][kThreads]
+  const uint32_t per_token = (rows + a.slots - 1) / a.slots, steps = (n + at_once - 1) / at_once * per_token;
+  uint32_t asked = 0, ask_tok = row_slot / a.slots, ask_r = slot;
+  auto ask = [&]() {
+    if (asked < steps && ask_tok < n && ask_r < rows) {
+      const bool is_q = ask_r < hq, is_v = ask_r >= hq + hk;
+      const uint32_t h = is_q ? ask_r : is_v ? ask_r - hq - hk : ask_r - hq;
+      const Rows& src = is_q ? a.q : is_v ? a.v : a.k;
+      const char* from = src.data + (uint64_t)(t0 + ask_tok) * src.token_stride + h * src.head_stride + lane * (16 * N);
+      uint4* to = ring + asked % DEPTH * (4 * N * kThreads) + threadIdx.x;
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to + (j * N + i) * kThreads)),
+                       "l"(from + j * (LANES * 16 * N) + i * 16) : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    ++asked;
+    ask_r += a.slots;
+    if (asked % per_token == 0) {
+      ask_r = slot;
+      ask_tok += at_once;
+    }
+  };
+#pragma unroll
+  for (uint32_t i = 0; i < DEPTH; ++i) ask();
+  uint32_t step = 0;
+  // 32 tokens at a time; one warp finds where the next ones go, and has their angles brought near, while these are worked on
+  auto place_ahead = [&](uint32_t c0) {
+    const uint32_t m = min(kTokensPerBlock, n - c0), l = threadIdx.x % 32, buf = c0 / kTokensPerBlock & 1;
+    place_by_warp(a.c, a.b, t0 + c0, m, places[buf], positions[buf], l);
+    if (l < m) {
+      const int32_t pos = a.positions ? __ldg(a.positions + t0 + c0 + l) : positions[buf][l];
+      if ((uint32_t)pos < a.n_positions)
+        for (uint32_t i = 0; i < HALF; i += 16) asm volatile("prefetch.global.L1 [%0];" ::"l"(a.table + (uint64_t)(uint32_t)pos * HALF + i) : "memory");
+    }
+  };
+  if (warp == 0) place_ahead(0);
   for (uint32_t tok0 = 0; tok0 < n; tok0 += at_once) {
-    const uint32_t tok = min(tok0 + row_slot / a.slots, n - 1);
-    const bool mine = tok0 + row_slot / a.slots < n && position[tok] != INT32_MIN;
+    if (tok0 % kTokensPerBlock == 0) {
+      __syncthreads();
+      if (tok0 + kTokensPerBlock < n && warp == tok0 / kTokensPerBlock % (kThreads / 32)) place_ahead(tok0 + kTokensPerBlock);
+    }
+    const uint32_t tok = min(tok0 + row_slot / a.slots, n - 1), buf = tok / kTokensPerBlock & 1, in_chunk = tok % kTokensPerBlock;
+    const int32_t place_pos = positions[buf][in_chunk];
+    const bool mine = tok0 + row_slot / a.slots < n && place_pos != INT32_MIN;
     const uint64_t t = t0 + tok;
-    const int32_t pos = a.positions ? __ldg(a.positions + t) : position[tok];
+    const int32_t pos = a.positions ? __ldg(a.positions + t) : place_pos;
     // a position that the table does not have turns everything into NaN
     const bool known = (uint32_t)pos < a.n_positions;
     float2 cs[kAngles];
@@ -64,18 +114,18 @@ wb_kv_write_rotated_kernel(const __grid_constant__ RotateArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; i += 2) fetch(j * 8 + i, (PART == 4 ? lane % (LANES / 2) : lane) * 8 + j * (LANES * 8) + i);
     }
-    const int2 at = place[tok];
-    for (uint32_t r = slot; r < (rows + a.slots - 1) / a.slots * a.slots; r += a.slots) {
+    const int2 at = places[buf][in_chunk];
+    for (uint32_t r = slot; r < per_token * a.slots; r += a.slots, ++step) {
       const bool is_q = r < hq, is_v = r >= hq + hk, in = mine && r < rows;
       const uint32_t h = is_q ? r : is_v ? r - hq - hk : r - hq;
-      const Rows& src = is_q ? a.q : is_v ? a.v : a.k;
-      const char* from = src.data + t * src.token_stride + h * src.head_stride + lane * (16 * N);
+      asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+      const uint4* mine_now = ring + step % DEPTH * (4 * N * kThreads) + threadIdx.x;
       float x[4][8];
 #pragma unroll
       for (uint32_t j = 0; j < 4; ++j) {
         uint4 raw[N];
 #pragma unroll
-        for (uint32_t i = 0; i < N; ++i) raw[i] = in ? __ldcs(reinterpret_cast<const uint4*>(from + j * (LANES * 16 * N)) + i) : make_uint4(0, 0, 0, 0);
+        for (uint32_t i = 0; i < N; ++i) raw[i] = mine_now[(j * N + i) * kThreads];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const uint4 y = raw[F32 ? e / 4 : 0];
@@ -83,6 +133,7 @@ wb_kv_write_rotated_kernel(const __grid_constant__ RotateArgs a) {
           x[j][e] = F32 ? __uint_as_float(w) : e & 1 ? bf16_hi(w) : bf16_lo(w);
         }
       }
+      ask();
       auto turn = [&](float& u, float& w, float2 z) {
         const float uc = __fmul_rn(u, z.x), ws = __fmul_rn(w, z.y), wc = __fmul_rn(w, z.x), us = __fmul_rn(u, z.y);
         u = __fsub_rn(uc, ws);
@@ -159,21 +210,28 @@ wb_kv_write_rotated_kernel(const __grid_constant__ RotateArgs a) {
   }
 }
 
-template <int D, int PART, bool PAIRS, bool F32>
-void launch_of(const RotateArgs& a, bool q, uint32_t grid, cudaStream_t stream) {
-  if (q) wb_kv_write_rotated_kernel<D, PART, PAIRS, F32, true><<<grid, kThreads, 0, stream>>>(a);
-  else wb_kv_write_rotated_kernel<D, PART, PAIRS, F32, false><<<grid, kThreads, 0, stream>>>(a);
+template <int D, int PART, bool PAIRS, bool F32, bool Q>
+cudaError_t launch_of(const RotateArgs& a, int dev, uint32_t grid, cudaStream_t stream) {
+  auto kernel = wb_kv_write_rotated_kernel<D, PART, PAIRS, F32, Q>;
+  static std::atomic<uint64_t> done{0};      // devices on which the kernel may have that much shared memory
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (!(done.load(std::memory_order_acquire) & bit)) {
+    if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingBytes<F32>)) return e;
+    done.fetch_or(bit, std::memory_order_release);
+  }
+  kernel<<<grid, kThreads, kRingBytes<F32>, stream>>>(a);
+  return cudaPeekAtLastError();
 }
-template <int D, int PART>
-void launch_part(const RotateArgs& a, bool pairs, bool f32, bool q, uint32_t grid, cudaStream_t stream) {
-  if (pairs) f32 ? launch_of<D, PART, true, true>(a, q, grid, stream) : launch_of<D, PART, true, false>(a, q, grid, stream);
-  else f32 ? launch_of<D, PART, false, true>(a, q, grid, stream) : launch_of<D, PART, false, false>(a, q, grid, stream);
+template <int D, int PART, bool PAIRS>
+cudaError_t launch_type(const RotateArgs& a, bool f32, bool q, int dev, uint32_t grid, cudaStream_t stream) {
+  if (f32) return q ? launch_of<D, PART, PAIRS, true, true>(a, dev, grid, stream) : launch_of<D, PART, PAIRS, true, false>(a, dev, grid, stream);
+  return q ? launch_of<D, PART, PAIRS, false, true>(a, dev, grid, stream) : launch_of<D, PART, PAIRS, false, false>(a, dev, grid, stream);
 }
 template <int D>
-void launch_dim(const RotateArgs& a, uint32_t part, bool pairs, bool f32, bool q, uint32_t grid, cudaStream_t stream) {
-  if (part == 1) launch_part<D, 1>(a, pairs, f32, q, grid, stream);
-  else if (part == 2) launch_part<D, 2>(a, pairs, f32, q, grid, stream);
-  else launch_part<D, 4>(a, pairs, f32, q, grid, stream);
+cudaError_t launch_dim(const RotateArgs& a, uint32_t part, bool pairs, bool f32, bool q, int dev, uint32_t grid, cudaStream_t stream) {
+  if (part == 1) return pairs ? launch_type<D, 1, true>(a, f32, q, dev, grid, stream) : launch_type<D, 1, false>(a, f32, q, dev, grid, stream);
+  if (part == 2) return pairs ? launch_type<D, 2, true>(a, f32, q, dev, grid, stream) : launch_type<D, 2, false>(a, f32, q, dev, grid, stream);
+  return pairs ? launch_type<D, 4, true>(a, f32, q, dev, grid, stream) : launch_type<D, 4, false>(a, f32, q, dev, grid, stream);
 }
 
 }  // namespace
@@ -214,14 +272,18 @@ extern "C" wb_status wb_kv_write_rotated(const wb_kv* kv, const wb_kv_batch* bat
   a.positions = rot->positions;
   a.n_positions = rot->n_positions;
   a.n_heads = n_heads;
-  a.per_block = std::min(kTokensPerBlock, std::max(1u, batch->n_tokens / (kNumSMs * 8)));
-  a.slots = 8;
+  // Eight slots for a token leave six rows to each of its threads at 32 query and 8 key heads.  With so few tokens that not every SM would
+  // get a block, a token gets more of them, up to a slot per row.  The grid is what fits at once.
   const uint32_t most = kThreads / (d / 32);
-  if (a.per_block == 1) a.slots = most;
+  a.slots = 8;
+  while (a.slots > most / kTokensPerBlock && a.slots / 2 >= n_heads + 2 * a.c.n_kv_heads) a.slots /= 2;
+  while (a.slots < most && (uint64_t)batch->n_tokens * a.slots < (uint64_t)most * kNumSMs) a.slots *= 2;
+  const uint32_t at_once = most / a.slots, groups = (batch->n_tokens + at_once - 1) / at_once;
+  a.per_block = (groups + 2 * kNumSMs - 1) / (2 * kNumSMs) * at_once;
   const uint32_t grid = (batch->n_tokens + a.per_block - 1) / a.per_block, part = d / rot->rotary_dim;
-  const bool f32 = k->dtype == WB_F32, e = kv->d.dtype == WB_E4M3;
+  const bool f32 = k->dtype == WB_F32, e = kv->d.dtype == WB_E4M3, pairs = rot->interleaved != 0;
   const cudaStream_t st = (cudaStream_t)stream;
-  if (d == 128) launch_dim<128>(a, part, rot->interleaved != 0, f32, e, grid, st);
-  else launch_dim<64>(a, part, rot->interleaved != 0, f32, e, grid, st);
-  return cudaPeekAtLastError() == cudaSuccess ? WB_OK : (cudaGetLastError(), WB_ERR_CUDA);
+  const cudaError_t err = d == 128 ? launch_dim<128>(a, part, pairs, f32, e, kv->device, grid, st) : launch_dim<64>(a, part, pairs, f32, e, kv->device, grid, st);
+  if (err != cudaSuccess) (void)cudaGetLastError();
+  return err == cudaSuccess ? WB_OK : WB_ERR_CUDA;
 }

@@ -48,13 +48,21 @@ __device__ __forceinline__ void tree_range(const T* p, const T* q, const float* 
   uint32_t v = v0;
   if ((((uintptr_t)(p + v0) | (RACE ? (uintptr_t)(e + v0) : 0) | (SUB ? (uintptr_t)(q + v0) : 0)) & 15u) == 0) {
     const uint32_t whole = v0 + (v1 - v0) / 8 * 8;
-    for (v = v0 + threadIdx.x * 8; v < whole; v += THREADS * 8) {
-      float x[8], y[8], z[8];
-      load8(p + v, x);
-      if (RACE) load8(e + v, z);
-      if (SUB) load8(q + v, y);
+    constexpr int U = RACE ? 2 : 4;        // groups of eight in flight: as many as 64 registers hold
+    for (v = v0 + threadIdx.x * 8; v < whole; v += U * THREADS * 8) {
+      float x[U][8], y[U][8], z[U][8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) take(x[i], SUB ? y[i] : 0.f, RACE ? z[i] : 0.f, v + i);
+      for (int u = 0; u < U; ++u) {
+        const uint32_t at = min(v + u * THREADS * 8, whole - 8);      // (the last group may be read again, not used)
+        load8(p + at, x[u]);
+        if (RACE) load8(e + at, z[u]);
+        if (SUB) load8(q + at, y[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (v + u * THREADS * 8 < whole)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) take(x[u][i], SUB ? y[u][i] : 0.f, RACE ? z[u][i] : 0.f, v + u * THREADS * 8 + i);
     }
     v = whole;
   }
@@ -269,7 +277,7 @@ template <typename T, bool SUB> wb_status launch_verify_of(const wb_verify_tree_
   if (cudaGetDevice(&dev) != cudaSuccess) { (void)cudaGetLastError(); return WB_ERR_CUDA; }
   for (uint32_t size : {16u, 8u})
     if (a.n_seqs <= resident_clusters(wb_verify_tree_kernel<T, SUB, 512>, 512, dev, size, known[0])) return launch_verify<T, SUB, 512>(a, size, stream);
-  for (uint32_t size = 8; size > 1; --size)
+  for (uint32_t size = 16; size > 1; --size)
     if (a.n_seqs <= resident_clusters(wb_verify_tree_kernel<T, SUB, 256>, 256, dev, size, known[1])) return launch_verify<T, SUB, 256>(a, size, stream);
   return launch_verify<T, SUB, 256>(a, 1, stream);
 }
