@@ -33,22 +33,35 @@ __device__ __forceinline__ float left_of(float p, float q, const float* mass, ui
 template <typename T, bool SUB, bool RACE, uint32_t THREADS>
 __device__ __forceinline__ void tree_range(const T* p, const T* q, const float* e, uint32_t v0, uint32_t v1, const float* mass, const int32_t* gone,
                                            uint32_t n, Best& best, double& sum) {
-  auto take = [&](float x, float y, float z, uint32_t v) {
-    const float w = SUB ? left_of(x, y, mass, n) : x;
-    if (!RACE) {
-      sum += w;
-      return;
+  // N elements: what is left of them, and then their part in the race or in the sum (two sums, whose additions do not wait for each other)
+  double sums[2] = {0., 0.};
+  auto take = [&](auto& x, const auto& y, const auto& z, auto at, uint32_t end) {
+    constexpr int N = sizeof(x) / sizeof(float);
+    if (SUB)
+      for (uint32_t j = 0; j < n; ++j) {
+        const float m = mass[j];
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = fmaxf(__fsub_rn(x[i], __fmul_rn(m, y[i])), 0.f);
+      }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t v = at(i);
+      if (v >= end) continue;
+      if (!RACE) {
+        sums[i & 1] += x[i];
+        continue;
+      }
+      if (!(x[i] > 0.f) || x[i] < best.bar * z[i]) continue;
+      bool out = false;
+      if (!SUB)
+        for (uint32_t k = 0; k < n; ++k) out |= gone[k] == (int32_t)v;
+      if (!out) best.offer(x[i], z[i], v);
     }
-    if (!(w > 0.f) || w < best.bar * z) return;
-    if (!SUB)
-      for (uint32_t i = 0; i < n; ++i)
-        if (gone[i] == (int32_t)v) return;
-    best.offer(w, z, v);
   };
   uint32_t v = v0;
   if ((((uintptr_t)(p + v0) | (RACE ? (uintptr_t)(e + v0) : 0) | (SUB ? (uintptr_t)(q + v0) : 0)) & 15u) == 0) {
     const uint32_t whole = v0 + (v1 - v0) / 8 * 8;
-    constexpr int U = RACE ? 2 : 4;        // groups of eight in flight: as many as 64 registers hold
+    constexpr int U = RACE && SUB ? 1 : 2;        // groups of eight in flight: as many as 64 registers hold
     for (v = v0 + threadIdx.x * 8; v < whole; v += U * THREADS * 8) {
       float x[U][8], y[U][8], z[U][8];
 #pragma unroll
@@ -59,10 +72,7 @@ __device__ __forceinline__ void tree_range(const T* p, const T* q, const float* 
         if (SUB) load8(q + at, y[u]);
       }
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (v + u * THREADS * 8 < whole)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) take(x[u][i], SUB ? y[u][i] : 0.f, RACE ? z[u][i] : 0.f, v + u * THREADS * 8 + i);
+      for (int u = 0; u < U; ++u) take(x[u], y[u], z[u], [&](int i) { return v + u * THREADS * 8 + i; }, whole);
     }
     v = whole;
   }
@@ -75,10 +85,9 @@ __device__ __forceinline__ void tree_range(const T* p, const T* q, const float* 
       if (RACE) z[i] = __ldg(e + at);
       if (SUB) y[i] = prob(q, at);
     }
-#pragma unroll
-    for (int i = 0; i < 6; ++i)
-      if (v + i * THREADS < v1) take(x[i], SUB ? y[i] : 0.f, RACE ? z[i] : 0.f, v + i * THREADS);
+    take(x, y, z, [&](int i) { return v + i * THREADS; }, v1);
   }
+  sum += sums[0] + sums[1];
 }
 
 template <typename T, bool SUB, uint32_t THREADS>
@@ -89,7 +98,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) wb_verify_tree_kernel
   __shared__ float chance_p[kRows], chance_q[kRows], coin[kRows];
   __shared__ float mass_of[kKids];
   __shared__ int32_t gone[kKids];
-  __shared__ double warp_sum[THREADS / 32], block_sum;
+  __shared__ double warp_sum[THREADS / 32], block_sum[2];
   __shared__ uint64_t warp_best[THREADS / 32], block_best;
   __shared__ int32_t s_here, s_kids, s_more;
   const int32_t start = min(max(__ldg(a.new_start + s), 0), (int32_t)a.n_tokens);
@@ -193,6 +202,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) wb_verify_tree_kernel
     }
     return false;
   };
+  uint32_t turn = 0;
   for (;;) {
     if (tid < 32) {
       const bool more = walk();
@@ -214,12 +224,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) wb_verify_tree_kernel
     __syncthreads();
     if (tid == 0) {
       for (uint32_t w = 1; w < THREADS / 32; ++w) sum += warp_sum[w];
-      block_sum = sum;
+      block_sum[turn] = sum;
     }
     cluster.sync();
+    // a lane fetches a block's sum; they are added in the blocks' order
+    const double part = lane < size ? *cluster.map_shared_rank(&block_sum[turn], lane) : 0.;
     sum = 0.;
-    for (uint32_t r = 0; r < size; ++r) sum += *cluster.map_shared_rank(&block_sum, r);
-    cluster.sync();                      // block_sum may be overwritten
+    for (uint32_t r = 0; r < size; ++r) sum += __shfl_sync(0xFFFFFFFFu, part, r);
+    turn ^= 1;                           // the other place is free: everybody has read it before the next time all meet
     mass = (float)sum;
     summed = kids;
   }
@@ -247,8 +259,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) wb_verify_tree_kernel
     }
     cluster.sync();
     // every block reads all shares: all of them have to know whether any weight was positive
-    winner = 0;
-    for (uint32_t r = 0; r < size; ++r) winner = key_max(winner, *cluster.map_shared_rank(&block_best, r));
+    winner = lane < size ? *cluster.map_shared_rank(&block_best, lane) : 0;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) winner = key_max(winner, __shfl_xor_sync(0xFFFFFFFFu, winner, d));
     cluster.sync();                      // block_best may be overwritten or its block may end
     if (winner || all) break;
     all = true;                          // nothing positive was left: draw from the target's row itself

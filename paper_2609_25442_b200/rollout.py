@@ -241,22 +241,24 @@ class KvCache:
         n, d, dev = batch.n_tokens, self.head_dim, self.device
         a = _heads(k, "k", n, self.n_kv_heads, d, dev)
         b = _heads(v, "v", n, self.n_kv_heads, d, dev)
-        _require(rotation.device == dev and rotation.rotary_dim in (d, d // 2, d // 4),
-                 f"rotation: a table on {dev} for {d}, {d // 2} or {d // 4} elements of a row")
+        if rotation.device != dev or rotation.rotary_dim not in (d, d // 2, d // 4):
+            raise ValueError(f"rotation: a table on {dev} for {d}, {d // 2} or {d // 4} elements of a row")
         args = batch._for(self)
         if positions is not None:
             _require(positions.shape == (n,) and positions.is_contiguous(), "positions: contiguous, [n_tokens]")
             _ints(positions, "positions", dev)
-        else:
-            _require(args.max_len <= rotation.n_positions, f"the batch's max_len is {args.max_len}, the rotation's table has {rotation.n_positions} positions")
+        elif args.max_len > rotation.n_positions:
+            raise ValueError(f"the batch's max_len is {args.max_len}, the rotation's table has {rotation.n_positions} positions")
         h, x, y = 0, None, None
         if q is None:
             _require(q_out is None, "q_out without q")
         else:
-            _require(q.dim() == 3, "q: [n_tokens, n_heads, head_dim]")
+            if q.dim() != 3:
+                raise ValueError("q: [n_tokens, n_heads, head_dim]")
             h = q.shape[1]
             x = _heads(q, "q", n, h, d, dev)
-            _require(q.dtype == k.dtype, f"q is {q.dtype}, k is {k.dtype}")
+            if q.dtype != k.dtype:
+                raise ValueError(f"q is {q.dtype}, k is {k.dtype}")
             if q_out is None:
                 q_out = self._like[torch.bfloat16].new_empty((n, h, d))
                 y = wb.wb_heads(q_out.data_ptr(), wb.WB_BF16, 0, h * d, d)
@@ -264,18 +266,19 @@ class KvCache:
                 y = _heads(q_out, "q_out", n, h, d, dev)
             if h == 0:
                 x = y = None
-        self._kv.write_rotated(args, rotation._args(positions), x, h, y, a, b, _stream(self._index))
+        self._kv.write_rotated(args, rotation._args if positions is None else rotation._at(positions), x, h, y, a, b, _stream(self._index))
         return q_out
 
     def attend_tree(self, batch: KvBatch, q: torch.Tensor, tree: "DraftTree", *, workspace: "AttendWorkspace", scale: Optional[float] = None,
                     window: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
         """attend() for the rows of trees: a row sees all tokens before its sequence's new ones (with window > 0, the latest of
         them as its depth has it) and its ancestors.  A window is at least the batch's max_new."""
-        _require(tree.mask.shape[0] == batch.n_tokens and tree.device == self.device, "tree: of the batch's rows, on the cache's device")
+        if tree.mask.shape[0] != batch.n_tokens or tree.device != self.device:
+            raise ValueError("tree: of the batch's rows, on the cache's device")
         a, h, b, out, lse = self._attention(batch, q, workspace, window, out, lse)
         args = batch._for(self)
-        _require(32 * tree.words >= args.max_new and not 0 < window < args.max_new,
-                 f"trees of up to {args.max_new} rows: the tree's mask has {32 * tree.words} bits, and a window is 0 or at least that many")
+        if 32 * tree.words < args.max_new or 0 < window < args.max_new:
+            raise ValueError(f"trees of up to {args.max_new} rows: the tree's mask has {32 * tree.words} bits, and a window is 0 or at least that many")
         self._kv.attend_tree(args, tree.mask.data_ptr(), tree.words, a, h, b, lse.data_ptr(), self._scale if scale is None else scale, window,
                              workspace.pointer, workspace.bytes, _stream(self._index))
         return out, lse
@@ -303,6 +306,7 @@ class Rotation:
         self.n_positions, self.rotary_dim, self.interleaved = _count(cos.shape[0], "positions"), 2 * int(cos.shape[1]), bool(interleaved)
         self.table = torch.stack((cos, sin), -1).to(torch.float32).contiguous()
         self.device = cos.device
+        self._args = self._at(None)
 
     @classmethod
     def of(cls, rotary_dim: int, n_positions: int, *, base: float = 10000.0, interleaved: bool = False, device="cuda") -> "Rotation":
@@ -313,7 +317,7 @@ class Rotation:
         angle = torch.arange(n_positions, dtype=torch.float64, device=device)[:, None] * freq
         return cls(angle.cos(), angle.sin(), interleaved=interleaved)
 
-    def _args(self, positions: Optional[torch.Tensor]) -> wb.wb_rotation:
+    def _at(self, positions: Optional[torch.Tensor]) -> wb.wb_rotation:
         return wb.wb_rotation(self.table.data_ptr(), None if positions is None else positions.data_ptr(), self.n_positions, self.rotary_dim,
                               int(self.interleaved), 0)
 
