@@ -15,6 +15,7 @@
 #include "wb_attend.cuh"
 #include "wb_attend_rows.cuh"
 #include "wb_attend_tiles.cuh"
+#include "wb_cluster.cuh"
 
 using namespace wbi;
 
@@ -57,7 +58,7 @@ template <int D, bool Q, int NT, bool TREE>
 cudaError_t launch_rows(const AttendArgs& a, int dev, cudaStream_t stream) {
   using C = RowsCfg<D, Q, NT>;
   const size_t smem = C::smem_bytes(a.b.n_seqs);
-  auto kernel = wb_attend_rows_kernel<D, Q, NT, TREE>;
+  auto kernel = wb_attend_rows_kernel<D, Q, NT, TREE ? RowsMode::kTree : RowsMode::kChunk>;
   // every block gets the same share of the tiles, so the grid is what fits at once (with thousands of sequences the table of
   // prefix sums takes the place of a block)
   const uint32_t per_sm = std::min<uint32_t>(C::kBlocksPerSm, (uint32_t)(kSmemPerSm / (smem + 2048)));
@@ -147,9 +148,40 @@ wb_status attend_args(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads*
   a.cuts = (char*)workspace + kHeaderBytes;
   a.partials = (float*)((char*)workspace + kHeaderBytes + kCutBytes);
   a.mask = nullptr;
-  a.words = 0;
+  a.words = a.row_blocks = 0;
   todo = true;
   return WB_OK;
+}
+
+// Trees by clusters, a cluster for every 8 NT rows of a (sequence, kv head), if all of them fit at once and a block's share is
+// kClusterTiles tiles of 64 positions or fewer: `taken` tells.
+constexpr uint32_t kClusterTiles = 8;
+template <int D, bool Q, int NT>
+cudaError_t launch_clusters(AttendArgs a, uint64_t rows, uint32_t max_tiles, int dev, cudaStream_t stream, bool& taken) {
+  using C = RowsCfg<D, Q, NT>;
+  const size_t smem = C::smem_bytes(0);
+  auto kernel = wb_attend_rows_kernel<D, Q, NT, RowsMode::kTreeCluster>;
+  static std::atomic<uint64_t> done{0};
+  static ClusterCounts known;
+  taken = false;
+  a.row_blocks = (uint32_t)((rows + C::kRows - 1) / C::kRows);
+  const uint64_t items = (uint64_t)a.b.n_seqs * a.c.n_kv_heads * a.row_blocks;
+  if (items > 2 * kNumSMs || max_tiles > 16 * kClusterTiles) return cudaSuccess;
+  if (cudaError_t e = prepare_kernel(kernel, 232448, 0, dev, done)) return e;
+  for (uint32_t size = std::min(16u, max_tiles); size * kClusterTiles >= max_tiles; --size) {
+    if (items > resident_clusters(kernel, C::kThreads, dev, size, known, smem)) continue;
+    cudaLaunchAttribute at[1];
+    const cudaLaunchConfig_t cfg = config_of((uint32_t)items, C::kThreads, size, at, stream, smem);
+    taken = true;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+  }
+  return cudaSuccess;
+}
+template <int D, bool Q>
+cudaError_t launch_clusters_of(const AttendArgs& a, uint64_t rows, uint32_t max_tiles, int dev, cudaStream_t stream, bool& taken) {
+  if (rows <= 8) return launch_clusters<D, Q, 1>(a, rows, max_tiles, dev, stream, taken);
+  if (rows <= 16) return launch_clusters<D, Q, 2>(a, rows, max_tiles, dev, stream, taken);
+  return launch_clusters<D, Q, 4>(a, rows, max_tiles, dev, stream, taken);
 }
 
 template <Rows256 MODE> cudaError_t launch_tiles_of(const AttendArgs& a, const wb_kv* kv, uint32_t skip_rows, cudaStream_t stream) {
@@ -162,6 +194,18 @@ template <bool TREE> wb_status launch_attend(const AttendArgs& a, const wb_kv* k
   const bool e = kv->d.dtype == WB_E4M3;
   const uint64_t rows = (uint64_t)batch->max_new * a.group;
   cudaError_t err = cudaSuccess;
+  bool taken = false;
+  if (TREE) {
+    // tiles that a row may see: up to max_len, or of a window and the tree (which may begin within a tile)
+    const uint64_t reach = a.window ? std::min<uint64_t>(batch->max_len, (uint64_t)a.window + batch->max_new) : batch->max_len;
+    const uint32_t tiles = (uint32_t)std::max<uint64_t>(1, (reach + kKvTile - 1) / kKvTile + (a.window ? 1 : 0));
+    if (kv->d.head_dim == 128) err = e ? launch_clusters_of<128, true>(a, rows, tiles, kv->device, st, taken) : launch_clusters_of<128, false>(a, rows, tiles, kv->device, st, taken);
+    else err = e ? launch_clusters_of<64, true>(a, rows, tiles, kv->device, st, taken) : launch_clusters_of<64, false>(a, rows, tiles, kv->device, st, taken);
+    if (taken || err != cudaSuccess) {
+      if (err != cudaSuccess) (void)cudaGetLastError();
+      return err == cudaSuccess ? WB_OK : WB_ERR_CUDA;
+    }
+  }
   // (a batch of trees is of a kind: sequences with few rows go with the others instead of costing two launches of their own)
   const bool mixed = !TREE && batch->n_seqs > 1;
   if (rows <= kMaxRows || mixed) {

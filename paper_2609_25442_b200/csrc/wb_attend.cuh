@@ -16,6 +16,7 @@ struct AttendArgs {
   uint32_t n_heads, group, window;
   uint32_t box_rows;
   uint32_t words;                               // of a row of mask
+  uint32_t row_blocks;                          // clusters only: of a sequence's rows, at most
   const uint32_t* mask;                         // trees only: what a row sees of its sequence's new tokens
   uint32_t* error;                              // workspace: first word, bits of AttendError
   char* cuts;                                   // CutItem of every block

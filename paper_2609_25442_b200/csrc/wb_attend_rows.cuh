@@ -22,7 +22,11 @@
 //   - Work is cut evenly over the SMs whatever the lengths: all (sequence, kv head) items form one line of tiles, every block
 //     takes the same number of consecutive tiles, and a second kernel joins the items that cross blocks, in the order of the
 //     tiles (so results do not depend on timing).
+//   - Few trees are a matter of latency.  A cluster of blocks then serves 32 rows of a (sequence, kv head): each block takes its share of the
+//     cache's tiles, and the cluster joins them over distributed shared memory, without a second kernel.
 #pragma once
+#include <cooperative_groups.h>
+
 #include "wb_attend.cuh"
 
 namespace wbi {
@@ -115,10 +119,14 @@ struct TilePlace {
   uint32_t slot;
 };
 
-template <int D, bool Q, int NT, bool TREE>
+// What a launch serves: chunks along the line of tiles, trees along it, or trees with a cluster for every 8 NT rows of a (sequence, kv head).
+enum class RowsMode { kChunk, kTree, kTreeCluster };
+
+template <int D, bool Q, int NT, RowsMode MODE>
 __global__ void __launch_bounds__(128, RowsCfg<D, Q, NT>::kBlocksPerSm)
 wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   using C = RowsCfg<D, Q, NT>;
+  constexpr bool TREE = MODE != RowsMode::kChunk, CLUSTER = MODE == RowsMode::kTreeCluster;
   extern __shared__ char smem_raw[];
   // slots (1024-byte aligned), their scales, join buffer, warps' maxima and sums, prefix sums
   const uint32_t base = (smem_addr(smem_raw) + 1023u) & ~1023u;
@@ -131,9 +139,45 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   __shared__ float down_of[C::kRows];      // what undoes the scaling of a row's query
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t4 = lane & 3, r8 = lane >> 2;
 
-  // ---- the line of tiles: cum[s] = tiles of the sequences before s ---------------------------------
+  // ---- a cluster's item: tiles [0, its_tiles) of a line of its own ------------------------------------
+  __shared__ int32_t row_token[CLUSTER ? C::kRows : 1], row_low[CLUSTER ? C::kRows : 1];      // of the step's tensors; lowest position seen
+  __shared__ float2 block_ml[CLUSTER ? C::kRows : 1];
   const uint32_t n_seqs = a.b.n_seqs, hk = a.c.n_kv_heads;
-  {
+  namespace cg = cooperative_groups;
+  uint32_t its_s = 0, its_h = 0, its_rows = 0, rank = 0, size = 1;
+  int32_t its_tile0 = 0, its_tiles = 0;
+  KvSeq its = {};
+  if (CLUSTER) {
+    rank = cg::this_cluster().block_rank();
+    size = cg::this_cluster().num_blocks();
+    const uint32_t item = blockIdx.x / size, rb = item % a.row_blocks;
+    its_h = item / a.row_blocks % hk;
+    its_s = item / a.row_blocks / hk;
+    its = attend_seq(a.b, its_s);
+    if (tid == 0 && rank == 0 && its_h == 0 && rb == 0) {
+      const KvSeq q = kv_seq(a.b, its_s);
+      if (q.n_new > 0 && q.len > a.b.max_len) atomicOr(a.error, kTooLong);
+    }
+    const uint32_t all = (uint32_t)its.n_new * a.group, r0 = rb * C::kRows;
+    if (r0 >= all) return;               // (all blocks of the cluster)
+    its_rows = min(all - r0, C::kRows);
+    if (tid < its_rows) {
+      const int32_t i = (int32_t)((r0 + tid) / a.group);
+      row_token[tid] = i;
+      row_low[tid] = tree_low(a, its, (uint32_t)(its.row0 + i), i);
+    }
+    its_tile0 = first_position<TREE>(its, a.window) / (int32_t)kKvTile;
+    // as far as its last row may see
+    const int32_t last = its.len - its.n_new + (int32_t)((r0 + its_rows - 1) / a.group);
+    its_tiles = max(1, (last + (int32_t)kKvTile) / (int32_t)kKvTile - its_tile0);
+  }
+  // row r of the item, as token of its sequence's new ones and query head of its kv head
+  const uint32_t group_inv = (65536 + a.group - 1) / a.group;      // r / group = r * group_inv >> 16 for r < 64
+  auto token_of = [&](uint32_t r) { return CLUSTER ? (uint32_t)row_token[r] : r * group_inv >> 16; };
+  auto head_of = [&](uint32_t r, uint32_t token) { return CLUSTER ? (blockIdx.x / size % a.row_blocks * C::kRows + r) % a.group : r - token * a.group; };
+
+  // ---- the line of tiles: cum[s] = tiles of the sequences before s ---------------------------------
+  if (!CLUSTER) {
     const uint32_t per = (n_seqs + 127) / 128, s0 = min(tid * per, n_seqs), s1 = min(s0 + per, n_seqs);
     int32_t sum = 0;
     for (uint32_t s = s0; s < s1; ++s) {
@@ -164,15 +208,20 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     if (tid == 0) cum[0] = 0;
     __syncthreads();
   }
-  const int32_t total = cum[n_seqs];
-  const int32_t per = (total + (int32_t)gridDim.x - 1) / (int32_t)gridDim.x;
-  const int32_t begin = min((int32_t)blockIdx.x * per, total), end = min(begin + per, total);
+  const int32_t total = CLUSTER ? its_tiles : cum[n_seqs];
+  const int32_t blocks = CLUSTER ? (int32_t)size : (int32_t)gridDim.x, per = (total + blocks - 1) / blocks;
+  const int32_t begin = min((CLUSTER ? (int32_t)rank : (int32_t)blockIdx.x) * per, total), end = min(begin + per, total);
   CutItem* const cut_item = reinterpret_cast<CutItem*>(a.cuts) + blockIdx.x;
-  if (tid == 0) cut_item->parts = 0;
-  if (begin >= end) return;
+  if (!CLUSTER && tid == 0) cut_item->parts = 0;
+  if (!CLUSTER && begin >= end) return;
+  if (CLUSTER) {
+    if (begin >= end && tid < its_rows) block_ml[tid] = make_float2(-INFINITY, 0.f);
+    __syncthreads();                     // the rows' tokens are known
+  }
 
   // the sequence of tile t
   auto find = [&](int32_t t) {
+    if (CLUSTER) return its_s;
     uint32_t lo = 0, hi = n_seqs;        // cum[lo] <= t < cum[hi]
     while (hi - lo > 1) {
       const uint32_t mid = (lo + hi) >> 1;
@@ -190,9 +239,14 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     const int32_t t = begin + (int32_t)(k0 + lane);
     if (t < end) {
       const uint32_t s = find(t);
-      const KvSeq q = attend_seq(a.b, s);
-      const int32_t nt = (cum[s + 1] - cum[s]) / (int32_t)hk, local = t - cum[s], h = local / nt;
-      const uint32_t pos = (uint32_t)(first_position<TREE>(q, a.window) / (int32_t)kKvTile + local - h * nt) * kKvTile + warp * 16;
+      const KvSeq q = CLUSTER ? its : attend_seq(a.b, s);
+      int32_t h = (int32_t)its_h, tile = its_tile0 + t;
+      if (!CLUSTER) {
+        const int32_t nt = (cum[s + 1] - cum[s]) / (int32_t)hk, local = t - cum[s];
+        h = local / nt;
+        tile = first_position<TREE>(q, a.window) / (int32_t)kKvTile + local - h * nt;
+      }
+      const uint32_t pos = (uint32_t)tile * kKvTile + warp * 16;
       const uint32_t entry = pos / a.c.page_size;
       x.slot = pos - entry * a.c.page_size;
       if (pos < (uint32_t)q.len && entry < a.b.table_stride) {
@@ -239,6 +293,10 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     int32_t h, tile0, i0, i1, row0, len, n_new;      // i0, i1: its tiles in the line
   };
   auto enter = [&](Item& x, int32_t t) {
+    if (CLUSTER) {
+      x = Item{its_s, its_rows, (int32_t)its_h, its_tile0, 0, its_tiles, its.row0, its.len, its.n_new};
+      return;
+    }
     while (cum[x.s + 1] <= t) ++x.s;
     const KvSeq q = attend_seq(a.b, x.s);
     const int32_t nt = (cum[x.s + 1] - cum[x.s]) / (int32_t)hk;
@@ -252,15 +310,16 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
     x.n_new = q.n_new;
   };
   uint32_t qf[kGroups][D / 16][2];
-  uint32_t tree[NT][2];            // trees: what rows 2t, 2t + 1 of every group of 8 see of the sequence's new tokens, at most 32
-  const uint32_t group_inv = (65536 + a.group - 1) / a.group;      // r / group = r * group_inv >> 16 for r < 64
+  // trees: what rows 2t, 2t + 1 of every group of 8 see of the sequence's new tokens, at most 32; with clusters, which may have more
+  // rows before them, of the tile's 16 positions
+  uint32_t tree[NT][2];
   auto fetch_queries = [&](const Item& x) {
 #pragma unroll
     for (int n = 0; n < kGroups; ++n) {
       const uint32_t r = (kShared ? warp : n) * 8 + r8;
       const bool in = r < x.n_rows;
-      const uint32_t i = in ? r * group_inv >> 16 : 0;
-      const char* src = a.q + (uint64_t)(x.row0 + (int32_t)i) * a.q_token + ((uint32_t)x.h * a.group + (in ? r - i * a.group : 0)) * a.q_head;
+      const uint32_t i = in ? token_of(r) : 0;
+      const char* src = a.q + (uint64_t)(x.row0 + (int32_t)i) * a.q_token + ((uint32_t)x.h * a.group + (in ? head_of(r, i) : 0)) * a.q_head;
 #pragma unroll
       for (int ks = 0; ks < D / 16; ++ks) {
         uint2 w = make_uint2(0, 0);
@@ -276,7 +335,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         qf[n][ks][1] = w.y;
       }
     }
-    if (TREE) {
+    if (TREE && !CLUSTER) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -289,9 +348,11 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
 
   // the first item's queries are on their way before the cache's tiles crowd the memory
   Item it = {};
-  it.s = find(begin);
-  enter(it, begin);
-  fetch_queries(it);
+  if (begin < end) {
+    it.s = find(begin);
+    enter(it, begin);
+    fetch_queries(it);
+  }
   const uint32_t n_tiles = (uint32_t)(end - begin);
   uint32_t requested = 0;
   for (; requested < C::kSlots; ++requested) {
@@ -359,9 +420,10 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       }
     };
     // how far row r sees; a row that is none sees everything
-    auto sees_to = [&](uint32_t r) { return r < n_rows ? first_hi + (int32_t)(r * group_inv >> 16) : 0x7FFFFFFF; };
+    auto sees_to = [&](uint32_t r) { return r < n_rows ? first_hi + (int32_t)token_of(r) : 0x7FFFFFFF; };
     // whether row 2t + e of group n does not see a position that it reaches: it lies before its window, or is not in its mask
     auto hidden = [&](int n, int e, int32_t up, int32_t pos) {
+      if (CLUSTER) return !(tree[n][e] >> (pos & 15) & 1) || (a.window && up != 0x7FFFFFFF && pos < first_hi && pos < row_low[n * 8 + 2 * t4 + e]);
       if (!TREE) return a.window && up != 0x7FFFFFFF && pos <= up - (int32_t)a.window;
       if (pos >= first_hi) return !(tree[n][e] >> ((pos - first_hi) & 31) & 1);
       // (its own position is first_hi plus the rows that it sees, less one)
@@ -434,6 +496,20 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       }
       // rows that some query row does not see, or that lie past the end of the cache
       const bool partial = (TREE ? pos0 + 15 >= first_hi : pos0 + 15 > first_hi) || pos0 < last_lo;
+      if (CLUSTER && partial) {
+        const int32_t j = pos0 - first_hi;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const uint32_t r = n * 8 + 2 * t4 + e;
+            tree[n][e] = 0xFFFFFFFFu;
+            if (r < n_rows && j > -16) {
+              const uint32_t t = (uint32_t)cur.row0 + token_of(r);
+              tree[n][e] = __funnelshift_r(tree_word(a, t, j >> 5), tree_word(a, t, (j >> 5) + 1), j & 31);
+            }
+          }
+      }
       if (partial) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -596,7 +672,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       copies_commit();
     }
 
-    if (t < end) {         // the next item's queries arrive during the join
+    if (!CLUSTER && t < end) {         // the next item's queries arrive during the join
       enter(it, t);
       fetch_queries(it);
     }
@@ -667,14 +743,21 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       return x;
     };
     auto write_row = [&](uint32_t r, float4 o, float m, float l) {
-      const uint32_t i = r * group_inv >> 16, head = (uint32_t)cur.h * a.group + r - i * a.group;
+      const uint32_t i = token_of(r), head = (uint32_t)cur.h * a.group + head_of(r, i);
       const uint64_t token = (uint64_t)(cur.row0 + (int32_t)i);
       const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
       *reinterpret_cast<uint2*>(a.out + token * a.o_token + head * a.o_head + d4 * 2) =
           make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
       if (a.lse && d4 == 0) a.lse[token * a.n_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
     };
-    if (whole) {
+    if (CLUSTER) {
+      for (uint32_t r = row_first; r < n_rows; r += kStep) {
+        float m, l;
+        total_of(r, m, l);
+        if (C::kBuffers == 2) *reinterpret_cast<float4*>(join + r * C::kPitch + d4) = joined(r);      // (its own elements)
+        if (d4 == 0) block_ml[r] = make_float2(m, l);
+      }
+    } else if (whole) {
       for (uint32_t r = row_first; r < n_rows; r += kStep) {
         float m, l;
         total_of(r, m, l);
@@ -694,6 +777,35 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       if (tid == 0 && cur.i0 >= begin) *cut_item = CutItem{(uint32_t)((cur.i1 - 1) / per - cur.i0 / per) + 1, (uint32_t)cur.row0, (uint32_t)cur.h, n_rows};
     }
     __syncthreads();       // the join buffer is free again
+  }
+
+  // ---- the cluster's result: a thread joins four columns of a row over the blocks, in their order -------
+  if (CLUSTER) {
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();
+    for (uint32_t x = rank * 128 + tid; x < its_rows * (D / 4); x += size * 128) {
+      const uint32_t r = x / (D / 4), c = x % (D / 4) * 4;
+      float top = -INFINITY, l = 0.f;
+#pragma unroll 4
+      for (uint32_t k = 0; k < size; ++k) top = fmaxf(top, cluster.map_shared_rank(block_ml, k)[r].x);
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+      for (uint32_t k = 0; k < size; ++k) {
+        const float2 ml = cluster.map_shared_rank(block_ml, k)[r];
+        const float4 y = *reinterpret_cast<const float4*>(cluster.map_shared_rank(join, k) + r * C::kPitch + c);
+        const float f = ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - top);        // (nothing seen: NaN, or nothing to add)
+        if (ml.y != 0.f) {
+          l += ml.y * f;
+          o.x += y.x * f; o.y += y.y * f; o.z += y.z * f; o.w += y.w * f;
+        }
+      }
+      const uint32_t i = token_of(r), head = its_h * a.group + head_of(r, i);
+      const uint64_t token = (uint64_t)(its.row0 + (int32_t)i);
+      const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
+      *reinterpret_cast<uint2*>(a.out + token * a.o_token + head * a.o_head + c * 2) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+      if (a.lse && c == 0) a.lse[token * a.n_heads + head] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+    }
+    cluster.sync();        // nobody's memory goes before all have read it
   }
 }
 

@@ -1,7 +1,6 @@
 // What the verification kernels share: probabilities as they are read, and the race for the next token.
 #pragma once
-#include <atomic>
-
+#include "wb_cluster.cuh"
 #include "wb_kv.cuh"
 
 namespace wbi {
@@ -38,39 +37,6 @@ __device__ __forceinline__ void load8(const uint16_t* p, float* x) {
   const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
-}
-
-inline cudaLaunchConfig_t config_of(uint32_t n_seqs, uint32_t threads, uint32_t size, cudaLaunchAttribute* at, cudaStream_t stream) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(n_seqs * size);
-  cfg.blockDim = dim3(threads);
-  cfg.stream = stream;
-  at->id = cudaLaunchAttributeClusterDimension;
-  at->val.clusterDim.x = size;
-  at->val.clusterDim.y = at->val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  return cfg;
-}
-
-// How many clusters of `size` blocks fit on the device at once: fewer than its places for blocks divided by size, because a
-// cluster lies within one group of SMs.  Asked for once per kernel, which `known` belongs to.
-struct ClusterCounts {
-  std::atomic<int32_t> plus_one[64][17];
-};
-template <typename K> uint32_t resident_clusters(K kernel, uint32_t threads, int dev, uint32_t size, ClusterCounts& known) {
-  const bool keep = (uint32_t)dev < 64;
-  if (const int32_t n = keep ? known.plus_one[dev][size].load(std::memory_order_acquire) : 0) return (uint32_t)(n - 1);
-  cudaLaunchAttribute at[1];
-  const cudaLaunchConfig_t cfg = config_of(1, threads, size, at, nullptr);
-  int n = 0;
-  if ((size > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
-      cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-    (void)cudaGetLastError();
-    n = 0;
-  }
-  if (keep) known.plus_one[dev][size].store(n + 1, std::memory_order_release);
-  return (uint32_t)n;
 }
 
 }  // namespace wbi
