@@ -154,21 +154,21 @@ wb_status attend_args(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads*
 }
 
 // Trees by clusters, a cluster for every 8 NT rows of a (sequence, kv head), if all of them fit at once and a block's share is
-// kClusterTiles tiles of 64 positions or fewer: `taken` tells.
+// kClusterTiles tiles of 64 positions or fewer: `taken` tells.  `whole`: only with as many blocks in a cluster as there may be.
 constexpr uint32_t kClusterTiles = 8;
 template <int D, bool Q, int NT>
-cudaError_t launch_clusters(AttendArgs a, uint64_t rows, uint32_t max_tiles, int dev, cudaStream_t stream, bool& taken) {
+cudaError_t launch_clusters(AttendArgs a, uint64_t rows, uint32_t max_tiles, bool whole, int dev, cudaStream_t stream, bool& taken) {
   using C = RowsCfg<D, Q, NT>;
   const size_t smem = C::smem_bytes(0);
   auto kernel = wb_attend_rows_kernel<D, Q, NT, RowsMode::kTreeCluster>;
   static std::atomic<uint64_t> done{0};
   static ClusterCounts known;
-  taken = false;
   a.row_blocks = (uint32_t)((rows + C::kRows - 1) / C::kRows);
   const uint64_t items = (uint64_t)a.b.n_seqs * a.c.n_kv_heads * a.row_blocks;
-  if (items > 2 * kNumSMs || max_tiles > 16 * kClusterTiles) return cudaSuccess;
+  if (items > C::kBlocksPerSm * kNumSMs) return cudaSuccess;
   if (cudaError_t e = prepare_kernel(kernel, 232448, 0, dev, done)) return e;
-  for (uint32_t size = std::min(16u, max_tiles); size * kClusterTiles >= max_tiles; --size) {
+  const uint32_t most = std::min(16u, max_tiles);
+  for (uint32_t size = most; size * kClusterTiles >= max_tiles && (!whole || size == most); --size) {
     if (items > resident_clusters(kernel, C::kThreads, dev, size, known, smem)) continue;
     cudaLaunchAttribute at[1];
     const cudaLaunchConfig_t cfg = config_of((uint32_t)items, C::kThreads, size, at, stream, smem);
@@ -177,11 +177,15 @@ cudaError_t launch_clusters(AttendArgs a, uint64_t rows, uint32_t max_tiles, int
   }
   return cudaSuccess;
 }
+// Few rows to a block make its work shorter, as long as every cluster still has all the blocks that it can use.
 template <int D, bool Q>
 cudaError_t launch_clusters_of(const AttendArgs& a, uint64_t rows, uint32_t max_tiles, int dev, cudaStream_t stream, bool& taken) {
-  if (rows <= 8) return launch_clusters<D, Q, 1>(a, rows, max_tiles, dev, stream, taken);
-  if (rows <= 16) return launch_clusters<D, Q, 2>(a, rows, max_tiles, dev, stream, taken);
-  return launch_clusters<D, Q, 4>(a, rows, max_tiles, dev, stream, taken);
+  taken = false;
+  if (max_tiles > 16 * kClusterTiles) return cudaSuccess;
+  cudaError_t e = launch_clusters<D, Q, 1>(a, rows, max_tiles, rows > 8, dev, stream, taken);
+  if (!taken && e == cudaSuccess && rows > 8) e = launch_clusters<D, Q, 2>(a, rows, max_tiles, rows > 16, dev, stream, taken);
+  if (!taken && e == cudaSuccess && rows > 16) e = launch_clusters<D, Q, 4>(a, rows, max_tiles, false, dev, stream, taken);
+  return e;
 }
 
 template <Rows256 MODE> cudaError_t launch_tiles_of(const AttendArgs& a, const wb_kv* kv, uint32_t skip_rows, cudaStream_t stream) {

@@ -297,7 +297,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       x = Item{its_s, its_rows, (int32_t)its_h, its_tile0, 0, its_tiles, its.row0, its.len, its.n_new};
       return;
     }
-    while (cum[x.s + 1] <= t) ++x.s;
+    while (!CLUSTER && cum[x.s + 1] <= t) ++x.s;
     const KvSeq q = attend_seq(a.b, x.s);
     const int32_t nt = (cum[x.s + 1] - cum[x.s]) / (int32_t)hk;
     x.tile0 = first_position<TREE>(q, a.window) / (int32_t)kKvTile;
@@ -699,21 +699,33 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         mine[n][e] = thr[n][e] == -INFINITY ? 1.f : fast_exp2(__fmul_rn(ref[n][e], c2q[n][e]) - m);      // (nothing seen: zeros, or NaN; the product is rounded, as m was)
         if (Q && ei[n][e] != 0.f) mine[n][e] *= lim[n][e] * (1.f / 256.f);
       }
-#pragma unroll
-    for (uint32_t round = 0; round < 4 / C::kBuffers; ++round) {
-      if (round == warp / C::kBuffers) {
-        float* const buf = join + warp % C::kBuffers * (C::kRows * C::kPitch);
+    // (one copy of the code for all rounds: with four, 48 KiB of it at 32 rows, an item's end took 7.6 us the first time; a cluster's block
+    // is done with its slots, which then have room for the other warps' buffers: one round instead of four)
+    static_assert((4 - C::kBuffers) * C::kRows * C::kPitch * 4 <= 4 * C::kSlots * C::kSlotBytes, "");
+    float* const spare = reinterpret_cast<float*>(gen);
+#pragma unroll 1
+    for (uint32_t round = 0; round < (CLUSTER ? 1 : 4 / C::kBuffers); ++round) {
+      if (CLUSTER || round == warp / C::kBuffers) {
+        float* const buf = !CLUSTER || warp < C::kBuffers ? join + warp % C::kBuffers * (C::kRows * C::kPitch) : spare + (warp - C::kBuffers) * (C::kRows * C::kPitch);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int i = 0; i < D / 16; ++i)
+          for (int i = 0; i < D / 16; i += 2) {
+            // eight elements are read before any is written (one by one, each waited for the one before: 5 us at 32 rows)
+            float before[8];
+            float* at[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t d = Q ? i * 16 + 2 * r8 + (e >> 1) : i * 16 + r8 + 8 * (e >> 1);
-              float* at = buf + (n * 8 + 2 * t4 + (e & 1)) * C::kPitch + d;
-              const float x = acc[n][i][e] * mine[n][e & 1];
-              *at = round == 0 ? x : *at + x;
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t c = i + (e >> 2), d = Q ? c * 16 + 2 * r8 + (e >> 1 & 1) : c * 16 + r8 + 8 * (e >> 1 & 1);
+              at[e] = buf + (n * 8 + 2 * t4 + (e & 1)) * C::kPitch + d;
+              before[e] = round == 0 ? 0.f : *at[e];
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float x = acc[n][i + (e >> 2)][e & 3] * mine[n][e & 1];
+              *at[e] = round == 0 ? x : before[e] + x;
+            }
+          }
       }
       __syncthreads();
     }
@@ -751,11 +763,20 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
       if (a.lse && d4 == 0) a.lse[token * a.n_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
     };
     if (CLUSTER) {
-      for (uint32_t r = row_first; r < n_rows; r += kStep) {
+      if (tid < n_rows) {
         float m, l;
-        total_of(r, m, l);
-        if (C::kBuffers == 2) *reinterpret_cast<float4*>(join + r * C::kPitch + d4) = joined(r);      // (its own elements)
-        if (d4 == 0) block_ml[r] = make_float2(m, l);
+        total_of(tid, m, l);
+        block_ml[tid] = make_float2(m, l);
+      }
+      for (uint32_t r = row_first; r < n_rows; r += kStep) {      // (a thread's own elements; the warps in their order)
+        float4 x = *reinterpret_cast<const float4*>(join + r * C::kPitch + d4);
+#pragma unroll
+        for (uint32_t w = 1; w < 4; ++w) {
+          const float4 y = *reinterpret_cast<const float4*>((w < C::kBuffers ? join + w * (C::kRows * C::kPitch) : spare + (w - C::kBuffers) * (C::kRows * C::kPitch)) +
+                                                            r * C::kPitch + d4);
+          x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+        }
+        *reinterpret_cast<float4*>(join + r * C::kPitch + d4) = x;
       }
     } else if (whole) {
       for (uint32_t r = row_first; r < n_rows; r += kStep) {
@@ -783,22 +804,31 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   if (CLUSTER) {
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
-    for (uint32_t x = rank * 128 + tid; x < its_rows * (D / 4); x += size * 128) {
-      const uint32_t r = x / (D / 4), c = x % (D / 4) * 4;
-      float top = -INFINITY, l = 0.f;
-#pragma unroll 4
-      for (uint32_t k = 0; k < size; ++k) top = fmaxf(top, cluster.map_shared_rank(block_ml, k)[r].x);
+    // (whole warps go through this loop together: its_rows rows of D / 4 threads, in steps of 128)
+    for (uint32_t x = rank * 128 + tid; x - lane < its_rows * (D / 4); x += size * 128) {
+      const uint32_t r = min(x / (D / 4), its_rows - 1), c = x % (D / 4) * 4, first = lane & ~(D / 4 - 1);      // the row's first lane
+      // a lane fetches a block's maximum and sum
+      float2 mine = make_float2(-INFINITY, 0.f);
+      if (lane - first < size) mine = cluster.map_shared_rank(block_ml, lane - first)[r];
+      float top = mine.x;
+#pragma unroll
+      for (uint32_t d = 8; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+      top = __shfl_sync(0xFFFFFFFFu, top, first);
+      const float f_mine = mine.x == -INFINITY ? 1.f : fast_exp2(mine.x - top);        // (nothing seen: NaN, or nothing to add)
+      float l = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-      for (uint32_t k = 0; k < size; ++k) {
-        const float2 ml = cluster.map_shared_rank(block_ml, k)[r];
-        const float4 y = *reinterpret_cast<const float4*>(cluster.map_shared_rank(join, k) + r * C::kPitch + c);
-        const float f = ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - top);        // (nothing seen: NaN, or nothing to add)
-        if (ml.y != 0.f) {
-          l += ml.y * f;
-          o.x += y.x * f; o.y += y.y * f; o.z += y.z * f; o.w += y.w * f;
-        }
+      float4 y[16];
+#pragma unroll
+      for (uint32_t k = 0; k < 16; ++k)
+        if (k < size) y[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(join, k) + r * C::kPitch + c);
+#pragma unroll
+      for (uint32_t k = 0; k < 16; ++k) {
+        const float lk = __shfl_sync(0xFFFFFFFFu, mine.y, first + k), f = __shfl_sync(0xFFFFFFFFu, f_mine, first + k);
+        if (k >= size || lk == 0.f) continue;
+        l += lk * f;
+        o.x += y[k].x * f; o.y += y[k].y * f; o.z += y[k].z * f; o.w += y[k].w * f;
       }
+      if (x >= its_rows * (D / 4)) continue;
       const uint32_t i = token_of(r), head = its_h * a.group + head_of(r, i);
       const uint64_t token = (uint64_t)(its.row0 + (int32_t)i);
       const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : NAN;
