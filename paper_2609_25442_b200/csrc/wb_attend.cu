@@ -1,6 +1,6 @@
 // Attention of a chunk of new tokens over the paged cache: which kernel takes a sequence, and the launches.
 //
-// Two kernels share a batch by the sequences' rows (new tokens x query heads per kv head).  Up to 32 rows the cache's bytes are the
+// Two kernels share a batch of chunks by the sequences' rows (new tokens x query heads per kv head).  Up to 32 rows the cache's bytes are the
 // bound, and a kernel that streams them through the legacy matrix instructions is the faster; beyond, the products are, and they
 // need tensor memory, in a kernel that fills tiles of 128 rows whatever there are.  24 sequences of 300 to 5000 positions with 8 to 32
 // rows: 73 us (E4M3) and 75 us (bf16) with the border at 32, 103 and 91 with it at 16, 129 and 95 at 8.  Both are launched where a
@@ -154,8 +154,15 @@ wb_status attend_args(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads*
 }
 
 // Trees by clusters, a cluster for every 8 NT rows of a (sequence, kv head), if all of them fit at once and a block's share is
-// kClusterTiles tiles of 64 positions or fewer: `taken` tells.  `whole`: only with as many blocks in a cluster as there may be.
-constexpr uint32_t kClusterTiles = 8;
+// small: `taken` tells.  `whole`: only with as many blocks in a cluster as there may be.
+//
+// What the kernels along the line cost more is a second launch and its reads, 4 to 10 us; what clusters cost more are uneven
+// shares and, beyond 32 rows, cache tiles read once per 32 of them.  Both sides, bf16, heads of 128, cluster | line, us: one sequence, 8 kv
+// heads, 4 rows 1000 positions 8.2 | 9.5, 8000 14.0 | 16.1, 16 thousand 21.1 | 19.0, 30 thousand 33.4 | 31.4; 32 rows 13.3 | 18.5, 23.1 |
+// 34.1, 35.3 | 42.8, 56.0 | 53.0; 128 rows 15.4 | 19.2, 35.1 | 35.9, 59.5 | 42.9; with 4 kv heads, which leaves clusters of 16, 26.0 | 46.1
+// and 41.2 | 47.7 of the latter two.  64 items of 32 rows, 256 and 2000 positions: 14.2 | 13.2 and 25.6 | 23.8;
+// beyond 128 rows, where the other kernel's tiles are not shared out, 49 items of a window of 1000 from codes 16.4 | 25.4.
+constexpr uint32_t kClusterTiles = 16, kClusterTilesWide = 8, kClusterItems = 48, kClusterItemsWide = 64;
 template <int D, bool Q, int NT>
 cudaError_t launch_clusters(AttendArgs a, uint64_t rows, uint32_t max_tiles, bool whole, int dev, cudaStream_t stream, bool& taken) {
   using C = RowsCfg<D, Q, NT>;
@@ -165,10 +172,10 @@ cudaError_t launch_clusters(AttendArgs a, uint64_t rows, uint32_t max_tiles, boo
   static ClusterCounts known;
   a.row_blocks = (uint32_t)((rows + C::kRows - 1) / C::kRows);
   const uint64_t items = (uint64_t)a.b.n_seqs * a.c.n_kv_heads * a.row_blocks;
-  if (items > C::kBlocksPerSm * kNumSMs) return cudaSuccess;
+  if (items > (rows > kQRows / 2 ? kClusterItemsWide : rows > kMaxRows ? kClusterItems : C::kBlocksPerSm * kNumSMs)) return cudaSuccess;
   if (cudaError_t e = prepare_kernel(kernel, 232448, 0, dev, done)) return e;
   const uint32_t most = std::min(16u, max_tiles);
-  for (uint32_t size = most; size * kClusterTiles >= max_tiles && (!whole || size == most); --size) {
+  for (uint32_t size = most; size * (rows <= kMaxRows || size == 16 ? kClusterTiles : kClusterTilesWide) >= max_tiles && (!whole || size == most); --size) {
     if (items > resident_clusters(kernel, C::kThreads, dev, size, known, smem)) continue;
     cudaLaunchAttribute at[1];
     const cudaLaunchConfig_t cfg = config_of((uint32_t)items, C::kThreads, size, at, stream, smem);
@@ -212,12 +219,14 @@ template <bool TREE> wb_status launch_attend(const AttendArgs& a, const wb_kv* k
   }
   // (a batch of trees is of a kind: sequences with few rows go with the others instead of costing two launches of their own)
   const bool mixed = !TREE && batch->n_seqs > 1;
-  if (rows <= kMaxRows || mixed) {
+  // (trees of 17 to 32 rows over a bf16 cache: the second kernel shares their tiles out, 4 sequences of 8000 positions 39.7 us instead of 52)
+  const bool few = rows <= (TREE && !e ? kMaxRows / 2 : kMaxRows);
+  if (few || mixed) {
     const uint32_t r = (uint32_t)std::min<uint64_t>(rows, kMaxRows);
     if (kv->d.head_dim == 128) err = e ? launch_rows_of<128, true, TREE>(r, a, kv->device, st) : launch_rows_of<128, false, TREE>(r, a, kv->device, st);
     else err = e ? launch_rows_of<64, true, TREE>(r, a, kv->device, st) : launch_rows_of<64, false, TREE>(r, a, kv->device, st);
   }
-  if (err == cudaSuccess && rows > kMaxRows) {
+  if (err == cudaSuccess && (!few || (mixed && rows > kMaxRows))) {
     const uint32_t skip = mixed ? kMaxRows : 0;
     constexpr Rows256 kMode = TREE ? Rows256::kTree : Rows256::kChunk;
     err = TREE && rows <= kQRows / 2 ? launch_tiles_of<Rows256::kTreeShared>(a, kv, skip, st) : launch_tiles_of<kMode>(a, kv, skip, st);

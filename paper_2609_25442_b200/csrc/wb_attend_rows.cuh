@@ -136,6 +136,7 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
   float2* const warp_ml = reinterpret_cast<float2*>(join + C::kJoinBytes / 4);        // [warp][row]
   int32_t* const cum = reinterpret_cast<int32_t*>(warp_ml + 4 * C::kRows);
   __shared__ int32_t scan_tmp[4];
+  float* const spare = reinterpret_cast<float*>(gen);      // the slots' memory, once a cluster's block is done with it
   __shared__ float down_of[C::kRows];      // what undoes the scaling of a row's query
   const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t4 = lane & 3, r8 = lane >> 2;
 
@@ -699,33 +700,37 @@ wb_attend_rows_kernel(const __grid_constant__ AttendArgs a) {
         mine[n][e] = thr[n][e] == -INFINITY ? 1.f : fast_exp2(__fmul_rn(ref[n][e], c2q[n][e]) - m);      // (nothing seen: zeros, or NaN; the product is rounded, as m was)
         if (Q && ei[n][e] != 0.f) mine[n][e] *= lim[n][e] * (1.f / 256.f);
       }
-    // (one copy of the code for all rounds: with four, 48 KiB of it at 32 rows, an item's end took 7.6 us the first time; a cluster's block
-    // is done with its slots, which then have room for the other warps' buffers: one round instead of four)
-    static_assert((4 - C::kBuffers) * C::kRows * C::kPitch * 4 <= 4 * C::kSlots * C::kSlotBytes, "");
-    float* const spare = reinterpret_cast<float*>(gen);
-#pragma unroll 1
-    for (uint32_t round = 0; round < (CLUSTER ? 1 : 4 / C::kBuffers); ++round) {
-      if (CLUSTER || round == warp / C::kBuffers) {
-        float* const buf = !CLUSTER || warp < C::kBuffers ? join + warp % C::kBuffers * (C::kRows * C::kPitch) : spare + (warp - C::kBuffers) * (C::kRows * C::kPitch);
+    if (CLUSTER) {
+      // a cluster's block is done with its slots, which then have room for the other warps' buffers: one round instead of four, which
+      // took 3 us, and four times the code, 48 KiB at 32 rows, which a block that runs it once has to wait for
+      static_assert((4 - C::kBuffers) * C::kRows * C::kPitch * 4 <= 4 * C::kSlots * C::kSlotBytes, "");
+      float* const buf = warp < C::kBuffers ? join + warp * (C::kRows * C::kPitch) : spare + (warp - C::kBuffers) * (C::kRows * C::kPitch);
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t d = Q ? i * 16 + 2 * r8 + (e >> 1) : i * 16 + r8 + 8 * (e >> 1);
+            buf[(n * 8 + 2 * t4 + (e & 1)) * C::kPitch + d] = acc[n][i][e] * mine[n][e & 1];
+          }
+      __syncthreads();
+    }
+#pragma unroll
+    for (uint32_t round = 0; round < (CLUSTER ? 0 : 4 / C::kBuffers); ++round) {
+      if (round == warp / C::kBuffers) {
+        float* const buf = join + warp % C::kBuffers * (C::kRows * C::kPitch);
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int i = 0; i < D / 16; i += 2) {
-            // eight elements are read before any is written (one by one, each waited for the one before: 5 us at 32 rows)
-            float before[8];
-            float* at[8];
+          for (int i = 0; i < D / 16; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const uint32_t c = i + (e >> 2), d = Q ? c * 16 + 2 * r8 + (e >> 1 & 1) : c * 16 + r8 + 8 * (e >> 1 & 1);
-              at[e] = buf + (n * 8 + 2 * t4 + (e & 1)) * C::kPitch + d;
-              before[e] = round == 0 ? 0.f : *at[e];
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t d = Q ? i * 16 + 2 * r8 + (e >> 1) : i * 16 + r8 + 8 * (e >> 1);
+              float* at = buf + (n * 8 + 2 * t4 + (e & 1)) * C::kPitch + d;
+              const float x = acc[n][i][e] * mine[n][e & 1];
+              *at = round == 0 ? x : *at + x;
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float x = acc[n][i + (e >> 2)][e & 3] * mine[n][e & 1];
-              *at[e] = round == 0 ? x : before[e] + x;
-            }
-          }
       }
       __syncthreads();
     }

@@ -522,8 +522,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         const int32_t warp_hi = TREE ? base_pos - 1 : __shfl_sync(0xFFFFFFFFu, x0.hi, 0);
         const int32_t warp_lo = !a.window ? 0 : TREE ? __reduce_max_sync(0xFFFFFFFFu, x0.lo) : __shfl_sync(0xFFFFFFFFu, x0.lo, 31);
         const bool takes_part = SHARED || i == 0 || !one_tile(w, a.group);
-        const uint32_t n_tiles = (uint32_t)(stop - t), q0 = 2 * jg;
-        jg += n_tiles;
+        const uint32_t n_tiles = SHARED ? (uint32_t)(stop - t) : 0;      // of the item here
         if (tid == 0) misc[8 + (item + 5) % 8] = 0;     // that of three items ago: the other tile is at most one behind, nobody five ahead
         Walk w2 = w;                                // the next item, once this one's last scores are there
         RowOf x2 = x0;
@@ -548,19 +547,20 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         // give weights of 2^8 and less), and that above which it moves
         float ref = 0.f, limit = -INFINITY;
         uint64_t sum2[2] = {0, 0};
-        bool first = true;
-        for (uint32_t j = SHARED ? i : 0; j < n_tiles; j += SHARED ? 2 : 1, first = false) {
-          const uint32_t qk = q0 + key_load(SHARED, j), qv = q0 + value_load(SHARED, j, n_tiles), sk = qk % C::kScaleSlots, sv = qv % C::kScaleSlots;
+        // one tile of the line, whose keys and values are loads qk and qv of the block
+        auto step = [&](int32_t tile, uint32_t qk, uint32_t qv, bool first, bool last) {
+          const uint32_t sk = qk % C::kScaleSlots, sv = SHARED ? qv % C::kScaleSlots : sk + 1, ready_k = qk / C::kScaleSlots & 1,
+                         ready_v = SHARED ? qv / C::kScaleSlots & 1 : ready_k;
           if (!takes_part) {                        // keeps the pace of the scales' ring
             if (Q) {
-              ok = wait_or_give_up(scale_ready + 8 * sk, (qk / C::kScaleSlots) & 1, ok, a.error);
-              ok = wait_or_give_up(scale_ready + 8 * sv, (qv / C::kScaleSlots) & 1, ok, a.error);
+              ok = wait_or_give_up(scale_ready + 8 * sk, ready_k, ok, a.error);
+              ok = wait_or_give_up(scale_ready + 8 * sv, ready_v, ok, a.error);
               bar_arrive(scale_empty + 8 * sk);
               bar_arrive(scale_empty + 8 * sv);
             }
-            continue;
+            return;
           }
-          const int32_t pos0 = (w.blk.kt0 + from + (int32_t)j - tile0) * (int32_t)kKeys;
+          const int32_t pos0 = (w.blk.kt0 + tile - tile0) * (int32_t)kKeys;
           const bool cut = pos0 + (int32_t)kKeys - 1 > cut_hi || pos0 < cut_lo;
           if (!Q && cut && (i == 0 || SHARED)) {
             // Values past the end, and values that are not finite, must not meet weights of zero.  Only the first tile's threads
@@ -576,10 +576,10 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           tc_after();
 #pragma unroll
           for (int c = 0; c < 128; c += 32) tm_load32(tm_s + c, reinterpret_cast<uint32_t*>(x) + c);
-          if (!SHARED && j + 1 == n_tiles && stop < end) prepare_next();
+          if (!SHARED && last && stop < end) prepare_next();
           tm_wait_load();
           if (Q) {
-            ok = wait_or_give_up(scale_ready + 8 * sk, (qk / C::kScaleSlots) & 1, ok, a.error);
+            ok = wait_or_give_up(scale_ready + 8 * sk, ready_k, ok, a.error);
             const uint32_t scales = base + C::kOffScale + sk * (kKeys * 4);
 #pragma unroll
             for (int c = 0; c < 128; c += 4) {
@@ -637,7 +637,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               }
             }
           }
-          if (Q) ok = wait_or_give_up(scale_ready + 8 * sv, (qv / C::kScaleSlots) & 1, ok, a.error);
+          if (Q) ok = wait_or_give_up(scale_ready + 8 * sv, ready_v, ok, a.error);
           const uint64_t c22 = pack2(c2, c2), ref2 = pack2(-ref, -ref);
           const uint32_t vscales = base + C::kOffScale + sv * (kKeys * 4);
 #pragma unroll
@@ -674,14 +674,24 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             bar_arrive_n(scale_empty + 8 * sk, SHARED ? 2 : 1);      // for the other group's threads too, which do not read them
             bar_arrive_n(scale_empty + 8 * sv, SHARED ? 2 : 1);
           }
+        };
+        if (SHARED) {
+          for (uint32_t j = i; j < n_tiles; j += 2) step(from + (int32_t)j, 2 * jg + key_load(true, j), 2 * jg + value_load(true, j, n_tiles), j < 2, false);
+          jg += n_tiles;
+          t = stop;
+        } else {
+          for (bool first = true; t < stop; ++t, ++jg, first = false) step(t, 2 * jg, 2 * jg + 1, first, t + 1 == stop);
         }
-        t = stop;
         float m2 = -INFINITY, l2 = 0.f;               // the other group's maximum and sum, where tiles are shared out
-        float l, l1;
-        unpack2(add2(sum2[0], sum2[1]), l, l1);
-        l += l1;
-        const float m = l == 0.f ? -INFINITY : ref * c2;
+        float l, m;
+        auto add_up = [&]() {
+          float l1;
+          unpack2(add2(sum2[0], sum2[1]), l, l1);
+          l += l1;
+          m = l == 0.f ? -INFINITY : ref * c2;
+        };
         if (SHARED) {      // they change hands in columns of the scores that weights do not reach; a row has the same lane in both groups
+          add_up();
           tm_store2(tm_s + 64, m, l);
           tm_wait_store();
           tc_before();
@@ -718,6 +728,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           const int32_t cuts = cuts_of(w.item0, item1, per);
           char* dst = a.out + (uint64_t)x0.tok * a.o_token + x0.head * a.o_head;
           float* part = a.partials + (size_t)(2 * blockIdx.x + (w.item0 >= begin ? 1 : 0)) * C::kPartFloats + (SHARED ? 0 : i * (D * 128 + 256)) + row;
+          if (!SHARED) add_up();
           float top = m, f = 1.f, f2 = 0.f;
           if (SHARED) {
             top = fmaxf(m, m2);
@@ -790,7 +801,8 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         constexpr uint32_t kQk = kF32Bf16 | (kKeys / 8) << 17, kPv = kF32Bf16 | 1u << 16 | (uint32_t)(D / 8) << 17;
         const uint32_t leader = lane == 0, tm = uniform(tmem);
         const int32_t t_end = uniform(end);
-        uint32_t jg = 0, item = 0, j0 = 0, js = 0;  // steps, items, steps of the first and the second tile
+        uint32_t jg = 0, item = 0, js = 0;          // steps, items, steps of the second tile
+        uint32_t j0 = 0;                            // (shared tiles: steps of the first group; js: of the second)
         bool ok = true;
         auto wait_all = [&](uint32_t bar, uint32_t parity) {
           ok = wait_or_give_up(bar, parity, ok, a.error);
@@ -856,8 +868,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             const uint32_t v_addr = slot_wait(2 * jg + 1);
             const bool more = t + 1 < stop;
             if (more) k_addr = slot_wait(2 * jg + 2);
-            values(0, v_addr, add, j0);
-            ++j0;
+            values(0, v_addr, add, jg);
             if (more) scores(0, k_addr); else tc_commit(o_full, leader);
             if (two) {
               values(1, v_addr, add, js);
@@ -880,21 +891,16 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         Walk w = walk_to<TREE>(a, cum, skip_rows, begin);
         for (int32_t t = begin; t < end;) {
           const int32_t stop = min(end, w.item0 + w.blk.n), tile0 = w.item0 + kItemCost;
-          t = max(t, tile0);
-          const uint32_t n = (uint32_t)(stop - t);
-            int32_t page = -1;
-          uint32_t in_page = 0;
           const uint32_t r0 = lane * a.box_rows;
-          for (uint32_t r = 0; r < 2 * n; ++r) {
-            const bool kv = load_is_value(SHARED, r, n);
-            if (!kv || SHARED) {      // (a tile's values follow its keys otherwise)
-              const int32_t pos = (w.blk.kt0 + t + (int32_t)load_tile(SHARED, r, n) - tile0) * (int32_t)kKeys + (int32_t)r0;
-              page = -1;
-              if (lane < pieces && pos < w.seq.len) page = kv_page(a.b, a.c.n_pages, a.c.page_size, w.s, pos);
-              in_page = (uint32_t)pos % a.c.page_size;
-            }
+          auto place = [&](int32_t tile, int32_t& page, uint32_t& in_page) {      // of the lane's piece of a tile, counted from the sequence's beginning
+            const int32_t pos = tile * (int32_t)kKeys + (int32_t)r0;
+            page = -1;
+            if (lane < pieces && pos < w.seq.len) page = kv_page(a.b, a.c.n_pages, a.c.page_size, w.s, pos);
+            in_page = (uint32_t)pos % a.c.page_size;
+          };
+          auto load = [&](uint32_t q, bool kv, int32_t page, uint32_t in_page) {
             const int32_t where = page < 0 ? (int32_t)a.c.n_pages : page;      // outside the cache: zeros
-            const uint32_t q = 2 * jg + r, ring = Q ? C::kRaws : C::kSlots, slot = q % ring, sc = q % C::kScaleSlots;
+            const uint32_t ring = Q ? C::kRaws : C::kSlots, slot = q % ring, sc = q % C::kScaleSlots;
             const uint32_t bar = (Q ? raw_full : full) + 8 * slot, sbar = scale_full + 8 * sc;
             if (q >= ring) ok = wait_or_give_up((Q ? raw_empty : empty) + 8 * slot, (q / ring + 1) & 1, ok, a.error);
             if (Q && q >= C::kScaleSlots) ok = wait_or_give_up(scale_empty + 8 * sc, (q / C::kScaleSlots + 1) & 1, ok, a.error);
@@ -917,9 +923,25 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               bar_arrive(bar);
               if (Q) bar_arrive(sbar);
             }
+          };
+          int32_t page;
+          uint32_t in_page;
+          t = max(t, tile0);
+          if (SHARED) {
+            const uint32_t n = (uint32_t)(stop - t);
+            for (uint32_t r = 0; r < 2 * n; ++r) {
+              place(w.blk.kt0 + t - tile0 + (int32_t)load_tile(true, r, n), page, in_page);
+              load(2 * jg + r, load_is_value(true, r, n), page, in_page);
+            }
+            jg += n;
+            t = stop;
+          } else {
+            for (; t < stop; ++t, ++jg) {
+              place(w.blk.kt0 + t - tile0, page, in_page);
+#pragma unroll
+              for (uint32_t kv = 0; kv < 2; ++kv) load(2 * jg + kv, kv, page, in_page);
+            }
           }
-          jg += n;
-          t = stop;
           if (t < end) walk_on<TREE>(w, a, cum, skip_rows);
         }
         // every load lands before the block ends, also where the others gave up waiting and left some unread
@@ -936,23 +958,28 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       bool ok = true;
       Walk w = walk_to<TREE>(a, cum, skip_rows, begin);
       int32_t t = begin;
-      uint32_t item = 0, q = 0, r = 0;                // loads of the block so far, and of the item
-      for (; t < end; ++q) {
-        if (r == 0) t = max(t, w.item0 + kItemCost);
-        const uint32_t n = (uint32_t)(min(end, w.item0 + w.blk.n) - t);
+      uint32_t item = 0, r = 0;                       // (shared tiles: loads of the item so far)
+      for (uint32_t q = 0; t < end; ++q) {
+        if (SHARED ? r == 0 : (q & 1) == 0) t = max(t, w.item0 + kItemCost);
+        const uint32_t n = SHARED ? (uint32_t)(min(end, w.item0 + w.blk.n) - t) : 0;
+        const bool is_value = SHARED ? load_is_value(true, r, n) : (q & 1) != 0;
         const uint32_t raw = q % C::kRaws, slot = q % C::kSlots, sc = q % C::kScaleSlots;
         ok = wait_or_give_up(scale_full + 8 * sc, (q / C::kScaleSlots) & 1, ok, a.error);
-        if (load_is_value(SHARED, r, n)) {
+        if (is_value) {
           // a weight of zero must not meet a scale that is none: one past the end may be anything, and one that is not
           // finite is taken out here and added to the rows that see it at the end
           float* at = reinterpret_cast<float*>(smem + C::kOffScale) + sc * kKeys + row;
-          const bool past = (w.blk.kt0 + t + (int32_t)load_tile(SHARED, r, n) - w.item0 - kItemCost) * (int32_t)kKeys + (int32_t)row >= w.seq.len;
+          const bool past = (w.blk.kt0 + t + (SHARED ? (int32_t)load_tile(true, r, n) : 0) - w.item0 - kItemCost) * (int32_t)kKeys + (int32_t)row >= w.seq.len;
           if (past || !isfinite(*at)) {
             if (!past) misc[8 + item % 8] = 1;
             *at = 0.f;                // (ordered before the next load into the same place by the fence below: see kScaleSlots)
           }
+          if (!SHARED && ++t == min(end, w.item0 + w.blk.n) && t < end) {
+            walk_on<TREE>(w, a, cum, skip_rows);
+            ++item;
+          }
         }
-        if (++r == 2 * n) {
+        if (SHARED && ++r == 2 * n) {
           r = 0;
           t += (int32_t)n;
           if (t < end) {
