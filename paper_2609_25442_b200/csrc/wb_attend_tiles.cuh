@@ -770,7 +770,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
                     y[k] = pack_bf16x2(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv);
                   *reinterpret_cast<uint4*>(dst + (c + 8 * e) * 2) = make_uint4(y[0], y[1], y[2], y[3]);
                 }
-            } else {
+            } else if (!TREE || x0.in) {      // (a tree's rows may be few of a tile: the others' places are not read)
 #pragma unroll
               for (int e = 0; e < W; ++e) part[(c + e) * 128] = __uint_as_float(o[e]);
             }

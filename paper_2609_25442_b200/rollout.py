@@ -206,13 +206,10 @@ class KvCache:
         """Attention of the new tokens' queries (bf16, [n_tokens, n_heads, head_dim]) over the cache, causal at the
         sequences' ends; window > 0 limits a query to that many latest positions.  Returns (out, lse), which are confirmed when
         workspace.check() has passed after them; rows that no sequence holds are left as they are."""
-        a, h, b, out, lse = self._attention(batch, q, workspace, window, out, lse)
-        self._kv.attend(batch._for(self), a, h, b, lse.data_ptr(), self._scale if scale is None else scale, window,
-                        workspace.pointer, workspace.bytes, _stream(self._index))
-        return out, lse
+        return self._attend(batch, q, workspace, scale, window, out, lse, None)
 
-    def _attention(self, batch: KvBatch, q: torch.Tensor, workspace: "AttendWorkspace", window: int, out: Optional[torch.Tensor],
-                   lse: Optional[torch.Tensor]):
+    def _attend(self, batch: KvBatch, q: torch.Tensor, workspace: "AttendWorkspace", scale: Optional[float], window: int,
+                out: Optional[torch.Tensor], lse: Optional[torch.Tensor], tree: Optional["DraftTree"]):
         if q.dim() != 3:
             raise ValueError("q: [n_tokens, n_heads, head_dim]")
         if workspace.device is not self.device and workspace.device != self.device:
@@ -230,7 +227,17 @@ class KvCache:
             lse = self._like[torch.float32].new_empty((n, h))
         elif lse.shape != (n, h) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != self.device:
             raise ValueError("lse: contiguous fp32 [n_tokens, n_heads]")
-        return a, h, b, out, lse
+        args = batch._for(self)
+        if scale is None:
+            scale = self._scale
+        if tree is None:
+            self._kv.attend(args, a, h, b, lse.data_ptr(), scale, window, workspace.pointer, workspace.bytes, _stream(self._index))
+            return out, lse
+        if 32 * tree.words < args.max_new or 0 < window < args.max_new:
+            raise ValueError(f"trees of up to {args.max_new} rows: the tree's mask has {32 * tree.words} bits, and a window is 0 or at least that many")
+        self._kv.attend_tree(args, tree.mask.data_ptr(), tree.words, a, h, b, lse.data_ptr(), scale, window, workspace.pointer, workspace.bytes,
+                             _stream(self._index))
+        return out, lse
 
     def write_rotated(self, batch: KvBatch, rotation: "Rotation", k: torch.Tensor, v: torch.Tensor, *, q: Optional[torch.Tensor] = None,
                       positions: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
@@ -275,13 +282,7 @@ class KvCache:
         them as its depth has it) and its ancestors.  A window is at least the batch's max_new."""
         if tree.mask.shape[0] != batch.n_tokens or tree.device != self.device:
             raise ValueError("tree: of the batch's rows, on the cache's device")
-        a, h, b, out, lse = self._attention(batch, q, workspace, window, out, lse)
-        args = batch._for(self)
-        if 32 * tree.words < args.max_new or 0 < window < args.max_new:
-            raise ValueError(f"trees of up to {args.max_new} rows: the tree's mask has {32 * tree.words} bits, and a window is 0 or at least that many")
-        self._kv.attend_tree(args, tree.mask.data_ptr(), tree.words, a, h, b, lse.data_ptr(), self._scale if scale is None else scale, window,
-                             workspace.pointer, workspace.bytes, _stream(self._index))
-        return out, lse
+        return self._attend(batch, q, workspace, scale, window, out, lse, tree)
 
     def keep(self, batch: KvBatch, path: torch.Tensor, accepted: torch.Tensor) -> None:
         """Moves the rows of accepted paths (`path` [n_seqs, depth], `accepted` [n_seqs], as verify_tree returns them) to the places
