@@ -17,9 +17,13 @@
 //   - One warp issues all products in the order  QK0 QK1 | PV0 QK0' PV1 QK1' | ..., one requests cache tiles into a
 //     ring of slots (keys, values, keys, ...) by tensor-map loads, a box per page piece and lane.
 //   - E4M3 caches: tiles arrive as codes, four more warps widen them to bf16 slots; the row scales multiply scores and
-//     weights in the softmax, where each is a value of its own.  This takes 682 us where bf16 takes 430 (tensor core 36 % busy,
+//     weights in the softmax, where each is a value of its own.  This takes 692 us where bf16 takes 430 (tensor core 36 % busy,
 //     issue slots 45 %, ALU 32 %): the step's chain is a microsecond longer, by the scales' loads, products and barriers, and by the
 //     widening warps' share of the schedulers; 616 us with nothing widened, 530 without scales as well.
+//   - Trees of at most 128 rows each have one tile of rows, with which half of the block would idle.  Both groups of softmax warps then hold the
+//     same rows and take every other cache tile, so that the loads are the bound: 1.35 us a tile and SM, 6.5 TB/s of a bf16 cache (E4M3 1.7
+//     to 1.8, widening).  24 trees of 9 to 27 rows of 4 heads over 300 to 6000 positions: 79 to 82 us, of which the cache's bytes are 51, the rest
+//     set-up, 2 to 3 changes of items per block and the join.
 //   - Work is cut as in the kernel for few rows: one line of 128-row tiles over all (sequence, kv head, row block)
 //     items, an equal share for every SM; a second kernel joins the cut items.
 #pragma once
@@ -390,7 +394,7 @@ __global__ void __launch_bounds__(TilesCfg<D, Q>::kThreads, 1)
 wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                        uint32_t skip_rows) {
   using C = TilesCfg<D, Q>;
-  constexpr bool TREE = MODE != Rows256::kChunk, SHARED = MODE == Rows256::kTreeShared;
+  constexpr bool TREE = MODE != Rows256::kChunk, SHARED = MODE == Rows256::kTreeShared, kEarly = SHARED || D == 64;
   extern __shared__ __align__(1024) char smem[];
   const uint32_t base = smem_addr(smem);
   const uint32_t tid = threadIdx.x, warp = uniform(tid >> 5), lane = tid & 31;
@@ -511,7 +515,6 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       for (int32_t t = begin; t < end; ++item) {
         const int32_t item1 = w.item0 + w.blk.n, stop = min(end, item1), tile0 = w.item0 + kItemCost;      // the item's first tile in the line
         t = max(t, tile0);
-        const int32_t from = t;
         const uint32_t n_rows = (uint32_t)w.seq.n_new * a.group;
         const int32_t base_pos = w.seq.len - w.seq.n_new;
         // tiles that not every row of the block sees whole
@@ -587,6 +590,10 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               unpack2(mul2(pack2(x[c], x[c + 1]), f.x), x[c], x[c + 1]);
               unpack2(mul2(pack2(x[c + 2], x[c + 3]), f.y), x[c + 2], x[c + 3]);
             }
+            // the keys' scales are done with, and the load that waits for their place can go on a microsecond before the step's end (tiles
+            // shared out: 2.85 -> 2.26 us a tile, the other group's threads do not read them; chunks with heads of 64: 678 -> 575 us for 2048
+            // tokens over 16384 positions, with heads of 128 692 -> 720)
+            if (kEarly) bar_arrive_n(scale_empty + 8 * sk, SHARED ? 2 : 1);
           }
           // masks: a bit per column for both ends at once, in groups of columns that some row of the warp does not see whole
           // (a comparison and a selection per column and end took 1.1 us of the step)
@@ -671,12 +678,12 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             bar_arrive(p_full + 8 * i);
           }
           if (Q) {
-            bar_arrive_n(scale_empty + 8 * sk, SHARED ? 2 : 1);      // for the other group's threads too, which do not read them
+            if (!kEarly) bar_arrive(scale_empty + 8 * sk);
             bar_arrive_n(scale_empty + 8 * sv, SHARED ? 2 : 1);
           }
         };
         if (SHARED) {
-          for (uint32_t j = i; j < n_tiles; j += 2) step(from + (int32_t)j, 2 * jg + key_load(true, j), 2 * jg + value_load(true, j, n_tiles), j < 2, false);
+          for (uint32_t j = i; j < n_tiles; j += 2) step(t + (int32_t)j, 2 * jg + key_load(true, j), 2 * jg + value_load(true, j, n_tiles), j < 2, false);
           jg += n_tiles;
           t = stop;
         } else {
@@ -756,7 +763,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               float y[W];
 #pragma unroll
               for (int e = 0; e < W; ++e) y[e] = __uint_as_float(o[e]);
-              add_odd_values<Q, TREE, W>(a, w, w.blk.kt0 + from - tile0, w.blk.kt0 + stop - tile0, x0.lo, x0.hi, x0.tok, c, y);
+              add_odd_values<Q, TREE, W>(a, w, w.blk.kt0 + max(begin - tile0, 0), w.blk.kt0 + stop - tile0, x0.lo, x0.hi, x0.tok, c, y);
 #pragma unroll
               for (int e = 0; e < W; ++e) o[e] = __float_as_uint(y[e]);
             }
@@ -992,10 +999,15 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         if (q >= C::kSlots) ok = wait_or_give_up(empty + 8 * slot, (q / C::kSlots + 1) & 1, ok, a.error);
         const char* src = smem + C::kOffRaw + raw * C::kRawBytes + row * D;
         char* dst = smem + C::kOffSlots + slot * C::kSlotBytes + row * 128;
+        // (tiles shared out, where widening is what they wait for: the whole row is read before any of it is written, because the compiler does
+        // not move a read past a write; 1.8 -> 1.7 us a tile)
+        uint4 codes[D / 16];
+#pragma unroll
+        for (uint32_t c = 0; SHARED && c < D / 16; ++c) codes[c] = *reinterpret_cast<const uint4*>(src + (D == 128 ? ((c ^ (row & 7)) << 4) : ((c ^ ((row >> 1) & 3)) << 4)));
 #pragma unroll
         for (uint32_t c = 0; c < D / 16; ++c) {
-          const uint4 x = *reinterpret_cast<const uint4*>(src + (D == 128 ? ((c ^ (row & 7)) << 4) : ((c ^ ((row >> 1) & 3)) << 4)));
-          const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+          if (!SHARED) codes[c] = *reinterpret_cast<const uint4*>(src + (D == 128 ? ((c ^ (row & 7)) << 4) : ((c ^ ((row >> 1) & 3)) << 4)));
+          const uint32_t xs[4] = {codes[c].x, codes[c].y, codes[c].z, codes[c].w};
           uint32_t y[8];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {

@@ -127,6 +127,22 @@ def test_write_rotated(dtype, src, dim, page, heads, kv_heads, lens, new, part, 
     assert int((~c.k_all.float().isnan()).sum()) == live and int((~c.v_all.float().isnan()).sum()) == live
 
 
+def test_write_rotated_many_tokens():
+    """More tokens than a block looks up at once (32 of them ahead of the rows): ragged chunks, some without tokens."""
+    rng = np.random.default_rng(6)
+    new = [int(x) for x in rng.integers(0, 700, 60)]
+    c = Case([x + int(y) for x, y in zip(new, rng.integers(0, 50, 60))], new, 2, 1, 64, 16, torch.bfloat16)
+    n = sum(new)
+    assert n > 2 * 296 * 32
+    q, k, v = (torch.tensor(rng.normal(size=(n, h, 64)), dtype=torch.float32, device=DEV) for h in (2, 1, 1))
+    cos, sin = (torch.tensor(x, device=DEV) for x in angles(max(c.lens), 32))
+    place = torch.tensor(np.concatenate([np.arange(length - m, length) for length, m in zip(c.lens, new)]), device=DEV).long()
+    got = c.cache.write_rotated(c.batch, rollout.Rotation(cos, sin), k, v, q=q)
+    turned = lambda x: torch.cat([x[..., :32] * cos[place][:, None] - x[..., 32:] * sin[place][:, None], x[..., 32:] * cos[place][:, None] + x[..., :32] * sin[place][:, None]], -1)
+    rk, rv = c.cache.read(c.batch)
+    assert torch.equal(got, turned(q).bfloat16()) and torch.equal(rk, turned(k).bfloat16()) and torch.equal(rv, v.bfloat16())
+
+
 def test_write_rotated_in_place_and_edges():
     """Queries in place; a token without a page still has its queries turned; a position outside the table gives NaN; rows that no
     sequence holds are left as they are."""
@@ -679,3 +695,18 @@ def test_a_captured_step():
         want = step()
         assert all(torch.equal(a.view(torch.uint8) if a.dtype == torch.uint8 else a.nan_to_num(7.0), b.nan_to_num(7.0)) for a, b in zip(got, want))
     ws.check()
+
+
+@pytest.mark.parametrize("dtype,seqs", [(torch.bfloat16, 600), (E4M3, 150)])
+@pytest.mark.parametrize("new", [3, 24])
+def test_many_sequences(dtype, seqs, new):
+    """More sequences than one launch of the kernel for long sequences takes, of few rows and of many; a sample of them is checked."""
+    rng = np.random.default_rng(seqs + new)
+    sizes = [int(x) for x in rng.integers(0, new + 1, seqs)]
+    c = Case([x + int(y) for x, y in zip(sizes, rng.integers(0, 300, seqs))], sizes, 4, 2, 64, 16, dtype)
+    fill(c)
+    loosen(c)
+    trees, parent = parents_of(c)
+    q = c.queries()
+    out, lse = attend(c, q, rollout.DraftTree(c.batch, parent))
+    check(c, q, out, lse, [bits_of(p) for p in trees], only=set(range(0, seqs, 37)) | {seqs - 1, 127, 128, 511 % seqs, 512 % seqs})
