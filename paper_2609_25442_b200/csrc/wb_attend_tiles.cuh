@@ -565,18 +565,22 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           }
           const int32_t pos0 = (w.blk.kt0 + tile - tile0) * (int32_t)kKeys;
           const bool cut = pos0 + (int32_t)kKeys - 1 > cut_hi || pos0 < cut_lo;
-          if (!Q && cut && (i == 0 || SHARED)) {
-            // Values past the end, and values that are not finite, must not meet weights of zero.  Only the first tile's threads
-            // (those that alone use the cache tile, where tiles are shared out) write, one to a row: each then orders its own writes before
-            // the products, which wait for this tile's weights first, and the other tile's products follow this one's.
+          // Values past the end, and values that are not finite, must not meet weights of zero.  Only the first tile's threads
+          // (those that alone use the cache tile, where tiles are shared out) write, one to a row: each then orders its own writes before
+          // the products, which wait for this tile's weights first, and the other tile's products follow this one's.
+          auto clear = [&]() {
             const uint32_t slot = qv % C::kSlots;
             ok = wait_or_give_up(full + 8 * slot, (qv / C::kSlots) & 1, ok, a.error);
             if (clear_values<D>(smem + C::kOffSlots + slot * C::kSlotBytes, row, pos0 + (int32_t)row >= w.seq.len, misc + 8 + item % 8)) fence_async();
-          }
+          };
+          if (!Q && !SHARED && cut && i == 0) clear();
           float x[128];
           ok = wait_or_give_up(s_full + 8 * i, js & 1, ok, a.error);
           ++js;
           tc_after();
+          // (Shared tiles: not before the scores are there.  The slot's last user may be the keys before these, which are the other group's:
+          // until they have arrived, the barrier's phase before last would pass for these values', and another tile would be cleared.)
+          if (!Q && SHARED && cut) clear();
 #pragma unroll
           for (int c = 0; c < 128; c += 32) tm_load32(tm_s + c, reinterpret_cast<uint32_t*>(x) + c);
           if (!SHARED && last && stop < end) prepare_next();
