@@ -712,14 +712,28 @@ def test_many_sequences(dtype, seqs, new):
     check(c, q, out, lse, [bits_of(p) for p in trees], only=set(range(0, seqs, 37)) | {seqs - 1, 127, 128, 511 % seqs, 512 % seqs})
 
 
+def check_products(c, trees, q, got, window=0):
+    """Against products in 64 bits on the device, within the bound of the other tests."""
+    t, g = 0, c.heads // c.kv_heads
+    for s, (k, v) in enumerate(c.values_of()):
+        n, length = c.new[s], c.lens[s]
+        k, v = (torch.tensor(x, device=DEV).repeat_interleave(g, 0) for x in (k, v))
+        hidden = torch.tensor(~orc.tree_sees(bits_of(trees[s]), length, window), device=DEV)
+        w = torch.softmax((q[t:t + n].float().transpose(0, 1).double() @ k.double().transpose(1, 2) * c.dim ** -0.5).masked_fill(hidden, -math.inf), -1)
+        want, mag = (w @ v.double()).transpose(0, 1), (w @ v.abs().double()).transpose(0, 1)
+        for x in got:
+            assert bool(((x[t:t + n] - want).abs() <= 2.0 ** -8 * (1 + 2.0 ** -6) * (want.abs() + mag) + 1e-6).all()), s
+        t += n
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
-@pytest.mark.parametrize("heads,kv_heads,dim,new", [(32, 8, 128, 27), (32, 8, 64, 20), (16, 4, 128, 63)])
+@pytest.mark.parametrize("heads,kv_heads,dim,new", [(32, 8, 128, 27), (32, 8, 64, 20), (16, 4, 128, 63), (32, 8, 128, 4), (32, 8, 64, 8)])
 def test_long_items_in_a_row(dtype, heads, kv_heads, dim, new):
     """Blocks that go through several items of many tiles each, whose last tiles end anywhere: a slot of the ring must not be touched before
-    its turn.  Three passes each, against products in 64 bits, within the bound of the other tests."""
+    its turn.  Three passes each."""
     rng = np.random.default_rng(dim + new)
     seqs = 24
-    sizes = [int(x) for x in rng.integers(max(9, new // 3), new + 1, seqs)]
+    sizes = [int(x) for x in rng.integers(max(1, new // 3), new + 1, seqs)]
     c = Case([int(x) for x in rng.integers(400, 2300, seqs)], sizes, heads, kv_heads, dim, 32, dtype)
     fill(c)
     trees, parent = parents_of(c)
@@ -728,13 +742,17 @@ def test_long_items_in_a_row(dtype, heads, kv_heads, dim, new):
     ws = rollout.AttendWorkspace(c.cache, heads, seqs)
     got = [c.cache.attend_tree(c.batch, q, tree, workspace=ws)[0].float() for _ in range(3)]
     ws.check()
-    t, g = 0, heads // kv_heads
-    for s, (k, v) in enumerate(c.values_of()):
-        n, length = sizes[s], c.lens[s]
-        k, v = (torch.tensor(x, device=DEV).repeat_interleave(g, 0) for x in (k, v))
-        hidden = torch.tensor(~orc.tree_sees(bits_of(trees[s]), length), device=DEV)
-        w = torch.softmax((q[t:t + n].float().transpose(0, 1).double() @ k.double().transpose(1, 2) * dim ** -0.5).masked_fill(hidden, -math.inf), -1)
-        want, mag = (w @ v.double()).transpose(0, 1), (w @ v.abs().double()).transpose(0, 1)
-        for x in got:
-            assert bool(((x[t:t + n] - want).abs() <= 2.0 ** -8 * (1 + 2.0 ** -6) * (want.abs() + mag) + 1e-6).all()), s
-        t += n
+    check_products(c, trees, q, got)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("lens,new,heads,kv_heads,dim,window", [([9001], [8], 32, 8, 128, 0), ([9001, 77], [2, 1], 8, 2, 64, 0), ([15999], [60], 4, 2, 64, 0),
+                                                                ([5000, 4000, 100], [30, 9, 12], 12, 3, 128, 0), ([9001, 300], [70, 40], 5, 1, 128, 3001)])
+def test_few_long_sequences(dtype, lens, new, heads, kv_heads, dim, window):
+    """What a cluster of blocks shares out: many tiles to a block, several blocks of rows, sequences that are much shorter."""
+    c = Case(lens, new, heads, kv_heads, dim, 16, dtype)
+    fill(c)
+    trees, parent = parents_of(c)
+    q = c.queries()
+    out, _ = attend(c, q, rollout.DraftTree(c.batch, parent), window=window)
+    check_products(c, trees, q, [out.float()], window)
