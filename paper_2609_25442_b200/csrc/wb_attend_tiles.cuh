@@ -22,7 +22,7 @@
 //     widening warps' share of the schedulers; 616 us with nothing widened, 530 without scales as well.
 //   - Trees of at most 128 rows each have one tile of rows, with which half of the block would idle.  Both groups of softmax warps then hold the
 //     same rows and take every other cache tile, so that the loads are the bound: 1.35 us a tile and SM, 6.5 TB/s of a bf16 cache (E4M3 1.7
-//     to 1.8, widening).  24 trees of 9 to 27 rows of 4 heads over 300 to 6000 positions: 79 to 82 us, of which the cache's bytes are 51, the rest
+//     to 1.8, widening).  24 trees of 9 to 27 rows of 4 heads over 300 to 6000 positions: 80 to 88 us, of which the cache's bytes are 51, the rest
 //     set-up, 2 to 3 changes of items per block and the join.
 //   - Work is cut as in the kernel for few rows: one line of 128-row tiles over all (sequence, kv head, row block)
 //     items, an equal share for every SM; a second kernel joins the cut items.

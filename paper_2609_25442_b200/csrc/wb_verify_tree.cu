@@ -9,7 +9,7 @@
 // (an exchange per step would cost more), so all of them come to the same passes, of which each takes its share; sums
 // are joined in the blocks' order in 64 bits, the race by the maximum of a 64-bit key.
 //
-// One tree of 60 rows, certain drafter, 151936 fp32: 14.4 us on the device.  48 sampled trees of up to 24 rows, 128256 bf16: 34 us, of which the
+// One tree of 60 rows, certain drafter, 151936 fp32: 14.4 to 16.4 us on the device.  48 sampled trees of up to 24 rows, 128256 bf16: 34 to 35 us, of which the
 // rows of the last pass are 7.5; the trees with the most rejected siblings make the most passes, 3 us each, and the others wait for
 // them.  (62 us with what is left formed element by element over the siblings, a loop of ten instructions each.)
 #include <cooperative_groups.h>
