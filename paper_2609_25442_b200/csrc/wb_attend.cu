@@ -75,7 +75,8 @@ template <int D, bool Q, bool TREE>
 cudaError_t launch_rows_of(uint32_t rows, const AttendArgs& a, int dev, cudaStream_t stream) {
   if (rows <= 8) return launch_rows<D, Q, 1, TREE>(a, dev, stream);
   if (rows <= 16) return launch_rows<D, Q, 2, TREE>(a, dev, stream);
-  return launch_rows<D, Q, 4, TREE>(a, dev, stream);
+  if constexpr (!TREE || Q) return launch_rows<D, Q, 4, TREE>(a, dev, stream);
+  return cudaErrorInvalidValue;        // (bf16 trees of more rows go to the other kernel)
 }
 
 template <int D, bool Q, Rows256 MODE>
@@ -205,8 +206,8 @@ template <bool TREE> wb_status launch_attend(const AttendArgs& a, const wb_kv* k
   const bool e = kv->d.dtype == WB_E4M3;
   const uint64_t rows = (uint64_t)batch->max_new * a.group;
   cudaError_t err = cudaSuccess;
-  bool taken = false;
-  if (TREE) {
+  if constexpr (TREE) {
+    bool taken = false;
     // tiles that a row may see: up to max_len, or of a window and the tree (which may begin within a tile)
     const uint64_t reach = a.window ? std::min<uint64_t>(batch->max_len, (uint64_t)a.window + batch->max_new) : batch->max_len;
     const uint32_t tiles = (uint32_t)std::max<uint64_t>(1, (reach + kKvTile - 1) / kKvTile + (a.window ? 1 : 0));

@@ -326,8 +326,9 @@ class Rotation:
 class DraftTree:
     """The trees that a batch's new tokens are: `parent` (int32 [n_tokens]) is the row that a row continues, counted within
     its sequence's new tokens, and an earlier one; any other value makes it a root, as row 0 always is.  `mask` [n_tokens, words] (int32)
-    holds a row's ancestors and itself as bits, `positions` [n_tokens] the place before the new tokens plus one plus the depth.  Rows that
-    no sequence holds are undefined in both.  build() finds them again after the batch's or the parents' tensors were changed."""
+    holds a row's ancestors and itself as bits, `positions` [n_tokens] the first new token's place plus the depth.  Rows that
+    no sequence holds are undefined in both.  A mask's row has as many bits as the batch's max_new (give it: the default, n_tokens, makes
+    masks of n_tokens^2 bits, and attention of few rows slower).  build() finds them again after the batch's or the parents' tensors were changed."""
 
     def __init__(self, batch: KvBatch, parent: torch.Tensor):
         _require(parent.shape == (batch.n_tokens,) and parent.is_contiguous(), "parent: contiguous, [n_tokens]")
