@@ -257,7 +257,7 @@ extern "C" wb_status wb_kv_attend_tree(const wb_kv* kv, const wb_kv_batch* batch
   if (((uintptr_t)mask & 3u) || (uint64_t)words * 32 < batch->max_new || words > 0x7FFFFFu) return WB_ERR_INVALID_ARG;
   // a window that reaches back over a whole tree never ends inside one
   if (window && window < batch->max_new) return WB_ERR_INVALID_ARG;
-  if (!todo) return WB_OK;
+  if (!todo || !batch->max_new) return WB_OK;      // (without new tokens there are rows that no sequence holds, and no trees)
   if (!mask || !words) return WB_ERR_INVALID_ARG;
   a.mask = mask;
   a.words = words;

@@ -756,3 +756,29 @@ def test_few_long_sequences(dtype, lens, new, heads, kv_heads, dim, window):
     q = c.queries()
     out, _ = attend(c, q, rollout.DraftTree(c.batch, parent), window=window)
     check_products(c, trees, q, [out.float()], window)
+
+
+@pytest.mark.parametrize("max_len", [64, 100000])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+def test_a_step_whose_rows_no_sequence_holds(dtype, max_len):
+    """A padded step: five rows, no new tokens.  Nothing is moved, attended or accepted, and every row is left as it is."""
+    c = Case([40, 17], [0, 0], 4, 2, 64, 16, dtype)
+    fill(c)
+    before = c.k.view(torch.uint8).clone(), c.v.view(torch.uint8).clone()
+    b = c.batch
+    batch = rollout.KvBatch(b.page_table, b.new_start, b.kv_len, n_tokens=5, max_new=0, max_len=max_len)
+    tree = rollout.DraftTree(batch, torch.zeros(5, **I32))
+    q, k, v = (torch.randn(5, h, 64, device=DEV).bfloat16() for h in (4, 2, 2))
+    turned = torch.full((5, 4, 64), 2.0, device=DEV).bfloat16()
+    c.cache.write_rotated(batch, rollout.Rotation.of(64, 100000, device=DEV), k, v, q=q, q_out=turned)
+    ws = rollout.AttendWorkspace(c.cache, 4, 2)
+    for call in (lambda **kw: c.cache.attend_tree(batch, q, tree, workspace=ws, **kw), lambda **kw: c.cache.attend(batch, q, workspace=ws, **kw)):
+        out, lse = torch.full((5, 4, 64), 3.0, device=DEV).bfloat16(), torch.full((5, 4), 5.0, device=DEV)
+        call(out=out, lse=lse)
+        call(out=out, lse=lse, window=7)
+        ws.check()
+        assert bool((out == 3).all()) and bool((lse == 5).all())
+    accepted, path, emitted = rollout.verify_tree(tree, torch.rand(5, 9, device=DEV), None, torch.zeros(5, **I32), torch.rand(5, device=DEV), torch.rand(2, 9, device=DEV), max_depth=2)
+    assert accepted.tolist() == [0, 0] and bool((path == -1).all()) and bool((emitted == -1).all())
+    c.cache.keep(batch, path, accepted)
+    assert bool((turned == 2).all()) and all(torch.equal(x.view(torch.uint8), y) for x, y in zip((c.k, c.v), before))
