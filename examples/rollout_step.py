@@ -156,13 +156,14 @@ def main() -> None:
     ap.add_argument("--tree", type=int, nargs="+", metavar="WIDTH", help="children of every row, level by level")
     args = ap.parse_args()
     weights, spec = remapped_weights()
-    most = 1 + args.drafts
+    most = per = 1 + args.drafts               # rows of a step, and tokens that it may add to a sequence
     if args.tree:
+        per = 1 + len(args.tree)
         level = most = 1
         for width in args.tree:
             level *= width
             most += level
-    engine = Engine(weights, spec, n_seqs=4, max_len=64 + args.steps * (args.drafts + 1) + most, rotary=bool(args.tree),
+    engine = Engine(weights, spec, n_seqs=4, max_len=64 + args.steps * per + most, rotary=bool(args.tree),
                     cache_dtype=torch.float8_e4m3fn if args.cache == "e4m3" else torch.bfloat16)
     engine.prefill(torch.randint(0, spec.V, (4, 37), device=engine.dev, generator=engine.g))
     total = 0
