@@ -782,3 +782,63 @@ def test_a_step_whose_rows_no_sequence_holds(dtype, max_len):
     assert accepted.tolist() == [0, 0] and bool((path == -1).all()) and bool((emitted == -1).all())
     c.cache.keep(batch, path, accepted)
     assert bool((turned == 2).all()) and all(torch.equal(x.view(torch.uint8), y) for x, y in zip((c.k, c.v), before))
+
+
+@pytest.mark.parametrize("loose", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("new,heads,kv_heads,dim,page,window", [([6, 3, 5, 6], 4, 2, 128, 16, 8), ([30, 12, 9, 30], 2, 2, 64, 48, 33), ([20, 9, 1, 31], 8, 2, 128, 16, 64),
+                                                               ([60, 33, 64, 5], 4, 2, 64, 32, 100), ([129, 60, 128, 7], 8, 2, 128, 16, 130), ([70, 9, 2, 70], 16, 4, 64, 16, 90)])
+def test_any_mask_under_a_window(new, heads, kv_heads, dim, page, window, dtype, loose):
+    """A row that sees few of the new rows has a window that begins before any tree's would.  Here the window of a row whose mask is empty begins
+    at the last position of a tile of 128, of 64, or anywhere, or reaches over the whole sequence; the position before it holds
+    infinities and NaN."""
+    before = [window + 255, window + 63, window + 100, window - 3]        # the tokens before the new ones
+    c = Case([b + n for b, n in zip(before, new)], new, heads, kv_heads, dim, page, dtype)
+    fill(c)
+    if loose:
+        loosen(c)
+    bits = [c.rng.random((n, n)) < 0.3 for n in new]
+    for b in bits:
+        b[0], b[len(b) // 2], b[-1] = False, False, False
+    tree = rollout.DraftTree(c.batch, torch.full((c.total,), -1, **I32))
+    full, t = np.zeros((c.total, tree.words * 32), bool), 0
+    for b in bits:
+        full[t:t + len(b), :len(b)] = b
+        t += len(b)
+    tree.mask.copy_(pack(full, tree.words))
+    values = c.values_of()
+    for s in range(3):
+        pos = before[s] - window - 1
+        at = int(c.table[s, pos // page]), slice(None), pos % page
+        if dtype == E4M3:
+            c.ks[at], c.vs[at] = math.nan, math.inf
+        else:
+            c.k[at], c.v[at] = math.inf, math.nan
+        for x in values[s]:
+            x[:, pos] = 0                                # (the oracle multiplies what no row sees by nothing, but looks for its largest key)
+    c.values_of = lambda: values
+    q = c.queries()
+    out, lse = attend(c, q, tree, window=window)
+    check(c, q, out, lse, bits, window)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, E4M3])
+@pytest.mark.parametrize("seqs,new,kv_heads", [(4, 6, 2), (4, 16, 2), (4, 60, 2), (4, 200, 1), (160, 6, 4), (160, 16, 4), (160, 60, 2), (160, 200, 1)])
+def test_too_long_sequences_of_every_kernel(seqs, new, kv_heads, dtype):
+    """Where clusters do not take a batch (a far bound, or more sequences than fit at once), a sequence beyond max_len is reported all the
+    same, has zeros, and the others have their results."""
+    rng = np.random.default_rng(seqs + new)
+    sizes = [new] + [int(x) for x in rng.integers(1, max(2, new if seqs < 100 else new // 8), seqs - 1)]
+    c = Case([n + int(x) for n, x in zip(sizes, rng.integers(0, 300, seqs))], sizes, 4, kv_heads, 64, 16, dtype)
+    fill(c)
+    trees, parent = parents_of(c)
+    lens, most = c.batch.kv_len.clone(), 20000 if seqs < 100 else 600
+    lens[0] = most + 1
+    batch = rollout.KvBatch(c.batch.page_table, c.batch.new_start, lens, n_tokens=c.total, max_new=new, max_len=most)
+    q, ws = c.queries(), rollout.AttendWorkspace(c.cache, 4, seqs)
+    out, lse = c.cache.attend_tree(batch, q, rollout.DraftTree(batch, parent), workspace=ws)
+    assert bool((out[:new] == 0).all()) and bool(lse[:new].isneginf().all())
+    with pytest.raises(Exception, match="INVALID_ARG"):
+        ws.check()
+    ws.check()
+    check(c, q, out, lse, [bits_of(p) for p in trees], only=set(range(1, seqs, max(1, seqs // 8))) | {seqs - 1})
