@@ -203,9 +203,6 @@ struct Walk {
   int32_t item0;           // the item's first tile in the line
 };
 
-// Whether an item's rows are one tile.
-__device__ __forceinline__ bool one_tile(const Walk& w, uint32_t group) { return (uint32_t)w.seq.n_new * group <= w.rb * kQRows + 128; }
-
 // A block's share of the line begins at the multiple of `per` that is its number, moved to the next end of an item where that is
 // not more than kSnap tiles away: joining a cut item costs more than so many tiles.  So an item [i0, i1) is cut at the multiples
 // of `per` that lie more than kSnap tiles inside.
@@ -515,6 +512,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
       for (int32_t t = begin; t < end; ++item) {
         const int32_t item1 = w.item0 + w.blk.n, stop = min(end, item1), tile0 = w.item0 + kItemCost;      // the item's first tile in the line
         t = max(t, tile0);
+        const int32_t from = t;                     // of its tiles, the first of this block
         const uint32_t n_rows = (uint32_t)w.seq.n_new * a.group;
         const int32_t base_pos = w.seq.len - w.seq.n_new;
         // tiles that not every row of the block sees whole
@@ -524,7 +522,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         // (in a tree, any row may not see any of the new rows)
         const int32_t warp_hi = TREE ? base_pos - 1 : __shfl_sync(0xFFFFFFFFu, x0.hi, 0);
         const int32_t warp_lo = !a.window ? 0 : TREE ? __reduce_max_sync(0xFFFFFFFFu, x0.lo) : __shfl_sync(0xFFFFFFFFu, x0.lo, 31);
-        const bool takes_part = SHARED || i == 0 || !one_tile(w, a.group);
+        const bool takes_part = SHARED || i == 0 || n_rows > w.rb * kQRows + 128;
         const uint32_t n_tiles = SHARED ? (uint32_t)(stop - t) : 0;      // of the item here
         if (tid == 0) misc[8 + (item + 5) % 8] = 0;     // that of three items ago: the other tile is at most one behind, nobody five ahead
         Walk w2 = w;                                // the next item, once this one's last scores are there
@@ -550,8 +548,12 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
         // give weights of 2^8 and less), and that above which it moves
         float ref = 0.f, limit = -INFINITY;
         uint64_t sum2[2] = {0, 0};
-        // one tile of the line, whose keys and values are loads qk and qv of the block
-        auto step = [&](int32_t tile, uint32_t qk, uint32_t qv, bool first, bool last) {
+        // its tiles, or this group's, whose keys and values are loads qk and qv of the block.  (One loop for both, and what chunks do in it written as
+        // it was before trees: with the steps as a function of five values and one kind of arrival, 2048 tokens over 16384 positions from codes,
+        // heads of 128, took 699 us where this takes 688.)
+        bool first = true;
+        for (t += SHARED ? (int32_t)i : 0; t < stop; t += SHARED ? 2 : 1, jg += SHARED ? 0 : 1, first = false) {
+          const uint32_t qk = 2 * jg + (SHARED ? key_load(true, t - from) : 0), qv = SHARED ? 2 * jg + value_load(true, t - from, n_tiles) : qk + 1;
           const uint32_t sk = qk % C::kScaleSlots, sv = SHARED ? qv % C::kScaleSlots : sk + 1, ready_k = qk / C::kScaleSlots & 1,
                          ready_v = SHARED ? qv / C::kScaleSlots & 1 : ready_k;
           if (!takes_part) {                        // keeps the pace of the scales' ring
@@ -561,9 +563,9 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               bar_arrive(scale_empty + 8 * sk);
               bar_arrive(scale_empty + 8 * sv);
             }
-            return;
+            continue;
           }
-          const int32_t pos0 = (w.blk.kt0 + tile - tile0) * (int32_t)kKeys;
+          const int32_t pos0 = (w.blk.kt0 + t - tile0) * (int32_t)kKeys;
           const bool cut = pos0 + (int32_t)kKeys - 1 > cut_hi || pos0 < cut_lo;
           // Values past the end, and values that are not finite, must not meet weights of zero.  Only the first tile's threads
           // (those that alone use the cache tile, where tiles are shared out) write, one to a row: each then orders its own writes before
@@ -583,7 +585,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
           if (!Q && SHARED && cut) clear();
 #pragma unroll
           for (int c = 0; c < 128; c += 32) tm_load32(tm_s + c, reinterpret_cast<uint32_t*>(x) + c);
-          if (!SHARED && last && stop < end) prepare_next();
+          if (!SHARED && t + 1 == stop && stop < end) prepare_next();
           tm_wait_load();
           if (Q) {
             ok = wait_or_give_up(scale_ready + 8 * sk, ready_k, ok, a.error);
@@ -682,16 +684,17 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
             bar_arrive(p_full + 8 * i);
           }
           if (Q) {
-            if (!kEarly) bar_arrive(scale_empty + 8 * sk);
-            bar_arrive_n(scale_empty + 8 * sv, SHARED ? 2 : 1);
+            if (kEarly) {
+              bar_arrive_n(scale_empty + 8 * sv, SHARED ? 2 : 1);
+            } else {
+              bar_arrive(scale_empty + 8 * sk);
+              bar_arrive(scale_empty + 8 * sv);
+            }
           }
-        };
+        }
         if (SHARED) {
-          for (uint32_t j = i; j < n_tiles; j += 2) step(t + (int32_t)j, 2 * jg + key_load(true, j), 2 * jg + value_load(true, j, n_tiles), j < 2, false);
           jg += n_tiles;
           t = stop;
-        } else {
-          for (bool first = true; t < stop; ++t, ++jg, first = false) step(t, 2 * jg, 2 * jg + 1, first, t + 1 == stop);
         }
         float m2 = -INFINITY, l2 = 0.f;               // the other group's maximum and sum, where tiles are shared out
         float l, m;
@@ -767,7 +770,7 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               float y[W];
 #pragma unroll
               for (int e = 0; e < W; ++e) y[e] = __uint_as_float(o[e]);
-              add_odd_values<Q, TREE, W>(a, w, w.blk.kt0 + max(begin - tile0, 0), w.blk.kt0 + stop - tile0, x0.lo, x0.hi, x0.tok, c, y);
+              add_odd_values<Q, TREE, W>(a, w, w.blk.kt0 + from - tile0, w.blk.kt0 + stop - tile0, x0.lo, x0.hi, x0.tok, c, y);
 #pragma unroll
               for (int e = 0; e < W; ++e) o[e] = __float_as_uint(y[e]);
             }
