@@ -362,6 +362,23 @@ class AttendWorkspace:
         wb.wb_kv_attend_check(self.pointer, _stream(self.device.index))
 
 
+def _check_verify(target: torch.Tensor, draft: Optional[torch.Tensor], uniform: torch.Tensor, race: torch.Tensor, dev: torch.device,
+                  n: int, total: int, vocab: int, rows: str) -> None:
+    """What both verifications want of the probabilities and variates: `total` drafted rows (`rows` in messages), `n` sequences."""
+    if _grad_enabled():
+        for t, name in ((target, "target"), (draft, "draft"), (race, "race"), (uniform, "uniform")):
+            if t is not None:
+                _no_gradient(t, name)
+    if target.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"probabilities of {target.dtype}: float32 or bfloat16")
+    if draft is not None and (draft.shape != (total, vocab) or draft.dtype != target.dtype or draft.device != dev or (draft.stride(1) != 1 and vocab != 1)):
+        raise ValueError(f"draft: [{rows}, vocab] of the target's type")
+    if uniform.shape != (total,) or uniform.dtype != torch.float32 or uniform.device != dev or not uniform.is_contiguous():
+        raise ValueError(f"uniform: fp32 [{rows}]")
+    if race.shape != (n, vocab) or race.dtype != torch.float32 or race.device != dev or (race.stride(1) != 1 and vocab != 1):
+        raise ValueError("race: fp32 [n_seqs, vocab]")
+
+
 def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tokens: torch.Tensor, draft_start: torch.Tensor,
                   uniform: torch.Tensor, race: torch.Tensor, *, max_drafts: int):
     """Accept or reject drafted tokens against the target's probabilities and draw the token after them.
@@ -376,18 +393,7 @@ def verify_drafts(target: torch.Tensor, draft: Optional[torch.Tensor], draft_tok
     if not target.is_cuda or n < 0 or target.shape[0] != total + n or (target.stride(1) != 1 and vocab != 1):
         raise ValueError("target: [n_drafts + n_seqs, vocab] with contiguous rows on a CUDA device")
     _on_device(dev.index)
-    if _grad_enabled():
-        for t, name in ((target, "target"), (draft, "draft"), (race, "race"), (uniform, "uniform")):
-            if t is not None:
-                _no_gradient(t, name)
-    if target.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"probabilities of {target.dtype}: float32 or bfloat16")
-    if draft is not None and (draft.shape != (total, vocab) or draft.dtype != target.dtype or draft.device != dev or (draft.stride(1) != 1 and vocab != 1)):
-        raise ValueError("draft: [n_drafts, vocab] of the target's type")
-    if uniform.shape != (total,) or uniform.dtype != torch.float32 or uniform.device != dev or not uniform.is_contiguous():
-        raise ValueError("uniform: fp32 [n_drafts]")
-    if race.shape != (n, vocab) or race.dtype != torch.float32 or race.device != dev or (race.stride(1) != 1 and vocab != 1):
-        raise ValueError("race: fp32 [n_seqs, vocab]")
+    _check_verify(target, draft, uniform, race, dev, n, total, vocab, "n_drafts")
     if not draft_tokens.is_contiguous() or not draft_start.is_contiguous():
         raise ValueError("draft_tokens, draft_start: contiguous")
     _ints(draft_tokens, "draft_tokens", dev)
@@ -416,18 +422,7 @@ def verify_tree(tree: DraftTree, target: torch.Tensor, draft: Optional[torch.Ten
         raise ValueError(f"target: [n_tokens, vocab] with contiguous rows on {dev}")
     vocab = target.shape[1]
     _on_device(dev.index)
-    if _grad_enabled():
-        for t, name in ((target, "target"), (draft, "draft"), (race, "race"), (uniform, "uniform")):
-            if t is not None:
-                _no_gradient(t, name)
-    if target.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"probabilities of {target.dtype}: float32 or bfloat16")
-    if draft is not None and (draft.shape != (total, vocab) or draft.dtype != target.dtype or draft.device != dev or (draft.stride(1) != 1 and vocab != 1)):
-        raise ValueError("draft: [n_tokens, vocab] of the target's type")
-    if uniform.shape != (total,) or uniform.dtype != torch.float32 or uniform.device != dev or not uniform.is_contiguous():
-        raise ValueError("uniform: fp32 [n_tokens]")
-    if race.shape != (n, vocab) or race.dtype != torch.float32 or race.device != dev or (race.stride(1) != 1 and vocab != 1):
-        raise ValueError("race: fp32 [n_seqs, vocab]")
+    _check_verify(target, draft, uniform, race, dev, n, total, vocab, "n_tokens")
     if tokens.shape != (total,) or not tokens.is_contiguous():
         raise ValueError("tokens: contiguous, [n_tokens]")
     _ints(tokens, "tokens", dev)
