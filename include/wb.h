@@ -761,7 +761,8 @@ wb_status wb_kv_write_rotated(const wb_kv* kv, const wb_kv_batch* batch, const w
 /* wb_kv_attend for trees: row i of a sequence's new tokens sees all positions before them, and of the new rows 0 .. i those whose bit
  * in its row of `mask` is set (itself only if its own is); later rows' bits are not looked at.  A window limits what it sees before
  * the new tokens, by its position: the first new token's place + the number of set bits up to its own - 1.  A window is at least max_new (it
- * cannot end inside a tree).  Everything else is wb_kv_attend's: types, empty rows, limits, workspace, wb_kv_attend_check. */
+ * cannot end inside a tree).  Which kernel serves the batch is decided by max_new and max_len: one tree far larger than the others makes all of them
+ * slower (max_new 0: there is nothing to do).  Everything else is wb_kv_attend's: types, empty rows, limits, workspace, wb_kv_attend_check. */
 wb_status wb_kv_attend_tree(const wb_kv* kv, const wb_kv_batch* batch, const uint32_t* mask, uint32_t words, const wb_heads* q,
                             uint32_t n_heads, const wb_heads* out, float* lse, float scale, uint32_t window, void* workspace,
                             size_t workspace_bytes, void* cuda_stream);

@@ -161,8 +161,12 @@ wb_status attend_args(const wb_kv* kv, const wb_kv_batch* batch, const wb_heads*
 // shares and, beyond 32 rows, cache tiles read once per 32 of them.  Both sides, bf16, heads of 128, cluster | line, us: one sequence, 8 kv
 // heads, 4 rows 1000 positions 8.2 | 9.5, 8000 14.0 | 16.1, 16 thousand 21.1 | 19.0, 30 thousand 33.4 | 31.4; 32 rows 13.3 | 18.5, 23.1 |
 // 34.1, 35.3 | 42.8, 56.0 | 53.0; 128 rows 15.4 | 19.2, 35.1 | 35.9, 59.5 | 42.9; with 4 kv heads, which leaves clusters of 16, 26.0 | 46.1
-// and 41.2 | 47.7 of the latter two.  64 items of 32 rows, 256 and 2000 positions: 14.2 | 13.2 and 25.6 | 23.8;
-// beyond 128 rows, where the other kernel's tiles are not shared out, 49 items of a window of 1000 from codes 16.4 | 25.4.
+// and 41.2 | 47.7 of the latter two.  64 items of 32 rows, 256 and 2000 positions: 14.2 | 13.2 and 25.6 | 23.8.
+// Hence the bounds on items beyond 32 rows.  128 rows, bf16 and E4M3, heads of 128, 300 positions: 40 items 13.6 | 14.9 and 12.1 | 15.9, 48 13.8 | 14.8 and
+// 15.5 | 15.8, 96 17.0 | 14.9 and 18.6 | 15.9; a window of 1000: 40 18.5 | 20.8 and 21.1 | 21.6, 48 19.8 | 20.9 and 22.5 | 21.6, 64 21.4 | 20.0 and
+// 24.0 | 22.1, 72 23.4 | 20.2 and 26.4 | 22.4.  Beyond 128 rows, where the other kernel's tiles are not shared out, 256 rows: 300 positions 48 items 13.9 | 19.4
+// and 16.0 | 20.8, 64 15.8 | 19.6 and 17.3 | 21.0, 96 19.1 | 19.7 and 20.8 | 21.2; 1000 positions 64 20.8 | 22.9 and 22.6 | 25.8, 72 21.5 | 23.2 and 23.5 | 25.9,
+// 96 28.3 | 23.2 and 30.3 | 26.0; the window 64 22.2 | 25.6 and 25.4 | 27.1, 72 23.5 | 25.7 and 26.9 | 27.2.
 constexpr uint32_t kClusterTiles = 16, kClusterTilesWide = 8, kClusterItems = 48, kClusterItemsWide = 64;
 template <int D, bool Q, int NT>
 cudaError_t launch_clusters(AttendArgs a, uint64_t rows, uint32_t max_tiles, bool whole, int dev, cudaStream_t stream, bool& taken) {
@@ -220,7 +224,9 @@ template <bool TREE> wb_status launch_attend(const AttendArgs& a, const wb_kv* k
   }
   // (a batch of trees is of a kind: sequences with few rows go with the others instead of costing two launches of their own)
   const bool mixed = !TREE && batch->n_seqs > 1;
-  // (trees of 17 to 32 rows over a bf16 cache: the second kernel shares their tiles out, 4 sequences of 8000 positions 39.7 us instead of 52)
+  // (trees of 17 to 32 rows over a bf16 cache: the second kernel shares their tiles out, 4 sequences of 8000 positions 39.7 us instead of 52.
+  // Over codes it widens, which takes longer than the row kernel's products: 96 sequences of 1500 positions, 8 kv heads of 128, 20 rows 210 us
+  // instead of 147, heads of 64 141 instead of 94; only of 300 positions 61 instead of 69, heads of 64 53 instead of 45)
   const bool few = rows <= (TREE && !e ? kMaxRows / 2 : kMaxRows);
   if (few || mixed) {
     const uint32_t r = (uint32_t)std::min<uint64_t>(rows, kMaxRows);

@@ -22,7 +22,7 @@
 //   - Work is cut evenly over the SMs whatever the lengths: all (sequence, kv head) items form one line of tiles, every block
 //     takes the same number of consecutive tiles, and a second kernel joins the items that cross blocks, in the order of the
 //     tiles (so results do not depend on timing).
-//   - Few trees are a matter of latency.  A cluster of blocks then serves 32 rows of a (sequence, kv head): each block takes its share of the
+//   - Few trees are a matter of latency.  A cluster of blocks then serves 8, 16 or 32 rows of a (sequence, kv head): each block takes its share of the
 //     cache's tiles, and the cluster joins them over distributed shared memory, without a second kernel.
 #pragma once
 #include <cooperative_groups.h>

@@ -17,13 +17,16 @@
 //   - One warp issues all products in the order  QK0 QK1 | PV0 QK0' PV1 QK1' | ..., one requests cache tiles into a
 //     ring of slots (keys, values, keys, ...) by tensor-map loads, a box per page piece and lane.
 //   - E4M3 caches: tiles arrive as codes, four more warps widen them to bf16 slots; the row scales multiply scores and
-//     weights in the softmax, where each is a value of its own.  This takes 692 us where bf16 takes 430 (tensor core 36 % busy,
+//     weights in the softmax, where each is a value of its own.  This takes 688 us where bf16 takes 423 (tensor core 36 % busy,
 //     issue slots 45 %, ALU 32 %): the step's chain is a microsecond longer, by the scales' loads, products and barriers, and by the
 //     widening warps' share of the schedulers; 616 us with nothing widened, 530 without scales as well.
 //   - Trees of at most 128 rows each have one tile of rows, with which half of the block would idle.  Both groups of softmax warps then hold the
-//     same rows and take every other cache tile, so that the loads are the bound: 1.35 us a tile and SM, 6.5 TB/s of a bf16 cache (E4M3 1.7
-//     to 1.8, widening).  24 trees of 9 to 27 rows of 4 heads over 300 to 6000 positions: 80 to 88 us, of which the cache's bytes are 51, the rest
-//     set-up, 2 to 3 changes of items per block and the join.
+//     same rows and take every other cache tile, so that the loads are the bound: 1.33 us a tile and SM with pages of 128 positions, 1.5 with pages of
+//     32, of a bf16 cache with heads of 128, 7.3 and 6.4 TB/s (differences of lengths; E4M3 1.8 and 2.0, widening; heads of 64 1.1 and 1.3, E4M3
+//     1.7 and 2.0).  24 trees of 9 to 27 rows of 4 heads over 300 to 6000 positions: 80 to 88 us, of which the cache's bytes are 51, the rest
+//     set-up, 2 to 3 changes of items per block and the join; over codes 128, where the bytes are 27.
+//     The whole batch has to be so (its max_new says it): the same kernel's form for any trees takes 76 us instead of 67 for 24 trees of 20 rows of 4
+//     heads over 3000 positions, 123 instead of 111 from codes.
 //   - Work is cut as in the kernel for few rows: one line of 128-row tiles over all (sequence, kv head, row block)
 //     items, an equal share for every SM; a second kernel joins the cut items.
 #pragma once
@@ -597,8 +600,8 @@ wb_attend_tiles_kernel(const __grid_constant__ AttendArgs a, const __grid_consta
               unpack2(mul2(pack2(x[c + 2], x[c + 3]), f.y), x[c + 2], x[c + 3]);
             }
             // the keys' scales are done with, and the load that waits for their place can go on a microsecond before the step's end (tiles
-            // shared out: 2.85 -> 2.26 us a tile, the other group's threads do not read them; chunks with heads of 64: 678 -> 575 us for 2048
-            // tokens over 16384 positions, with heads of 128 692 -> 720)
+            // shared out: 2.85 -> 2.26 us a tile, the other group's threads do not read them; chunks with heads of 64: 640 -> 580 us for 2048
+            // tokens over 16384 positions, but seven windowed prompts 87.5 -> 88.3; with heads of 128 688 -> 730)
             if (kEarly) bar_arrive_n(scale_empty + 8 * sk, SHARED ? 2 : 1);
           }
           // masks: a bit per column for both ends at once, in groups of columns that some row of the warp does not see whole

@@ -4,7 +4,7 @@
 // of the row's own scale.
 //
 // Each element is read once and written once, so the bound is memory bandwidth: 13.7 thousand tokens of 32 query and 8 key heads of 128, bf16 to
-// E4M3, take 58 us, 5.3 TB/s.  (With the next row in registers 72 us, with blocks that look 8 tokens up and end 82: latency, not
+// E4M3, take 59 to 61 us, 5.1 to 5.2 TB/s, into a bf16 cache 62.6, 5.4 TB/s.  (With the next row in registers 72 us, with blocks that look 8 tokens up and end 82: latency, not
 // bytes, was what they waited for.)  A thread has 32 elements of a row, as four
 // pieces of 8 that lie so that both elements of a pair are in one thread (or in two of one row, where a quarter of the row turns), and
 // their 16 angles at most stay in registers while it goes through the rows of one token: the table is read once per token and
@@ -31,7 +31,7 @@ struct RotateArgs {
   uint32_t slots;            // rows of a token that are worked on at once: a power of two, at most kThreads / (D / 32)
 };
 
-// Rows in flight per thread: 64 KiB a block, three blocks an SM, or of fp32 rows 96 KiB and two.
+// Rows in flight per thread: 64 KiB a block, or of fp32 rows 96 KiB, and two blocks an SM (their registers allow no third).
 template <bool F32> constexpr uint32_t kDepth = F32 ? 3 : 4;
 template <bool F32> constexpr uint32_t kRingBytes = kDepth<F32> * (F32 ? 8 : 4) * kThreads * 16;
 

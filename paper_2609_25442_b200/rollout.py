@@ -279,7 +279,8 @@ class KvCache:
     def attend_tree(self, batch: KvBatch, q: torch.Tensor, tree: "DraftTree", *, workspace: "AttendWorkspace", scale: Optional[float] = None,
                     window: int = 0, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None):
         """attend() for the rows of trees: a row sees all tokens before its sequence's new ones (with window > 0, the latest of
-        them as its depth has it) and its ancestors.  A window is at least the batch's max_new."""
+        them as its depth has it) and its ancestors.  A window is at least the batch's max_new.  The kernel is chosen for the whole batch by max_new and max_len:
+        a tree far larger than the others is better off in a batch of its own."""
         if tree.mask.shape[0] != batch.n_tokens or tree.device != self.device:
             raise ValueError("tree: of the batch's rows, on the cache's device")
         return self._attend(batch, q, workspace, scale, window, out, lse, tree)
